@@ -224,6 +224,10 @@ def prepare(case, seed):
     if c["op"] == "head_token":
         s["cache"] = torch.randn(c["cache"], c["hk"], d, device=DEVICE, generator=g).to(dt)
         s["slots"] = torch.randperm(c["cache"], device=DEVICE, generator=g)[:t].contiguous()
+    if own:         # the layer's settings and table, as a program keeps them
+        from paper_1910_00643_amd import HeadNormRotary
+        s["handle"] = HeadNormRotary(d, s["table"], dtype=c["dtype"], norm=c["norm"], eps=HEAD_EPS,
+                                     interleaved=c["interleaved"], pair_axis=s["pair_axis"])
     return s
 
 
@@ -249,18 +253,15 @@ def run(s):
         return {"out": s["out"]}
     c = s["case"]
     if own:
-        from paper_1910_00643_amd import head_norm_rotary, head_norm_rotary_backward
-        more = {"q_weight": s["wq"], "k_weight": s["wk"], "eps": HEAD_EPS, "norm": c["norm"],
-                "interleaved": c["interleaved"], "pair_axis": s["pair_axis"]}
+        h = s["handle"]
         if op == "head_backward":
-            dq, dk, dwq, dwk = head_norm_rotary_backward(s["gq"], s["gk"], s["q"], s["k"], s["table"],
-                                                         s["positions"], **more)
+            dq, dk, dwq, dwk = h.backward(s["gq"], s["gk"], s["q"], s["k"], s["positions"], s["wq"], s["wk"])
             return {"dq": dq, "dk": dk, **({"dwq": dwq, "dwk": dwk} if c["norm"] else {})}
         if op == "head_token":
-            q, k = head_norm_rotary(s["q"], s["k"], s["table"], s["positions"], k_out=s["cache"],
-                                    k_slots=s["slots"], **more)
+            q, k = h.forward(s["q"], s["k"], s["positions"], s["wq"], s["wk"], k_out=s["cache"],
+                             k_slots=s["slots"])
             return {"q": q, "cache": k}
-        q, k = head_norm_rotary(s["q"], s["k"], s["table"], s["positions"], **more)
+        q, k = h.forward(s["q"], s["k"], s["positions"], s["wq"], s["wk"])
         return {"q": q, "k": k}
     cos, sin = _plain_rows(s)
     if op == "head_backward":
