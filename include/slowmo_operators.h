@@ -1,0 +1,109 @@
+/*
+ * slowmo_operators.h -- C ABI of the operators that a worker's local step needs
+ * around a Transformer's matrices, for one AMD MI355X (gfx950); in the same
+ * library as slowmo.h, with its status codes, element types and conventions:
+ *
+ *  - slowmo_head_norm_rotary and its backward pass: the norm of queries and
+ *    keys for each head with the position rotation in the same pass, for
+ *    positions along one axis (text) or several (time, height, width).
+ *
+ * Conventions
+ *  - Pointers named "device" are HIP device pointers; everything else is host
+ *    memory that may be freed as soon as the call returns.
+ *  - Calls enqueue work on `stream` (a hipStream_t, NULL = the default stream)
+ *    and return without synchronizing; they allocate nothing on the device,
+ *    copy nothing from the host and clear nothing by memset, so they
+ *    may be recorded into a HIP graph.
+ *  - Errors: every entry point returns a slowmo_status; nothing aborts or
+ *    throws.  Arguments are checked before anything is launched;
+ *    slowmo_last_error(NULL) has the message of the last failure on this thread.
+ */
+#ifndef SLOWMO_OPERATORS_H
+#define SLOWMO_OPERATORS_H
+
+#include "slowmo.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- norm of queries and keys for each head, with the position rotation ---- */
+
+#define SLOWMO_MAX_HEAD_DIM 512
+#define SLOWMO_MAX_AXES 4
+
+/* What the heads of one call have in common. */
+typedef struct {
+  int32_t dtype;       /* slowmo_dtype of every element of slowmo_heads */
+  int32_t head_dim;    /* D, 1..SLOWMO_MAX_HEAD_DIM */
+  int32_t rotary_dim;  /* R, even, 0..D: the first R elements of a head are turned */
+  int32_t interleaved; /* pair i is elements (2i, 2i+1) if 1, (i, i + R/2) if 0 */
+  int32_t norm;        /* 1: divide by sqrt(mean(x^2) + eps) and multiply by the weight; 0: turn only */
+  float eps;           /* >= 0 */
+  int32_t n_axes;      /* 1..SLOWMO_MAX_AXES */
+  const uint8_t *pair_axis; /* host: the axis (0..n_axes-1) of each of the R/2 pairs; NULL: axis 0 */
+  const float *q_weight;    /* device, D floats; NULL: ones */
+  const float *k_weight;
+  const float *table;       /* device, [table_rows][2][R/2]: cos, then sin, of the angle of a pair at a
+                               position; 4-byte aligned */
+  int64_t table_rows;
+  const int64_t *positions; /* device, [n_axes][tokens]: row of the table for each axis and token; -1: the
+                               axis's pairs are not turned.  Any other place outside the table gives
+                               NaN in the axis's pairs and nothing else */
+  int64_t position_stride;  /* elements from one axis to the next */
+} slowmo_head_config;
+
+/* A [tokens][heads][D] array; the D elements of a head are contiguous.  Strides in
+ * elements, >= 0; data aligned to its element size. */
+typedef struct {
+  void *data;      /* device; may be NULL if heads == 0 */
+  int32_t heads;   /* >= 0 */
+  int64_t token_stride, head_stride;
+} slowmo_heads;
+
+/*
+ * For every token and every head of q and k,
+ *   x^ = w * x / sqrt(mean(x^2) + eps)           (x^ = x without norm)
+ *   pair (u, v), at the token's position along the pair's axis:
+ *   (u, v) <- (u cos - v sin, u sin + v cos)
+ * in one pass: fp32 inside, one rounding at the end.
+ *   q_out, k_out : as q and k; may be q and k themselves (same data and strides),
+ *                  and must not overlap them otherwise.
+ *   k_slots      : device, `tokens` entries, or NULL.  Token t's keys go to row
+ *                  k_slots[t] of k_out, which has k_rows rows (a cache); to no
+ *                  row where the entry lies outside 0..k_rows-1.  Entries inside
+ *                  must differ.  k_rows is ignored without k_slots.
+ * Errors: ARG, ALIGN, HIP.
+ */
+slowmo_status slowmo_head_norm_rotary(const slowmo_head_config *cfg, int64_t tokens,
+                                      const slowmo_heads *q, const slowmo_heads *k,
+                                      const slowmo_heads *q_out, const slowmo_heads *k_out,
+                                      const int64_t *k_slots, int64_t k_rows, void *stream);
+
+/*
+ * The gradient of slowmo_head_norm_rotary (without slots) for q, k and the weights.
+ * With g the output's gradient turned back and x^ = x / sqrt(mean(x^2) + eps):
+ *   dx = (g w - x^ mean(g w x^)) / sqrt(mean(x^2) + eps),   dw = sum over tokens and heads of g x^
+ * (dx = g without norm).
+ *   gq, gk : gradients of q_out and k_out
+ *   q, k   : the inputs of the forward call
+ *   dq, dk : written; may be gq, gk (same data and strides)
+ *   dq_weight, dk_weight : device, D floats each; NULL: not wanted (must be NULL
+ *            without norm).  Zeros if there are no tokens or heads.
+ *   workspace : device, 16-byte aligned, slowmo_head_backward_bytes() long; NULL if
+ *            that is 0.  Sums run in an order fixed by the sizes.
+ * Errors: ARG, ALIGN, NOMEM (workspace too small), HIP.
+ */
+size_t slowmo_head_backward_bytes(const slowmo_head_config *cfg, int64_t tokens, int32_t q_heads,
+                                  int32_t k_heads);
+slowmo_status slowmo_head_norm_rotary_backward(const slowmo_head_config *cfg, int64_t tokens,
+                                               const slowmo_heads *gq, const slowmo_heads *gk,
+                                               const slowmo_heads *q, const slowmo_heads *k,
+                                               const slowmo_heads *dq, const slowmo_heads *dk,
+                                               float *dq_weight, float *dk_weight, void *workspace,
+                                               size_t workspace_bytes, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SLOWMO_OPERATORS_H */

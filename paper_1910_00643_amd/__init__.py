@@ -19,4 +19,7 @@ def __getattr__(name):          # torch is imported only when the holder is used
     if name in ("SlowMo", "make_config"):
         from . import optimizer
         return getattr(optimizer, name)
+    if name in ("Orthogonalizer", "HeadNormRotary", "rotary_table"):
+        from . import operators
+        return getattr(operators, name)
     raise AttributeError(name)

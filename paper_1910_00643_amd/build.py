@@ -8,8 +8,10 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslowmo.so")
-SOURCES = ["slowmo_kernels.hip", "slowmo_api.cpp", "slowmo_plan.cpp"]
-HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", os.path.join("..", "..", "include", "slowmo.h")]
+SOURCES = ["slowmo_kernels.hip", "slowmo_heads.hip", "slowmo_api.cpp", "slowmo_plan.cpp"]
+HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", "slowmo_status.h",
+           os.path.join("..", "..", "include", "slowmo.h"),
+           os.path.join("..", "..", "include", "slowmo_operators.h")]
 
 # -ffp-contract=off: every product and sum rounds on its own, in source order
 # (the order of the paper's formulas); the packed-fp32 feature is disabled.

@@ -16,6 +16,7 @@
 #include "../../include/slowmo.h"
 #include "slowmo_kernels.h"
 #include "slowmo_plan.h"
+#include "slowmo_status.h"
 
 using namespace slowmo;
 
@@ -318,6 +319,30 @@ slowmo_status fail_hip(slowmo_ctx *ctx, hipError_t e, const char *what) {
   return fail(ctx, SLOWMO_ERR_HIP,
               std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
 }
+
+}  // namespace
+
+namespace slowmo {
+// For the entry points in other files; a message that no memory is left for is dropped.
+slowmo_status fail_thread(slowmo_status st, const char *msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {
+    g_err.clear();
+  }
+  return st;
+}
+slowmo_status fail_thread_hip(hipError_t e, const char *what) noexcept {
+  try {
+    return fail_hip(nullptr, e, what);
+  } catch (...) {
+    g_err.clear();
+    return SLOWMO_ERR_HIP;
+  }
+}
+}  // namespace slowmo
+
+namespace {
 
 // Every kernel launch of a context goes through here (see fail_launch_at).
 template <typename F>

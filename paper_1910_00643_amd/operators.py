@@ -1,0 +1,215 @@
+"""Operators of a worker's local step for callers that keep their tensors in
+PyTorch: a thin holder around include/slowmo_operators.h.  PyTorch supplies
+device memory and the stream; all arithmetic on elements runs in libslowmo.so.
+
+    Orthogonalizer   -- updates orthogonalised by Newton-Schulz products, alone or
+                        behind the momentum of the SGD row of Table C.1
+    HeadNormRotary   -- the norm of queries and keys for each head and the position
+                        rotation, one pass, with its gradient
+    rotary_table     -- the table of angles the rotation reads
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as B
+from .optimizer import _DTYPE, _TORCH_GRAD, _raw_stream
+
+SLOWMO_MAX_HEAD_DIM, SLOWMO_MAX_AXES, SLOWMO_MAX_ORTH_STEPS = 512, 4, 16
+_SCALE = {"none": 0, "shape": 1, "rms": 2}
+
+# every symbol include/slowmo_operators.h declares
+EXPORTS = ["slowmo_head_norm_rotary", "slowmo_head_norm_rotary_backward", "slowmo_head_backward_bytes"]
+
+
+class slowmo_head_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float),
+                ("n_axes", C.c_int32), ("pair_axis", C.c_void_p), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("table", C.c_void_p), ("table_rows", C.c_int64),
+                ("positions", C.c_void_p), ("position_stride", C.c_int64)]
+
+
+class slowmo_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("heads", C.c_int32), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class slowmo_orth_config(C.Structure):
+    _fields_ = [("in_dtype", C.c_int32), ("out_dtype", C.c_int32), ("steps", C.c_int32),
+                ("scale", C.c_int32), ("eps", C.c_float), ("coefficients", C.POINTER(C.c_float))]
+
+
+_declared = None
+
+
+def lib() -> C.CDLL:
+    """The library with the operators' entry points declared."""
+    global _declared
+    if _declared is not None:
+        return _declared
+    L = B.lib()
+    vp, i32, i64, size = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    cfg, heads = C.POINTER(slowmo_head_config), C.POINTER(slowmo_heads)
+    L.slowmo_head_norm_rotary.argtypes = [cfg, i64, heads, heads, heads, heads, vp, i64, vp]
+    L.slowmo_head_norm_rotary_backward.argtypes = [cfg, i64, heads, heads, heads, heads, heads, heads,
+                                                   vp, vp, vp, size, vp]
+    L.slowmo_head_backward_bytes.argtypes = [cfg, i64, i32, i32]
+    L.slowmo_head_backward_bytes.restype = size
+    if hasattr(L, "slowmo_orth_bytes"):
+        ocfg, list64, ptrs = C.POINTER(slowmo_orth_config), C.POINTER(i64), C.POINTER(vp)
+        L.slowmo_orth_bytes.argtypes = [ocfg, i32, list64, list64, list64]
+        L.slowmo_orth_bytes.restype = size
+        L.slowmo_orth_create.argtypes = [C.POINTER(vp), ocfg, i32, list64, list64, list64, vp, size, vp]
+        L.slowmo_orthogonalize.argtypes = [vp, ptrs, ptrs, vp]
+        L.slowmo_momentum_orthogonalize.argtypes = [vp, ptrs, ptrs, ptrs, C.c_float, i32, vp]
+        L.slowmo_orth_destroy.argtypes = [vp]
+    _declared = L
+    return L
+
+
+def _check(status: int) -> None:
+    if status != B.SLOWMO_OK:
+        raise B.SlowMoError(status, B.slowmo_last_error(None))
+
+
+# ---- norm of queries and keys with the position rotation ------------------------
+
+def rotary_table(rows: int, pairs, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """cos and sin of (position * base^(-i / n)) for positions 0..rows-1, as [rows, 2, pairs]
+    fp32, computed in 64 bits.  `pairs`: the number of pairs, or, for several axes, how many
+    each axis has: every axis then has frequencies of its own (i from 0 to n - 1)."""
+    sections = [pairs] if isinstance(pairs, int) else list(pairs)
+    freq = torch.cat([float(base) ** (-torch.arange(n, dtype=torch.float64) / n) for n in sections])
+    angle = torch.arange(rows, dtype=torch.float64, device=device)[:, None] * freq.to(device)
+    return torch.stack([angle.cos(), angle.sin()], 1).float().contiguous()
+
+
+class HeadNormRotary:
+    """The norm of queries and keys for each head and the position rotation.
+
+    head_dim    -- elements of a head
+    table       -- rotary_table(...), [rows, 2, pairs] fp32 on the GPU: the first 2 * pairs elements
+                   of a head are turned; None: no rotation
+    dtype       -- "bf16" or "f32": of queries, keys, results and their gradients
+    norm, eps   -- whether to divide by sqrt(mean(x^2) + eps) and multiply by the weights
+    interleaved -- pair i is elements (2i, 2i + 1); else (i, i + pairs)
+    pair_axis   -- the axis of positions that each pair belongs to; None: one axis
+
+    Queries and keys are [tokens, heads, head_dim] (or with more leading dimensions that
+    flatten without a copy), each head's elements contiguous, other strides free.
+    `positions` is int64, [tokens] or [axes, tokens]: rows of the table, -1 for no turn."""
+
+    def __init__(self, head_dim: int, table: Optional[torch.Tensor] = None, *, dtype: str = "bf16",
+                 norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
+                 pair_axis: Optional[Sequence[int]] = None):
+        pairs = 0
+        if table is not None:
+            assert table.dtype == torch.float32 and table.is_contiguous() and table.is_cuda
+            assert table.dim() == 3 and table.shape[1] == 2
+            pairs = table.shape[2]
+        assert pair_axis is None or len(pair_axis) == pairs
+        self.table, self.dtype, self.norm = table, _TORCH_GRAD[dtype], bool(norm)
+        self.head_dim, self.pairs = int(head_dim), pairs
+        self._axis = None if pair_axis is None else (C.c_uint8 * max(pairs, 1))(*pair_axis)
+        self._fixed = dict(dtype=_DTYPE[dtype], head_dim=head_dim, rotary_dim=2 * pairs,
+                           interleaved=int(interleaved), norm=int(norm), eps=eps,
+                           pair_axis=C.addressof(self._axis) if self._axis is not None else None,
+                           table=table.data_ptr() if table is not None else None,
+                           table_rows=table.shape[0] if table is not None else 0)
+
+    def _heads(self, x: torch.Tensor, what: str) -> slowmo_heads:
+        assert x.dtype == self.dtype and x.is_cuda, what
+        assert x.dim() == 3 and x.shape[2] == self.head_dim, what
+        st = x.stride()
+        assert st[2] == 1 or self.head_dim == 1 or x.numel() == 0, f"{what}: a head's elements must be contiguous"
+        return slowmo_heads(x.data_ptr() or None, x.shape[1], st[0], st[1])
+
+    def _config(self, positions, tokens, wq, wk) -> slowmo_head_config:
+        for w in (wq, wk):
+            assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.is_cuda
+                                 and w.numel() == self.head_dim), "weights: [head_dim] fp32"
+        cfg = slowmo_head_config(q_weight=wq.data_ptr() if wq is not None else None,
+                                 k_weight=wk.data_ptr() if wk is not None else None,
+                                 n_axes=1, **self._fixed)
+        if self.pairs:
+            assert positions.dtype == torch.int64 and positions.is_cuda
+            if positions.dim() == 2:
+                cfg.n_axes, cfg.position_stride = positions.shape[0], positions.stride(0)
+                if positions.shape[0] == 1:
+                    cfg.position_stride = 0
+            assert positions.shape[-1] == tokens and (tokens < 2 or positions.stride(-1) == 1)
+            cfg.positions = positions.data_ptr() or None
+        return cfg
+
+    @staticmethod
+    def _flat(x):
+        return x if x.dim() == 3 else x.view(-1, x.shape[-2], x.shape[-1])
+
+    def forward(self, q, k, positions=None, q_weight=None, k_weight=None, q_out=None, k_out=None,
+                k_slots=None):
+        """(turned queries, turned keys); written to q_out and k_out where given (they may be q
+        and k).  With k_slots (int64, [tokens]), token t's keys go to row k_slots[t] of k_out,
+        [rows, heads, head_dim], and to none where that lies outside it."""
+        shapes = q.shape, k.shape
+        q, k = self._flat(q), self._flat(k)
+        tokens = q.shape[0]
+        assert k.shape[0] == tokens
+        yq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else self._flat(q_out)
+        yk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else self._flat(k_out)
+        assert yq.shape == q.shape and (k_slots is not None or yk.shape == k.shape)
+        slots = None
+        if k_slots is not None:
+            assert k_out is not None and k_slots.dtype == torch.int64 and k_slots.is_contiguous()
+            assert k_slots.is_cuda and k_slots.numel() == tokens
+            slots = k_slots.data_ptr() or None
+        cfg = self._config(positions, tokens, q_weight, k_weight)
+        _check(lib().slowmo_head_norm_rotary(cfg, tokens, self._heads(q, "q"), self._heads(k, "k"),
+                                             self._heads(yq, "q_out"), self._heads(yk, "k_out"), slots,
+                                             yk.shape[0], _raw_stream(q.device) or None))
+        return (yq.view(shapes[0]) if q_out is None else q_out,
+                yk.view(shapes[1]) if k_out is None else k_out)
+
+    def backward(self, gq, gk, q, k, positions=None, q_weight=None, k_weight=None):
+        """(dq, dk, dq_weight, dk_weight) from the gradients of forward's results and its inputs;
+        the last two are None without the norm."""
+        shapes = q.shape, k.shape
+        gq, gk, q, k = (self._flat(x) for x in (gq, gk, q, k))
+        tokens, dev = q.shape[0], q.device
+        assert gq.shape == q.shape and gk.shape == k.shape and k.shape[0] == tokens
+        dq, dk = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
+        cfg = self._config(positions, tokens, q_weight, k_weight)
+        dwq = dwk = space = None
+        nbytes = 0
+        if self.norm:
+            dwq, dwk = torch.empty(2, self.head_dim, dtype=torch.float32, device=dev)
+            nbytes = lib().slowmo_head_backward_bytes(cfg, tokens, q.shape[1], k.shape[1])
+            space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(lib().slowmo_head_norm_rotary_backward(
+            cfg, tokens, self._heads(gq, "gq"), self._heads(gk, "gk"), self._heads(q, "q"),
+            self._heads(k, "k"), self._heads(dq, "dq"), self._heads(dk, "dk"),
+            dwq.data_ptr() if self.norm else None, dwk.data_ptr() if self.norm else None,
+            space.data_ptr() if nbytes else None, nbytes, _raw_stream(dev) or None))
+        return dq.view(shapes[0]), dk.view(shapes[1]), dwq, dwk
+
+    def __call__(self, q, k, positions=None, q_weight=None, k_weight=None):
+        """forward() that autograd differentiates, for q, k and the weights."""
+        return _HeadNormRotary.apply(self, q, k, positions, q_weight, k_weight)
+
+
+class _HeadNormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, op, q, k, positions, q_weight, k_weight):
+        ctx.op = op
+        ctx.save_for_backward(q, k, positions, q_weight, k_weight)
+        return op.forward(q, k, positions, q_weight, k_weight)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, gq, gk):
+        q, k, positions, wq, wk = ctx.saved_tensors
+        dq, dk, dwq, dwk = ctx.op.backward(gq.contiguous(), gk.contiguous(), q, k, positions, wq, wk)
+        return (None, dq, dk, None, dwq if wq is not None else None, dwk if wk is not None else None)
