@@ -3,6 +3,10 @@
  * around a Transformer's matrices, for one AMD MI355X (gfx950); in the same
  * library as slowmo.h, with its status codes, element types and conventions:
  *
+ *  - slowmo_orthogonalize / slowmo_momentum_orthogonalize: an update, or the
+ *    direction of the SGD row of Table C.1, replaced by (nearly) the closest
+ *    matrix with orthonormal rows or columns, by Newton-Schulz products.  What
+ *    they write is handed to slowmo_local_step as the gradient.
  *  - slowmo_head_norm_rotary and its backward pass: the norm of queries and
  *    keys for each head with the position rotation in the same pass, for
  *    positions along one axis (text) or several (time, height, width).
@@ -12,8 +16,8 @@
  *    memory that may be freed as soon as the call returns.
  *  - Calls enqueue work on `stream` (a hipStream_t, NULL = the default stream)
  *    and return without synchronizing; they allocate nothing on the device,
- *    copy nothing from the host and clear nothing by memset, so they
- *    may be recorded into a HIP graph.
+ *    copy nothing from the host and clear nothing by memset, so all but
+ *    slowmo_orth_create may be recorded into a HIP graph.
  *  - Errors: every entry point returns a slowmo_status; nothing aborts or
  *    throws.  Arguments are checked before anything is launched;
  *    slowmo_last_error(NULL) has the message of the last failure on this thread.
@@ -102,6 +106,77 @@ slowmo_status slowmo_head_norm_rotary_backward(const slowmo_head_config *cfg, in
                                                const slowmo_heads *dq, const slowmo_heads *dk,
                                                float *dq_weight, float *dk_weight, void *workspace,
                                                size_t workspace_bytes, void *stream);
+
+/* ---- orthogonalised updates ------------------------------------------------ */
+
+typedef struct slowmo_orth slowmo_orth; /* opaque */
+
+/* The factor s on the result for a matrix of `rows` by `cols`. */
+typedef enum {
+  SLOWMO_SCALE_NONE = 0,  /* 1 */
+  SLOWMO_SCALE_SHAPE = 1, /* sqrt(max(1, rows / cols)): the same change of outputs for all shapes */
+  SLOWMO_SCALE_RMS = 2    /* 0.2 sqrt(max(rows, cols)): elements as large as Adam's */
+} slowmo_orth_scale;
+
+#define SLOWMO_MAX_ORTH_STEPS 16
+
+typedef struct {
+  int32_t in_dtype;   /* slowmo_dtype of the matrices read */
+  int32_t out_dtype;  /* slowmo_dtype of the results.  It decides how the products are formed: of
+                         11-bit halves for bf16 results, of pairs of halves (22 bits) for fp32 */
+  int32_t steps;      /* Newton-Schulz steps, 1..SLOWMO_MAX_ORTH_STEPS */
+  int32_t scale;      /* slowmo_orth_scale */
+  float eps;          /* added to the Frobenius norm, >= 0 */
+  const float *coefficients; /* host, [steps][3]: a, b, c of every step, finite; NULL: (3.4445, -4.7750, 2.0315) */
+} slowmo_orth_config;
+
+/*
+ * Orthogonalising a list of matrices.  For each one, U with n <= k its shorter and
+ * longer side,
+ *   X_0 = U / (|U|_F + eps)     (as n x k: transposed if it has more rows than columns)
+ *   A = X X^T;   X <- a X + (b A + c A A) X,   `steps` times
+ *   O = s X                     (in U's own orientation)
+ * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN
+ * everywhere.  A handle is made for a list of shapes and keeps a workspace:
+ *   rows, cols : host, n_matrices entries each, >= 0 (an empty matrix is skipped),
+ *                at most 65536 a side
+ *   ld         : host, elements from one row to the next (>= cols), for inputs and
+ *                results alike; NULL: cols
+ *   workspace  : device, 256-byte aligned, at least slowmo_orth_bytes() long; owned by
+ *                the caller, kept until slowmo_orth_destroy.
+ * slowmo_orth_create waits for `stream`; slowmo_orth_bytes returns 0 for bad arguments and is
+ * host-only.  Calls on one handle must be issued on one stream or be ordered by the caller.
+ * Errors: ARG, ALIGN, NOMEM, HIP.
+ */
+size_t slowmo_orth_bytes(const slowmo_orth_config *cfg, int32_t n_matrices, const int64_t *rows,
+                         const int64_t *cols, const int64_t *ld);
+slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cfg,
+                                 int32_t n_matrices, const int64_t *rows, const int64_t *cols,
+                                 const int64_t *ld, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * out[i] <- the orthogonalised in[i].  `in` and `out` are host arrays of n_matrices device
+ * pointers, aligned to their element size; out[i] may be in[i] where the types are the same.
+ * Errors: ARG, ALIGN, HIP.
+ */
+slowmo_status slowmo_orthogonalize(slowmo_orth *h, const void *const *in, void *const *out,
+                                   void *stream);
+
+/*
+ * The same behind the momentum of the SGD row of Table C.1:
+ *   M <- mu M + G,   U = G + mu M (nesterov) or M,   out <- the orthogonalised U.
+ *   momentum : host array of n_matrices device pointers to fp32 matrices (row distance ld), updated
+ *              in place; zeros at the start.
+ *   mu       : 0 <= mu < 1
+ * Errors: ARG, ALIGN, HIP.
+ */
+slowmo_status slowmo_momentum_orthogonalize(slowmo_orth *h, const void *const *grads,
+                                            float *const *momentum, void *const *out, float mu,
+                                            int32_t nesterov, void *stream);
+
+/* Frees the handle's host memory; never the workspace.  NULL is accepted. */
+slowmo_status slowmo_orth_destroy(slowmo_orth *h);
 
 #ifdef __cplusplus
 }

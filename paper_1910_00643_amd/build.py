@@ -8,8 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslowmo.so")
-SOURCES = ["slowmo_kernels.hip", "slowmo_heads.hip", "slowmo_api.cpp", "slowmo_plan.cpp"]
-HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", "slowmo_status.h",
+SOURCES = ["slowmo_kernels.hip", "slowmo_heads.hip", "slowmo_orth.hip", "slowmo_orth.cpp", "slowmo_api.cpp", "slowmo_plan.cpp"]
+HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", "slowmo_status.h", "slowmo_orth.h",
            os.path.join("..", "..", "include", "slowmo.h"),
            os.path.join("..", "..", "include", "slowmo_operators.h")]
 

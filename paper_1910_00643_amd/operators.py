@@ -22,7 +22,9 @@ SLOWMO_MAX_HEAD_DIM, SLOWMO_MAX_AXES, SLOWMO_MAX_ORTH_STEPS = 512, 4, 16
 _SCALE = {"none": 0, "shape": 1, "rms": 2}
 
 # every symbol include/slowmo_operators.h declares
-EXPORTS = ["slowmo_head_norm_rotary", "slowmo_head_norm_rotary_backward", "slowmo_head_backward_bytes"]
+EXPORTS = ["slowmo_head_norm_rotary", "slowmo_head_norm_rotary_backward", "slowmo_head_backward_bytes",
+           "slowmo_orth_bytes", "slowmo_orth_create", "slowmo_orthogonalize",
+           "slowmo_momentum_orthogonalize", "slowmo_orth_destroy"]
 
 
 class slowmo_head_config(C.Structure):
@@ -59,14 +61,13 @@ def lib() -> C.CDLL:
                                                    vp, vp, vp, size, vp]
     L.slowmo_head_backward_bytes.argtypes = [cfg, i64, i32, i32]
     L.slowmo_head_backward_bytes.restype = size
-    if hasattr(L, "slowmo_orth_bytes"):
-        ocfg, list64, ptrs = C.POINTER(slowmo_orth_config), C.POINTER(i64), C.POINTER(vp)
-        L.slowmo_orth_bytes.argtypes = [ocfg, i32, list64, list64, list64]
-        L.slowmo_orth_bytes.restype = size
-        L.slowmo_orth_create.argtypes = [C.POINTER(vp), ocfg, i32, list64, list64, list64, vp, size, vp]
-        L.slowmo_orthogonalize.argtypes = [vp, ptrs, ptrs, vp]
-        L.slowmo_momentum_orthogonalize.argtypes = [vp, ptrs, ptrs, ptrs, C.c_float, i32, vp]
-        L.slowmo_orth_destroy.argtypes = [vp]
+    ocfg, list64, ptrs = C.POINTER(slowmo_orth_config), C.POINTER(i64), C.POINTER(vp)
+    L.slowmo_orth_bytes.argtypes = [ocfg, i32, list64, list64, list64]
+    L.slowmo_orth_bytes.restype = size
+    L.slowmo_orth_create.argtypes = [C.POINTER(vp), ocfg, i32, list64, list64, list64, vp, size, vp]
+    L.slowmo_orthogonalize.argtypes = [vp, ptrs, ptrs, vp]
+    L.slowmo_momentum_orthogonalize.argtypes = [vp, ptrs, ptrs, ptrs, C.c_float, i32, vp]
+    L.slowmo_orth_destroy.argtypes = [vp]
     _declared = L
     return L
 
@@ -213,3 +214,105 @@ class _HeadNormRotary(torch.autograd.Function):
         q, k, positions, wq, wk = ctx.saved_tensors
         dq, dk, dwq, dwk = ctx.op.backward(gq.contiguous(), gk.contiguous(), q, k, positions, wq, wk)
         return (None, dq, dk, None, dwq if wq is not None else None, dwk if wk is not None else None)
+
+
+# ---- orthogonalised updates -------------------------------------------------------
+
+class Orthogonalizer:
+    """Orthogonalises a list of matrices by Newton-Schulz products.
+
+    shapes       -- (rows, cols) of every tensor, or (count, rows, cols) for a stack of
+                    matrices (the experts of a layer); convolutions as (outputs, inputs * window)
+    dtype        -- "bf16" or "f32": of the tensors read
+    out_dtype    -- of the results (default: dtype); "bf16": products of halves, "f32": of pairs of halves
+    steps, eps, coefficients -- as in slowmo_orth_config; coefficients: (a, b, c) for all
+                    steps or one such triple for each
+    scale        -- "none", "shape" or "rms" (slowmo_orth_scale)
+    ld           -- elements from one row to the next for each tensor (default: cols)
+
+    Tensors are contiguous (or, with ld, have that row stride and, in a stack, any distance
+    between matrices); the workspace is allocated once, here."""
+
+    def __init__(self, shapes, *, dtype: str = "bf16", out_dtype: Optional[str] = None, steps: int = 5,
+                 eps: float = 1e-7, coefficients=None, scale: str = "none", ld=None, device="cuda"):
+        self.shapes = [tuple(int(v) for v in s) for s in shapes]
+        assert all(len(s) in (2, 3) for s in self.shapes)
+        out_dtype = dtype if out_dtype is None else out_dtype
+        self.dtype, self.out_dtype = _TORCH_GRAD[dtype], _TORCH_GRAD[out_dtype]
+        self.device = torch.device(device)
+        rows, cols, lds = [], [], []
+        for j, s in enumerate(self.shapes):
+            count = s[0] if len(s) == 3 else 1
+            rows += [s[-2]] * count
+            cols += [s[-1]] * count
+            lds += [s[-1] if ld is None or ld[j] is None else int(ld[j])] * count
+        self.ld = [s[-1] if ld is None or ld[j] is None else int(ld[j]) for j, s in enumerate(self.shapes)]
+        self.n_matrices = len(rows)
+        coef = None
+        if coefficients is not None:
+            flat = list(coefficients)
+            triples = [flat] * steps if not isinstance(flat[0], (list, tuple)) else flat
+            assert len(triples) == steps and all(len(t) == 3 for t in triples)
+            coef = (C.c_float * (3 * steps))(*[float(v) for t in triples for v in t])
+        cfg = slowmo_orth_config(in_dtype=_DTYPE[dtype], out_dtype=_DTYPE[out_dtype], steps=steps,
+                                 scale=_SCALE[scale], eps=eps, coefficients=coef)
+        n = max(self.n_matrices, 1)
+        arrays = [(C.c_int64 * n)(*v) for v in (rows, cols, lds)]
+        nbytes = lib().slowmo_orth_bytes(cfg, self.n_matrices, *arrays)
+        if nbytes == 0:
+            raise B.SlowMoError(B.SLOWMO_ERR_ARG, B.slowmo_last_error(None))
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.handle = C.c_void_p()
+            _check(lib().slowmo_orth_create(C.byref(self.handle), cfg, self.n_matrices, *arrays,
+                                            self.workspace.data_ptr(), nbytes,
+                                            torch.cuda.current_stream(self.device).cuda_stream or None))
+
+    def pointer_array(self, tensors, dtype: torch.dtype):
+        """ctypes array of every matrix's address (reusable for the same tensors)."""
+        if len(tensors) != len(self.shapes):
+            raise ValueError(f"{len(self.shapes)} tensors wanted, {len(tensors)} given")
+        flat = []
+        for t, s, ld in zip(tensors, self.shapes, self.ld):
+            if tuple(t.shape) != s or t.dtype != dtype or t.device.type != "cuda":
+                raise ValueError(f"a {dtype} tensor of shape {s} on the GPU is wanted: got {tuple(t.shape)}, "
+                                 f"{t.dtype}, {t.device}")
+            st = t.stride()
+            if t.numel() and (s[-1] > 1 and st[-1] != 1 or s[-2] > 1 and st[-2] != ld):
+                raise ValueError(f"rows must be contiguous and {ld} elements apart: strides are {st}")
+            at = t.data_ptr()
+            if len(s) == 2:
+                flat.append(at if t.numel() else 0)
+            else:
+                step = st[0] * t.element_size()
+                flat += [at + i * step if t.numel() else 0 for i in range(s[0])]
+        return (C.c_void_p * max(len(flat), 1))(*flat)
+
+    def _array(self, tensors, dtype):
+        return tensors if isinstance(tensors, C.Array) else self.pointer_array(tensors, dtype)
+
+    def orthogonalize(self, inputs, out) -> None:
+        """out[i] <- the orthogonalised inputs[i]: lists of tensors, or arrays from
+        pointer_array().  out may be inputs where the types are the same."""
+        _check(lib().slowmo_orthogonalize(self.handle, self._array(inputs, self.dtype),
+                                          self._array(out, self.out_dtype), _raw_stream(self.device) or None))
+
+    def momentum_orthogonalize(self, grads, momentum, out, mu: float, nesterov: bool = True) -> None:
+        """momentum <- mu momentum + grads (fp32, in place); out <- the orthogonalised
+        grads + mu momentum (nesterov) or momentum.  What `out` holds goes to SlowMo.local_step
+        as the gradient, with momentum 0 there."""
+        _check(lib().slowmo_momentum_orthogonalize(
+            self.handle, self._array(grads, self.dtype), self._array(momentum, torch.float32),
+            self._array(out, self.out_dtype), mu, int(nesterov), _raw_stream(self.device) or None))
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            torch.cuda.synchronize(self.device)
+            lib().slowmo_orth_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
