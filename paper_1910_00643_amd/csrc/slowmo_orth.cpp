@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <memory>
 #include <vector>
@@ -19,11 +20,11 @@ struct slowmo_orth {
   Steps steps{};
   std::vector<Matrix> matrices;     // those that are not empty
   std::vector<int32_t> index;       // their places in the caller's list
-  int32_t n_matrices = 0;
+  int32_t n_matrices = 0, tile = 0;
   Call call{};
-  const Item *patches = nullptr, *padded = nullptr, *square = nullptr, *update = nullptr;
+  const Item *patches = nullptr, *padded = nullptr, *gram = nullptr, *square = nullptr, *update = nullptr;
   const int32_t *tiny = nullptr;
-  int32_t n_tiny = 0, n_patches = 0, n_padded = 0, n_square = 0, n_update = 0;
+  int32_t n_tiny = 0, n_patches = 0, n_padded = 0, n_gram = 0, n_square = 0, n_update = 0;
 };
 
 namespace {
@@ -36,12 +37,13 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Everything a handle needs, laid out from the configuration and the shapes alone.
 struct Plan {
+  int32_t tile = 128;
   std::vector<Matrix> matrices;
   std::vector<int32_t> index;
-  std::vector<Item> patches, padded, square, update;
+  std::vector<Item> patches, padded, gram, square, update;
   std::vector<int32_t> tiny;
   size_t tiny_at = 0, matrices_at = 0, addresses_at = 0, squares_at = 0, inverse_at = 0, patches_at = 0, padded_at = 0,
-         square_at = 0, update_at = 0, arena_at = 0, total = 0;
+         gram_at = 0, square_at = 0, update_at = 0, arena_at = 0, total = 0;
 };
 
 const char *check(const slowmo_orth_config *c, int32_t n, const int64_t *rows, const int64_t *cols,
@@ -73,10 +75,59 @@ float factor(const slowmo_orth_config &c, int64_t rows, int64_t cols) {
                                                             : 0.2 * std::sqrt(std::max(r, k)));
 }
 
+// Tiles of a grid in blocks of 4 x 8, which 32 neighbouring workgroups share factors in.
+template <typename F>
+void walk(int32_t down, int32_t across, F &&f) {
+  for (int32_t a0 = 0; a0 < down; a0 += 4)
+    for (int32_t b0 = 0; b0 < across; b0 += 8)
+      for (int32_t a = a0; a < std::min(down, a0 + 4); ++a)
+        for (int32_t b = b0; b < std::min(across, b0 + 8); ++b) f(a, b);
+}
+
+// Workgroups go to the 8 dies in turn: of every 256, each die gets 32 neighbours of the list.
+std::vector<Item> spread(const std::vector<Item> &v) {
+  std::vector<Item> out(v.size());
+  for (size_t base = 0; base < v.size(); base += 256) {
+    const size_t count = std::min<size_t>(256, v.size() - base), each = count / 8, more = count % 8;
+    for (size_t b = 0; b < count; ++b) {
+      const size_t die = b % 8;
+      out[base + b] = v[base + die * each + std::min(die, more) + b / 8];
+    }
+  }
+  return out;
+}
+
+// The products' workgroups, those of long sums first.
+void order(Plan &p) {
+  std::vector<int32_t> by(p.matrices.size());
+  for (size_t i = 0; i < by.size(); ++i) by[i] = static_cast<int32_t>(i);
+  auto grams = by, updates = by;
+  std::stable_sort(grams.begin(), grams.end(), [&](int32_t a, int32_t b) { return p.matrices[a].kp > p.matrices[b].kp; });
+  std::stable_sort(updates.begin(), updates.end(), [&](int32_t a, int32_t b) { return p.matrices[a].np > p.matrices[b].np; });
+  std::vector<Item> gram, square, update;
+  for (int32_t at : grams) {
+    const int32_t n = p.matrices[at].np / p.tile;
+    walk(n, n, [&](int32_t i, int32_t j) {
+      if (j <= i) gram.push_back({at, i, j, 0});
+    });
+  }
+  for (int32_t at : updates) {
+    const int32_t n = p.matrices[at].np / p.tile, k = p.matrices[at].kp / p.tile;
+    walk(n, n, [&](int32_t i, int32_t j) {
+      if (j <= i) square.push_back({at, i, j, 0});
+    });
+    walk(n, k, [&](int32_t i, int32_t j) { update.push_back({at, i, j, 0}); });
+  }
+  p.gram = spread(gram);
+  p.square = spread(square);
+  p.update = spread(update);
+}
+
 Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, const int64_t *cols,
           const int64_t *ld) {
   Plan p;
   const bool split = c.out_dtype == SLOWMO_F32;
+  if (const char *force = std::getenv("SLOWMO_ORTH_TILE")) p.tile = std::atoi(force);
   int64_t halves = 0;
   auto take = [&](int64_t count) {
     const int64_t at = halves;
@@ -98,19 +149,17 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
       p.index.push_back(i);
       continue;
     }
-    m.np = static_cast<int32_t>(up(m.n, kTile));
-    m.kp = static_cast<int32_t>(up(m.k, kTile));
+    m.np = static_cast<int32_t>(up(m.n, p.tile));
+    m.kp = static_cast<int32_t>(up(m.k, p.tile));
     m.ld = ld ? ld[i] : cols[i];
     m.scale = factor(c, rows[i], cols[i]);
     const int64_t wide = static_cast<int64_t>(m.np) * m.kp, square = static_cast<int64_t>(m.np) * m.np;
-    m.x = take(wide);
-    for (int64_t &at : m.xt) at = take(wide);
+    for (int64_t &to : m.x) to = take(wide);
     m.a = take(square);
     m.p = take(square);
-    m.xt_lo[0] = take(wide);
+    m.x_lo[0] = take(wide);
     if (split) {
-      m.xt_lo[1] = take(wide);
-      m.x_lo = take(wide);
+      m.x_lo[1] = take(wide);
       m.a_lo = take(square);
       m.p_lo = take(square);
     }
@@ -123,13 +172,10 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     cover(p.patches, rows[i], cols[i]);
     cover(p.padded, m.tall ? m.kp : m.np, m.tall ? m.np : m.kp);
     m.patches = static_cast<int32_t>(p.patches.size()) - m.first_patch;
-    for (int32_t a = 0; a < m.np / kTile; ++a)
-      for (int32_t b = 0; b <= a; ++b) p.square.push_back({at, a, b, 0});
-    for (int32_t a = 0; a < m.kp / kTile; ++a)
-      for (int32_t b = 0; b < m.np / kTile; ++b) p.update.push_back({at, a, b, 0});
     p.matrices.push_back(m);
     p.index.push_back(i);
   }
+  order(p);
   size_t off = 0;
   auto section = [&](size_t bytes) {
     const size_t at = off;
@@ -143,6 +189,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.tiny_at = section(p.tiny.size() * sizeof(int32_t));
   p.patches_at = section(p.patches.size() * sizeof(Item));
   p.padded_at = section(p.padded.size() * sizeof(Item));
+  p.gram_at = section(p.gram.size() * sizeof(Item));
   p.square_at = section(p.square.size() * sizeof(Item));
   p.update_at = section(p.update.size() * sizeof(Item));
   p.arena_at = section(static_cast<size_t>(halves) * sizeof(uint16_t));
@@ -185,14 +232,16 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
     return fail_thread_hip(e, "slowmo_orthogonalize");
   if (h->n_tiny == count) return SLOWMO_OK;
   if (!ok(launch_squares(c, h->patches, h->n_patches, s)) || !ok(launch_norms(c, count, s)) ||
-      !ok(launch_load(c, h->padded, h->n_padded, split, s)))
+      !ok(launch_load(c, h->padded, h->n_padded, s)))
     return fail_thread_hip(e, "slowmo_orthogonalize");
-  for (int32_t t = 0; t < h->cfg.steps; ++t) {
+  for (int32_t t = 0; t < h->steps.count; ++t) {
     const float *k = h->steps.abc[t];
-    const Step st{k[0], k[1], k[2], t & 1, t + 1 == h->cfg.steps};
-    if (!ok(launch_products(c, kGram, st, h->square, h->n_square, split, s)) ||
-        !ok(launch_products(c, kPolynomial, st, h->square, h->n_square, split, s)) ||
-        !ok(launch_products(c, kUpdate, st, h->update, h->n_update, split, s)))
+    // Pairs of halves have bits enough; of single ones the last two steps, whose roundings grow no more.
+    auto carries = [&](int32_t step) { return !split && step < h->steps.count - 2; };
+    const Step st{k[0], k[1], k[2], t & 1, t + 1 == h->steps.count, carries(t), carries(t + 1)};
+    if (!ok(launch_products(c, h->tile, kGram, st, h->gram, h->n_gram, split, s)) ||
+        !ok(launch_products(c, h->tile, kPolynomial, st, h->square, h->n_square, split, s)) ||
+        !ok(launch_products(c, h->tile, kUpdate, st, h->update, h->n_update, split, s)))
       return fail_thread_hip(e, "slowmo_orthogonalize");
   }
   return SLOWMO_OK;
@@ -235,6 +284,9 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
       for (int i = 0; i < 3; ++i)
         h->steps.abc[t][i] = cfg->coefficients ? cfg->coefficients[3 * t + i] : kDefault[i];
     h->n_matrices = n_matrices;
+    h->tile = p.tile;
+    if (hipError_t e = prepare_products(p.tile, cfg->out_dtype == SLOWMO_F32); e != hipSuccess)
+      return fail_thread_hip(e, "slowmo_orth_create");
     h->matrices = p.matrices;
     h->index = p.index;
     char *base = static_cast<char *>(workspace);
@@ -254,6 +306,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     h->n_tiny = static_cast<int32_t>(p.tiny.size());
     items(p.patches_at, p.patches, h->patches, h->n_patches);
     items(p.padded_at, p.padded, h->padded, h->n_padded);
+    items(p.gram_at, p.gram, h->gram, h->n_gram);
     items(p.square_at, p.square, h->square, h->n_square);
     items(p.update_at, p.update, h->update, h->n_update);
     hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here

@@ -11,6 +11,8 @@
 // lo hi, 22 bits.
 #include "slowmo_orth.h"
 
+#include <type_traits>
+
 namespace slowmo {
 namespace orth {
 namespace {
@@ -18,6 +20,7 @@ namespace {
 typedef _Float16 half;
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32;
 
@@ -87,21 +90,16 @@ __global__ __launch_bounds__(256) void k_norms(Call c) {
   c.inverse[blockIdx.x] = norm == 0. ? 0.f : norm < 1.7e308 ? static_cast<float>(1. / norm) : __builtin_nanf("");
 }
 
-// X_0 and its transpose as halves, with zeros in the padding (which an earlier call's NaN may have
-// reached).
-template <bool SPLIT>
+// X_0 (n x k, turned if the caller's matrix is tall) as halves hi and lo, with zeros in the padding (which
+// an earlier call's NaN may have reached).
 __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
   const Addresses at = c.addresses[it.matrix];
   const int rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k;
-  const int prows = m.tall ? m.kp : m.np, pcols = m.tall ? m.np : m.kp;
-  half *natural = c.arena + (m.tall ? m.xt[0] : m.x), *turned = c.arena + (m.tall ? m.x : m.xt[0]);
-  // lo parts: of XT always, of X where products are split
-  half *natural_lo = m.tall ? c.arena + m.xt_lo[0] : SPLIT ? c.arena + m.x_lo : nullptr;
-  half *turned_lo = m.tall ? (SPLIT ? c.arena + m.x_lo : nullptr) : c.arena + m.xt_lo[0];
+  half *x = c.arena + m.x[0], *x_lo = c.arena + m.x_lo[0];
   const float inverse = c.inverse[it.matrix];
-  __shared__ half hi[kPatch][kPatch + 2], lo[kPatch][kPatch + 2];
+  __shared__ float turn[kPatch][kPatch + 1];
   const int lane = threadIdx.x & 63;
   for (int r = threadIdx.x >> 6; r < kPatch; r += 4) {
     const int row = it.i * kPatch + r, col = it.j * kPatch + lane;
@@ -116,169 +114,326 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
       }
       u = u * inverse * kScaleX;
     }
-    split_half(u, hi[r][lane], lo[r][lane]);
-    const int64_t to = static_cast<int64_t>(row) * pcols + col;
-    natural[to] = hi[r][lane];
-    if (natural_lo) natural_lo[to] = lo[r][lane];
+    if (m.tall) {
+      turn[r][lane] = u;
+    } else {
+      const int64_t to = static_cast<int64_t>(row) * m.kp + col;
+      split_half(u, x[to], x_lo[to]);
+    }
   }
+  if (!m.tall) return;
   __syncthreads();
   for (int r = threadIdx.x >> 6; r < kPatch; r += 4) {
-    const int64_t to = static_cast<int64_t>(it.j * kPatch + r) * prows + it.i * kPatch + lane;
-    turned[to] = hi[lane][r];
-    if (turned_lo) turned_lo[to] = lo[lane][r];
+    const int64_t to = static_cast<int64_t>(it.j * kPatch + r) * m.kp + it.i * kPatch + lane;
+    split_half(turn[lane][r], x[to], x_lo[to]);
   }
 }
 
-// C = A B^T over tiles of 128 x 128, 4 waves of 64 x 64.  Both factors lie with the summed side
-// contiguous and padded, so nothing is checked in the loop.  A step of 64 goes from memory straight to
-// shared memory, 16 bytes a lane; there the 16-byte pieces of a row of 128 bytes are placed at
-// (piece xor row mod 8), so that lanes that read the same piece of neighbouring rows meet different banks.
-template <int PHASE, bool SPLIT>
-__global__ __launch_bounds__(256) void k_products(Call c, Step st, const Item *items) {
-  __shared__ half tiles[2][2][kTile * kDepth];
+// 8 neighbouring results of one row of the caller's matrix (rows x cols, ld apart).
+__device__ __forceinline__ void write_out(const Call &c, const Addresses &at, int64_t ld, int row, int rows,
+                                          int col, int cols, const float *v, float scale) {
+  if (row >= rows || col >= cols) return;
+  const int64_t to = row * ld + col;
+  if (c.out_bf16) {
+    uint16_t *o = static_cast<uint16_t *>(at.out) + to;
+    if (col + 8 <= cols && reinterpret_cast<uintptr_t>(o) % 16 == 0) {
+      typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+      bf16x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = static_cast<__bf16>(v[e] * scale);
+      *reinterpret_cast<bf16x8 *>(o) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < cols) o[e] = narrow_bf16(v[e] * scale);
+    }
+  } else {
+    float *o = static_cast<float *>(at.out) + to;
+    if (col + 8 <= cols && reinterpret_cast<uintptr_t>(o) % 16 == 0) {
+      *reinterpret_cast<f32x4 *>(o) = f32x4{v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale};
+      *reinterpret_cast<f32x4 *>(o + 4) = f32x4{v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < cols) o[e] = v[e] * scale;
+    }
+  }
+}
+
+// ---- products -----------------------------------------------------------------
+//
+// Tiles of T x T by 4 waves of T/2 x T/2.  Steps of 32 of the summed side go from memory straight to a
+// ring of kRing stages in shared memory (16 bytes a lane), kRing - 1 steps ahead of their use: memory's
+// latency is 0.7 us and a step's products take 0.25 us (T = 256).  A wave reads the next 16's factors into
+// registers before it issues the products of this 16, across the barrier of a step too, so that with
+// one wave per SIMD (T = 256: 256 accumulators a lane) the matrix cores go on.
+//
+// Rows of 32 halves (both factors contiguous along the summed side: X X^T, A A, and P of P X) are four
+// pieces of 16 bytes; piece p of row r lies at p xor (r / 4 mod 4), so that 16 lanes that read the same
+// piece of neighbouring rows meet all 64 banks once.  X of P X lies with the summed side across: its
+// rows are read turned (4 rows x 16 columns per 16 lanes), with piece p of row r at p xor 4 (r mod 4).
+// Everything is padded to whole tiles; nothing is checked in the loop.
+
+constexpr int kDeep = 32, kRing = 4;
+
+__device__ __forceinline__ void to_shared(u32 shared, u32 offset, const half *base) {
+  // m0 is written and read within this block; the wait covers its hazard and that of a base that a
+  // vector instruction has just brought to scalar registers.  No vector register is written.
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(shared), "v"(offset),
+               "s"(base)
+               : "memory");
+}
+// All but the N newest loads of this wave have arrived, its reads of shared memory are done, and so it is
+// for every wave of the workgroup.
+template <int N>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+
+template <int T, int PHASE, bool SPLIT>
+__global__ __launch_bounds__(256, T == 256 ? 1 : 2) void k_products(Call c, Step st, const Item *items) {
+  extern __shared__ half ring[];
+  constexpr int kBlocks = T / 64;            // blocks of 32 x 32 along a side of a wave's share
+  constexpr int kShare = T * kDeep;          // halves of one factor in a stage
+  constexpr int kLoads = kShare * 2 / 1024 / 4;  // loads of a wave per factor and stage
+  constexpr int kWide = T / 2;               // side of a wave's share
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
-  const int depth = PHASE == kGram ? m.kp : m.np;
-  const int64_t rows_hi = PHASE == kGram ? m.x : PHASE == kPolynomial ? m.a : m.xt[st.from];
-  const int64_t rows_lo = PHASE == kGram ? m.x_lo : PHASE == kPolynomial ? m.a_lo : m.xt_lo[st.from];
-  const int64_t cols_hi = PHASE == kUpdate ? m.p : rows_hi;
-  const int64_t cols_lo = PHASE == kUpdate ? m.p_lo : rows_lo;
-  const int steps = depth / kDepth, total = SPLIT ? 3 * steps : steps;
+  const int wa = wave & 1, wb = wave >> 1;
+  const int low = lane & 31, high = lane >> 5;
+
+  // factor a: columns of the tile (j), factor b: rows (i).  The accumulators' four neighbours run along a.
+  const int depth = PHASE == kGram ? m.kp : m.np, steps = depth / kDeep;
+  const int64_t a_hi = PHASE == kPolynomial ? m.a : m.x[st.from];
+  const int64_t a_lo = PHASE == kPolynomial ? m.a_lo : m.x_lo[st.from];
+  const int64_t b_hi = PHASE == kUpdate ? m.p : a_hi, b_lo = PHASE == kUpdate ? m.p_lo : a_lo;
+  const int64_t a_at = PHASE == kUpdate ? static_cast<int64_t>(it.j) * T : static_cast<int64_t>(it.j) * T * depth;
+  const int64_t b_at = static_cast<int64_t>(it.i) * T * depth;
+  const int64_t a_step = PHASE == kUpdate ? static_cast<int64_t>(kDeep) * m.kp : kDeep;
+  const int total = SPLIT ? 3 * steps : steps;
+
+  u32 a_off[kLoads], b_off[kLoads];          // bytes
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) {
+    const int load = wave * kLoads + q;
+    const int row = load * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 2) & 3);
+    b_off[q] = (row * depth + piece * 8) * 2;
+    if constexpr (PHASE == kUpdate) {
+      constexpr int kAcross = T / 8;         // pieces of a row
+      const int r = load * (64 / kAcross) + lane / kAcross, p = (lane % kAcross) ^ (4 * (r & 3));
+      a_off[q] = (r * m.kp + p * 8) * 2;
+    } else {
+      a_off[q] = b_off[q];
+    }
+  }
+  const u32 shared0 = static_cast<u32>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half *)ring));
 
   auto fetch = [&](int t) {
     // split: the small products first (hi lo, lo hi), while their sums are small, then hi hi
-    const int seg = SPLIT ? t / steps : 2;
-    const int64_t at = static_cast<int64_t>(SPLIT ? t - seg * steps : t) * kDepth;
-    const half *a = c.arena + (seg == 1 ? rows_lo : rows_hi) + static_cast<int64_t>(it.i) * kTile * depth + at;
-    const half *b = c.arena + (seg == 0 ? cols_lo : cols_hi) + static_cast<int64_t>(it.j) * kTile * depth + at;
+    const int seg = SPLIT ? (t >= 2 * steps ? 2 : t >= steps ? 1 : 0) : 2;
+    const int at = SPLIT ? t - seg * steps : t;
+    const half *a = c.arena + (seg == 1 ? a_lo : a_hi) + a_at + at * a_step;
+    const half *b = c.arena + (seg == 0 ? b_lo : b_hi) + b_at + static_cast<int64_t>(at) * kDeep;
+    const u32 slot = shared0 + (t % kRing) * (2 * kShare * 2) + wave * kLoads * 1024;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int row = (wave * 4 + q) * 8 + (lane >> 3);
-      const int piece = (lane & 7) ^ (lane >> 3);
-      const int64_t off = static_cast<int64_t>(row) * depth + piece * 8;
-      half *la = &tiles[t & 1][0][(wave * 4 + q) * 8 * kDepth], *lb = &tiles[t & 1][1][(wave * 4 + q) * 8 * kDepth];
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a + off),
-                                       (__attribute__((address_space(3))) void *)la, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(b + off),
-                                       (__attribute__((address_space(3))) void *)lb, 16, 0, 0);
+    for (int q = 0; q < kLoads; ++q) {
+      to_shared(slot + q * 1024, a_off[q], a);
+      to_shared(slot + kShare * 2 + q * 1024, b_off[q], b);
     }
   };
 
-  f32x16 acc[2][2];
+  half8 fa[2][kBlocks], fb[2][kBlocks];
+  auto read = [&](int t, int kk, half8 *a, half8 *b) {
+    const half *sa = ring + (t % kRing) * 2 * kShare, *sb = sa + kShare;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
-  fetch(0);
-  for (int t = 0; t < total; ++t) {
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();  // this step's tiles are there, and nobody reads the other pair any more
-    half8 fa[4][2], fb[4][2];
-    const half *ta = tiles[t & 1][0], *tb = tiles[t & 1][1];
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int ra = wm * 64 + i * 32 + (lane & 31), rb = wn * 64 + i * 32 + (lane & 31);
-        const int piece = kk * 2 + (lane >> 5);
-        fa[kk][i] = *reinterpret_cast<const half8 *>(ta + ra * kDepth + ((piece ^ (ra & 7)) * 8));
-        fb[kk][i] = *reinterpret_cast<const half8 *>(tb + rb * kDepth + ((piece ^ (rb & 7)) * 8));
+    for (int x = 0; x < kBlocks; ++x) {
+      const int rb = wb * kWide + x * 32 + low;
+      b[x] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+      if constexpr (PHASE == kUpdate) {
+        const int r = kk * 16 + high * 8 + ((lane >> 2) & 3);
+        const int col = wa * kWide + x * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        const int piece = (col >> 3) ^ (4 * (r & 3));
+        const half *from = sa + r * T + piece * 8 + (col & 7);
+        typedef __attribute__((address_space(3))) short4v *shared4;
+        const short4v lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from));
+        const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * T));
+        a[x] = __builtin_bit_cast(half8, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+      } else {
+        const int ra = wa * kWide + x * 32 + low;
+        a[x] = *reinterpret_cast<const half8 *>(sa + ra * kDeep + (((kk * 2 + high) ^ ((ra >> 2) & 3)) * 8));
       }
     }
-    if (t + 1 < total) fetch(t + 1);
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[kk][j], fa[kk][i], acc[i][j], 0, 0, 0);
-  }
+  };
 
-  // A lane holds, of a block of 32 x 32, row (lane & 31) and four times four neighbouring columns.
-  const Addresses at = c.addresses[it.matrix];
+  f32x16 acc[kBlocks][kBlocks];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int x = 0; x < kBlocks; ++x)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int y = 0; y < kBlocks; ++y)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int row = it.i * kTile + wm * 64 + i * 32 + (lane & 31);
-        const int col = it.j * kTile + wn * 64 + j * 32 + g * 8 + (lane >> 5) * 4;
-        float v[4];
+      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
+  auto multiply = [&](const half8 *a, const half8 *b) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][g * 4 + e];
-        const int64_t pos = static_cast<int64_t>(row) * m.np + col;
-        if constexpr (PHASE == kUpdate) {
-          const half4 hi = *reinterpret_cast<const half4 *>(c.arena + m.xt[st.from] + pos);
-          const half4 lo = *reinterpret_cast<const half4 *>(c.arena + m.xt_lo[SPLIT ? st.from : 0] + pos);
-          half4 nh, nl;
+    for (int x = 0; x < kBlocks; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = static_cast<float>(hi[e]) + static_cast<float>(lo[e]);
-            v[e] = fmaf(st.a, x, v[e] * (1.f / kScaleP));
-            half h, l;
-            split_half(v[e], h, l);
-            nh[e] = h;
-            nl[e] = l;
-          }
-          if (!st.last) {
-            *reinterpret_cast<half4 *>(c.arena + m.xt[1 - st.from] + pos) = nh;
-            *reinterpret_cast<half4 *>(c.arena + m.xt_lo[SPLIT ? 1 - st.from : 0] + pos) = nl;
+      for (int y = 0; y < kBlocks; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
+  };
+
+  constexpr int kPending = 2 * kLoads * (kRing - 2);
+  for (int t = 0; t < kRing && t < total; ++t) fetch(t);
+  if (total >= kRing)
+    arrive<kPending + 2 * kLoads>();
+  else
+    arrive<0>();
+  read(0, 0, fa[0], fb[0]);
+  for (int t = 0; t < total; ++t) {
+    read(t, 1, fa[1], fb[1]);
+    multiply(fa[0], fb[0]);
+    if (t + 1 < total) {
+      if (t + kRing <= total)
+        arrive<kPending>();
+      else
+        arrive<0>();
+      if (t + kRing < total) fetch(t + kRing);  // where step t was: everybody has read it
+      read(t + 1, 0, fa[0], fb[0]);
+    }
+    multiply(fa[1], fb[1]);
+  }
+  __syncthreads();
+
+  // The results pass through shared memory, 32 rows of a wave's share at a time, to leave in whole rows.
+  constexpr int kPitch = kWide + 4, kLanes = kWide / 8, kRows = 64 / kLanes;
+  float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
+  const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
+  // rows y of factor b, along a
+  auto direct = [&](int y) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int64_t to = static_cast<int64_t>(col + e) * m.kp + row;
-              c.arena[m.x + to] = nh[e];
-              if (SPLIT) c.arena[m.x_lo + to] = nl[e];
-            }
-          } else {
+    for (int x = 0; x < kBlocks; ++x)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (row >= m.k || col + e >= m.n) continue;
-              const int64_t to = m.tall ? row * m.ld + col + e : (col + e) * m.ld + row;
-              const float o = v[e] * (m.scale / kScaleX);
-              if (c.out_bf16)
-                static_cast<uint16_t *>(at.out)[to] = narrow_bf16(o);
-              else
-                static_cast<float *>(at.out)[to] = o;
-            }
-          }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(stage + low * kPitch + x * 32 + g * 8 + high * 4) =
+            f32x4{acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
+  };
+  // rows x of factor a, along b
+  auto turned = [&](int x) {
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        stage[((r >> 2) * 8 + high * 4 + (r & 3)) * kPitch + y * 32 + low] = acc[x][y][r];
+  };
+  auto take = [&](int r, float *v) {
+    const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + c8),
+                q = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + c8 + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = p[e], v[4 + e] = q[e];
+  };
+  const int ai = it.j * T + wa * kWide, bi = it.i * T + wb * kWide;  // first place along each factor
+
+  if constexpr (PHASE == kUpdate) {
+    const Addresses at = c.addresses[it.matrix];
+    if (st.last && m.tall) {  // the caller's matrix is k x n: rows of factor a
+      const float scale = m.scale / (kScaleX * kScaleP);
+#pragma unroll
+      for (int x = 0; x < kBlocks; ++x) {
+        turned(x);
+#pragma unroll
+        for (int r = 0; r < 32; r += kRows) {
+          float v[8];
+          take(r + sub, v);
+          write_out(c, at, m.ld, ai + x * 32 + r + sub, m.k, bi + c8, m.n, v, scale);
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y) {
+      direct(y);
+#pragma unroll
+      for (int r = 0; r < 32; r += kRows) {
+        const int row = bi + y * 32 + r + sub;
+        float v[8];
+        take(r + sub, v);
+        if (st.last) {
+          write_out(c, at, m.ld, row, m.n, ai + c8, m.k, v, m.scale / (kScaleX * kScaleP));
+          continue;
+        }
+        const int64_t pos = static_cast<int64_t>(row) * m.kp + ai + c8;
+        half8 nh, nl;
+        if (st.carry) {
+          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.x[st.from] + pos);
+          const half8 l = *reinterpret_cast<const half8 *>(c.arena + m.x_lo[0] + pos);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            v[e] = fmaf(st.a, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e] * (1.f / kScaleP));
         } else {
-          half4 nh, nl, ah, al;
-          if constexpr (PHASE == kPolynomial) {
-            ah = *reinterpret_cast<const half4 *>(c.arena + m.a + pos);
-            if (SPLIT) al = *reinterpret_cast<const half4 *>(c.arena + m.a_lo + pos);
-          }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (PHASE == kGram) {
-              v[e] *= kScaleA / (kScaleX * kScaleX);
-            } else {
-              const float x = static_cast<float>(ah[e]) + (SPLIT ? static_cast<float>(al[e]) : 0.f);
-              v[e] = fmaf(st.b * (kScaleP / kScaleA), x, st.c * (kScaleP / (kScaleA * kScaleA)) * v[e]);
-            }
-            half h, l;
-            split_half(v[e], h, l);
-            nh[e] = h;
-            nl[e] = l;
-          }
-          half *to_hi = c.arena + (PHASE == kGram ? m.a : m.p), *to_lo = c.arena + (PHASE == kGram ? m.a_lo : m.p_lo);
-          *reinterpret_cast<half4 *>(to_hi + pos) = nh;
-          if (SPLIT) *reinterpret_cast<half4 *>(to_lo + pos) = nl;
-          if (it.i != it.j) {
+          for (int e = 0; e < 8; ++e) v[e] *= 1.f / kScaleP;
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int64_t to = static_cast<int64_t>(col + e) * m.np + row;
-              to_hi[to] = nh[e];
-              if (SPLIT) to_lo[to] = nl[e];
-            }
+        for (int e = 0; e < 8; ++e) {
+          half h, l;
+          split_half(v[e], h, l);
+          nh[e] = h;
+          nl[e] = l;
+        }
+        *reinterpret_cast<half8 *>(c.arena + m.x[1 - st.from] + pos) = nh;
+        if (SPLIT)
+          *reinterpret_cast<half8 *>(c.arena + m.x_lo[1 - st.from] + pos) = nl;
+        else if (st.carry_next)
+          *reinterpret_cast<half8 *>(c.arena + m.x_lo[0] + pos) = nl;
+      }
+    }
+  } else {
+    half *to_hi = c.arena + (PHASE == kGram ? m.a : m.p), *to_lo = c.arena + (PHASE == kGram ? m.a_lo : m.p_lo);
+    auto rows = [&](int row0, int col0) {  // 32 staged rows of the symmetric result
+#pragma unroll
+      for (int r = 0; r < 32; r += kRows) {
+        const int row = row0 + r + sub, col = col0 + c8;
+        const int64_t pos = static_cast<int64_t>(row) * m.np + col;
+        float v[8];
+        take(r + sub, v);
+        if constexpr (PHASE == kGram) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= kScaleA / (kScaleX * kScaleX);
+        } else {
+          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.a + pos);
+          half8 l;
+          if (SPLIT) l = *reinterpret_cast<const half8 *>(c.arena + m.a_lo + pos);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f);
+            v[e] = fmaf(st.b * (kScaleP / kScaleA), x, st.c * (kScaleP / (kScaleA * kScaleA)) * v[e]);
+            if (!st.carry && row == col + e) v[e] += st.a * kScaleP;
           }
         }
+        half8 nh, nl;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          half h, l;
+          split_half(v[e], h, l);
+          nh[e] = h;
+          nl[e] = l;
+        }
+        *reinterpret_cast<half8 *>(to_hi + pos) = nh;
+        if (SPLIT) *reinterpret_cast<half8 *>(to_lo + pos) = nl;
+      }
+    };
+#pragma unroll
+    for (int y = 0; y < kBlocks; ++y) {
+      direct(y);
+      rows(bi + y * 32, ai);
+    }
+    if (it.i != it.j) {
+#pragma unroll
+      for (int x = 0; x < kBlocks; ++x) {
+        turned(x);
+        rows(ai + x * 32, bi);
       }
     }
   }
@@ -384,26 +539,51 @@ hipError_t launch_norms(const Call &c, int32_t matrices, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_load(const Call &c, const Item *items, int32_t count, bool split, hipStream_t s) {
-  if (split)
-    k_load<true><<<count, 256, 0, s>>>(c, items);
-  else
-    k_load<false><<<count, 256, 0, s>>>(c, items);
+hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStream_t s) {
+  k_load<<<count, 256, 0, s>>>(c, items);
   return hipGetLastError();
 }
 
-hipError_t launch_products(const Call &c, Phase phase, const Step &st, const Item *items, int32_t count,
+namespace {
+template <int T>
+constexpr size_t shared_bytes() {
+  return sizeof(half) * kRing * 2 * T * kDeep;
+}
+
+template <typename F>
+hipError_t with_products(int tile, Phase phase, bool split, F &&f) {
+  auto sized = [&](auto t) {
+    constexpr int T = t();
+    if (phase == kGram)
+      return split ? f(k_products<T, kGram, true>, shared_bytes<T>()) : f(k_products<T, kGram, false>, shared_bytes<T>());
+    if (phase == kPolynomial)
+      return split ? f(k_products<T, kPolynomial, true>, shared_bytes<T>())
+                   : f(k_products<T, kPolynomial, false>, shared_bytes<T>());
+    return split ? f(k_products<T, kUpdate, true>, shared_bytes<T>())
+                 : f(k_products<T, kUpdate, false>, shared_bytes<T>());
+  };
+  return tile == 256 ? sized(std::integral_constant<int, 256>{}) : sized(std::integral_constant<int, 128>{});
+}
+}  // namespace
+
+// More shared memory than a kernel may have unasked.
+hipError_t prepare_products(int tile, bool split) {
+  for (Phase p : {kGram, kPolynomial, kUpdate}) {
+    hipError_t e = with_products(tile, p, split, [](auto *k, size_t bytes) {
+      return hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                 static_cast<int>(bytes));
+    });
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_products(const Call &c, int tile, Phase phase, const Step &st, const Item *items, int32_t count,
                            bool split, hipStream_t s) {
-  if (phase == kGram)
-    split ? k_products<kGram, true><<<count, 256, 0, s>>>(c, st, items)
-          : k_products<kGram, false><<<count, 256, 0, s>>>(c, st, items);
-  else if (phase == kPolynomial)
-    split ? k_products<kPolynomial, true><<<count, 256, 0, s>>>(c, st, items)
-          : k_products<kPolynomial, false><<<count, 256, 0, s>>>(c, st, items);
-  else
-    split ? k_products<kUpdate, true><<<count, 256, 0, s>>>(c, st, items)
-          : k_products<kUpdate, false><<<count, 256, 0, s>>>(c, st, items);
-  return hipGetLastError();
+  return with_products(tile, phase, split, [&](auto *k, size_t bytes) {
+    k<<<count, 256, bytes, s>>>(c, st, items);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace orth
