@@ -4,9 +4,9 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <memory>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/slowmo_operators.h"
@@ -15,16 +15,41 @@
 using namespace slowmo;
 using namespace slowmo::orth;
 
+namespace {
+
+// One launch's worth of the program that every matrix goes through.
+struct Op {
+  bool update;
+  Symmetric symmetric;
+  Update up;
+};
+
+// The tiles of the three kinds of products: X X^T, n x n by n x n, and n x n by X.
+struct Lists {
+  std::vector<Tile> gram, square, update;
+};
+
+struct Device {
+  const Tile *gram = nullptr, *square = nullptr, *update = nullptr;
+  int32_t n_gram = 0, n_square = 0, n_update = 0;
+};
+
+constexpr int kClasses = 2;
+constexpr int32_t kTileOf[kClasses] = {128, 256};
+constexpr int32_t kSlotsOf[kClasses] = {768, 256};  // workgroups that run at a time
+
+}  // namespace
+
 struct slowmo_orth {
-  slowmo_orth_config cfg;
+  bool split = false;
   Steps steps{};
-  std::vector<Matrix> matrices;     // those that are not empty
-  std::vector<int32_t> index;       // their places in the caller's list
-  int32_t n_matrices = 0, tile = 0;
+  std::vector<Op> program;
+  std::vector<int32_t> index;       // places in the caller's list of the matrices that are not empty
   Call call{};
-  const Item *patches = nullptr, *padded = nullptr, *gram = nullptr, *square = nullptr, *update = nullptr;
+  const Item *sums = nullptr, *load = nullptr;
   const int32_t *tiny = nullptr;
-  int32_t n_tiny = 0, n_patches = 0, n_padded = 0, n_gram = 0, n_square = 0, n_update = 0;
+  int32_t n_tiny = 0, n_sums = 0, n_load = 0;
+  Device tiles[kClasses];
 };
 
 namespace {
@@ -37,13 +62,15 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Everything a handle needs, laid out from the configuration and the shapes alone.
 struct Plan {
-  int32_t tile = 128;
+  bool pairs = false;
   std::vector<Matrix> matrices;
-  std::vector<int32_t> index;
-  std::vector<Item> patches, padded, gram, square, update;
-  std::vector<int32_t> tiny;
-  size_t tiny_at = 0, matrices_at = 0, addresses_at = 0, squares_at = 0, inverse_at = 0, patches_at = 0, padded_at = 0,
-         gram_at = 0, square_at = 0, update_at = 0, arena_at = 0, total = 0;
+  std::vector<int32_t> index, tiny;
+  std::vector<Item> sums, load;
+  Lists lists[kClasses];
+  int64_t partial_sums = 0;   // floats
+  int32_t tickets = 0;
+  size_t matrices_at = 0, addresses_at = 0, sums_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
+         tiles_at[kClasses][3] = {}, tickets_at = 0, partial_at = 0, arena_at = 0, total = 0;
 };
 
 const char *check(const slowmo_orth_config *c, int32_t n, const int64_t *rows, const int64_t *cols,
@@ -68,13 +95,6 @@ const char *check(const slowmo_orth_config *c, int32_t n, const int64_t *rows, c
   return nullptr;
 }
 
-float factor(const slowmo_orth_config &c, int64_t rows, int64_t cols) {
-  const double r = static_cast<double>(rows), k = static_cast<double>(cols);
-  return static_cast<float>(c.scale == SLOWMO_SCALE_NONE    ? 1.
-                            : c.scale == SLOWMO_SCALE_SHAPE ? std::sqrt(std::max(1., r / k))
-                                                            : 0.2 * std::sqrt(std::max(r, k)));
-}
-
 // Tiles of a grid in blocks of 4 x 8, which 32 neighbouring workgroups share factors in.
 template <typename F>
 void walk(int32_t down, int32_t across, F &&f) {
@@ -85,8 +105,8 @@ void walk(int32_t down, int32_t across, F &&f) {
 }
 
 // Workgroups go to the 8 dies in turn: of every 256, each die gets 32 neighbours of the list.
-std::vector<Item> spread(const std::vector<Item> &v) {
-  std::vector<Item> out(v.size());
+std::vector<Tile> spread(const std::vector<Tile> &v) {
+  std::vector<Tile> out(v.size());
   for (size_t base = 0; base < v.size(); base += 256) {
     const size_t count = std::min<size_t>(256, v.size() - base), each = count / 8, more = count % 8;
     for (size_t b = 0; b < count; ++b) {
@@ -97,85 +117,167 @@ std::vector<Item> spread(const std::vector<Item> &v) {
   return out;
 }
 
-// The products' workgroups, those of long sums first.
-void order(Plan &p) {
-  std::vector<int32_t> by(p.matrices.size());
-  for (size_t i = 0; i < by.size(); ++i) by[i] = static_cast<int32_t>(i);
-  auto grams = by, updates = by;
-  std::stable_sort(grams.begin(), grams.end(), [&](int32_t a, int32_t b) { return p.matrices[a].kp > p.matrices[b].kp; });
-  std::stable_sort(updates.begin(), updates.end(), [&](int32_t a, int32_t b) { return p.matrices[a].np > p.matrices[b].np; });
-  std::vector<Item> gram, square, update;
-  for (int32_t at : grams) {
-    const int32_t n = p.matrices[at].np / p.tile;
-    walk(n, n, [&](int32_t i, int32_t j) {
-      if (j <= i) gram.push_back({at, i, j, 0});
-    });
+// What is left of the list after whole rounds of `slots` workgroups would leave most of the card idle
+// for the length of its longest tile: its tiles are cut along the summed side into shares of about equal
+// length, as many as there are slots.  Shares are no shorter than 32 steps and no more than 16 to
+// a tile, since the last one adds the others' sums up.
+void balance(std::vector<Tile> &v, int32_t slots, int64_t tile, Plan &p) {
+  const size_t whole = v.size() / slots * slots;
+  if (whole == v.size()) return;
+  int32_t longest = 0;
+  for (size_t i = whole; i < v.size(); ++i) longest = std::max(longest, v[i].count);
+  auto shares = [&](int32_t length) {
+    int64_t n = 0;
+    for (size_t i = whole; i < v.size(); ++i) n += (v[i].count + length - 1) / length;
+    return n;
+  };
+  int32_t lo = std::max(32, (longest + 15) / 16), hi = std::max(longest, lo);
+  while (lo < hi) {
+    const int32_t mid = (lo + hi) / 2;
+    if (shares(mid) <= slots)
+      hi = mid;
+    else
+      lo = mid + 1;
   }
-  for (int32_t at : updates) {
-    const int32_t n = p.matrices[at].np / p.tile, k = p.matrices[at].kp / p.tile;
-    walk(n, n, [&](int32_t i, int32_t j) {
-      if (j <= i) square.push_back({at, i, j, 0});
-    });
-    walk(n, k, [&](int32_t i, int32_t j) { update.push_back({at, i, j, 0}); });
+  std::vector<Tile> out(v.begin(), v.begin() + whole);
+  int64_t slot = 0;
+  int32_t ticket = 0;
+  for (size_t i = whole; i < v.size(); ++i) {
+    const int32_t pieces = (v[i].count + lo - 1) / lo;
+    if (pieces < 2) {
+      out.push_back(v[i]);
+      continue;
+    }
+    for (int32_t q = 0; q < pieces; ++q) {
+      Tile t = v[i];
+      t.first = static_cast<int32_t>(static_cast<int64_t>(v[i].count) * q / pieces);
+      t.count = static_cast<int32_t>(static_cast<int64_t>(v[i].count) * (q + 1) / pieces) - t.first;
+      t.piece = q;
+      t.pieces = pieces;
+      t.slot = static_cast<int32_t>(slot);
+      t.ticket = ticket;
+      out.push_back(t);
+    }
+    slot += pieces;
+    ++ticket;
   }
-  p.gram = spread(gram);
-  p.square = spread(square);
-  p.update = spread(update);
+  p.partial_sums = std::max(p.partial_sums, slot * tile * tile);
+  p.tickets = std::max(p.tickets, ticket);
+  v.swap(out);
+}
+
+// Squares of 256 have half the traffic in shared memory per product but one workgroup per CU, which
+// stands still while it writes its results: they pay where sums are long and tiles are many.
+// 8192 x 8192, tiles of 256 / 128: 983 / 1190 us a product; 1024 x 4096: 1.3 times as long.
+bool large_tiles(const Matrix &m) {
+  return m.n >= 2048 && static_cast<int64_t>(m.n) * m.k >= int64_t(256) * 256 * 256;
+}
+
+float factor(const slowmo_orth_config &c, int64_t rows, int64_t cols) {
+  const double r = static_cast<double>(rows), k = static_cast<double>(cols);
+  return static_cast<float>(c.scale == SLOWMO_SCALE_NONE    ? 1.
+                            : c.scale == SLOWMO_SCALE_SHAPE ? std::sqrt(std::max(1., r / k))
+                                                            : 0.2 * std::sqrt(std::max(r, k)));
+}
+
+Steps steps_of(const slowmo_orth_config &c) {
+  Steps s{};
+  s.count = c.steps;
+  for (int32_t t = 0; t < c.steps; ++t)
+    for (int i = 0; i < 3; ++i) s.abc[t][i] = c.coefficients ? c.coefficients[3 * t + i] : kDefault[i];
+  return s;
 }
 
 Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, const int64_t *cols,
           const int64_t *ld) {
   Plan p;
   const bool split = c.out_dtype == SLOWMO_F32;
-  if (const char *force = std::getenv("SLOWMO_ORTH_TILE")) p.tile = std::atoi(force);
-  int64_t halves = 0;
-  auto take = [&](int64_t count) {
-    const int64_t at = halves;
-    halves += up(count, kAlign / sizeof(uint16_t));
-    return at;
-  };
+  double one_by_one = 0., by_pairs = 0.;
+  std::vector<int32_t> of[kClasses];
   for (int32_t i = 0; i < n_matrices; ++i) {
     if (!rows[i] || !cols[i]) continue;
     Matrix m{};
     m.tall = rows[i] > cols[i];
     m.n = static_cast<int32_t>(std::min(rows[i], cols[i]));
     m.k = static_cast<int32_t>(std::max(rows[i], cols[i]));
-    const int32_t at = static_cast<int32_t>(p.matrices.size());
-    if (m.n <= kTinySide && static_cast<int64_t>(m.n) * m.k <= kTinyElements) {
-      m.ld = ld ? ld[i] : cols[i];
-      m.scale = factor(c, rows[i], cols[i]);
-      p.tiny.push_back(at);
-      p.matrices.push_back(m);
-      p.index.push_back(i);
-      continue;
-    }
-    m.np = static_cast<int32_t>(up(m.n, p.tile));
-    m.kp = static_cast<int32_t>(up(m.k, p.tile));
     m.ld = ld ? ld[i] : cols[i];
     m.scale = factor(c, rows[i], cols[i]);
-    const int64_t wide = static_cast<int64_t>(m.np) * m.kp, square = static_cast<int64_t>(m.np) * m.np;
-    for (int64_t &to : m.x) to = take(wide);
-    m.a = take(square);
-    m.p = take(square);
-    m.x_lo[0] = take(wide);
-    if (split) {
-      m.x_lo[1] = take(wide);
-      m.a_lo = take(square);
-      m.p_lo = take(square);
+    const int32_t at = static_cast<int32_t>(p.matrices.size());
+    if (m.n <= kTinySide && static_cast<int64_t>(m.n) * m.k <= kTinyElements) {
+      p.tiny.push_back(at);
+    } else {
+      const int which = large_tiles(m);
+      of[which].push_back(at);
+      m.np = static_cast<int32_t>(up(m.n, kTileOf[which]));
+      m.kp = static_cast<int32_t>(up(m.k, kTileOf[which]));
+      const double n = m.np, k = m.kp;
+      one_by_one += 6. * n * n * k + 2. * n * n * n;
+      by_pairs += 3. * n * n * k + 5. * n * n * n;
     }
-    m.first_patch = static_cast<int32_t>(p.patches.size());
-    auto cover = [&](std::vector<Item> &to, int64_t down, int64_t across) {
-      for (int64_t a = 0; a < down; a += kPatch)
-        for (int64_t b = 0; b < across; b += kPatch)
-          to.push_back({at, static_cast<int32_t>(a / kPatch), static_cast<int32_t>(b / kPatch), 0});
-    };
-    cover(p.patches, rows[i], cols[i]);
-    cover(p.padded, m.tall ? m.kp : m.np, m.tall ? m.np : m.kp);
-    m.patches = static_cast<int32_t>(p.patches.size()) - m.first_patch;
     p.matrices.push_back(m);
     p.index.push_back(i);
   }
-  order(p);
+  // Two steps at a time, on n x n matrices: see program().
+  p.pairs = c.steps >= 3 && by_pairs < 0.93 * one_by_one;
+
+  int64_t halves = 0;
+  auto take = [&](int64_t count) {
+    const int64_t at = halves;
+    halves += up(count, kAlign / sizeof(uint16_t));
+    return at;
+  };
+  int32_t sums = 0;
+  for (auto &list : of) {
+    for (int32_t at : list) {
+      Matrix &m = p.matrices[at];
+      const int64_t wide = static_cast<int64_t>(m.np) * m.kp, square = static_cast<int64_t>(m.np) * m.np;
+      const int32_t squares = p.pairs ? kSquares : 2;
+      for (int64_t &to : m.x) to = take(wide);
+      m.x_lo[0] = take(wide);
+      for (int32_t q = 0; q < squares; ++q) m.square[q] = take(square);
+      if (split) {
+        m.x_lo[1] = take(wide);
+        for (int32_t q = 0; q < squares; ++q) m.square_lo[q] = take(square);
+      }
+      m.first_sum = sums;
+      m.sums = static_cast<int32_t>(std::min<int64_t>(kMostSums, (static_cast<int64_t>(m.n) * m.k + 16383) / 16384));
+      sums += m.sums;
+      for (int32_t q = 0; q < m.sums; ++q) p.sums.push_back({at, q, m.sums, 0});
+      const int32_t down = (m.tall ? m.kp : m.np) / kPatch, across = (m.tall ? m.np : m.kp) / kPatch;
+      for (int32_t a = 0; a < down; ++a)
+        for (int32_t b = 0; b < across; b += kPatches) p.load.push_back({at, a, b, 0});
+    }
+  }
+  for (int which = 0; which < kClasses; ++which) {
+    auto grams = of[which], updates = of[which];
+    auto by = [&](auto side) {
+      return [&p, side](int32_t a, int32_t b) { return p.matrices[a].*side > p.matrices[b].*side; };
+    };
+    std::stable_sort(grams.begin(), grams.end(), by(&Matrix::kp));  // long sums first
+    std::stable_sort(updates.begin(), updates.end(), by(&Matrix::np));
+    const int32_t tile = kTileOf[which], times = split ? 3 : 1;
+    Lists &to = p.lists[which];
+    auto put = [&](std::vector<Tile> &v, int32_t at, int32_t i, int32_t j, int32_t depth) {
+      v.push_back({at, i, j, 0, times * (depth / kDeep), 0, 1, 0, 0, {}});
+    };
+    for (int32_t at : grams) {
+      const Matrix &m = p.matrices[at];
+      walk(m.np / tile, m.np / tile, [&](int32_t i, int32_t j) {
+        if (j <= i) put(to.gram, at, i, j, m.kp);
+      });
+    }
+    for (int32_t at : updates) {
+      const Matrix &m = p.matrices[at];
+      walk(m.np / tile, m.np / tile, [&](int32_t i, int32_t j) {
+        if (j <= i) put(to.square, at, i, j, m.np);
+      });
+      walk(m.np / tile, m.kp / tile, [&](int32_t i, int32_t j) { put(to.update, at, i, j, m.np); });
+    }
+    for (std::vector<Tile> *v : {&to.gram, &to.square, &to.update}) {
+      balance(*v, kSlotsOf[which], tile, p);
+      *v = spread(*v);
+    }
+  }
   size_t off = 0;
   auto section = [&](size_t bytes) {
     const size_t at = off;
@@ -184,24 +286,112 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   };
   p.matrices_at = section(p.matrices.size() * sizeof(Matrix));
   p.addresses_at = section(p.matrices.size() * sizeof(Addresses));
-  p.squares_at = section(p.patches.size() * sizeof(double));
-  p.inverse_at = section(p.matrices.size() * sizeof(float));
+  p.sums_at = section(p.sums.size() * sizeof(double));
   p.tiny_at = section(p.tiny.size() * sizeof(int32_t));
-  p.patches_at = section(p.patches.size() * sizeof(Item));
-  p.padded_at = section(p.padded.size() * sizeof(Item));
-  p.gram_at = section(p.gram.size() * sizeof(Item));
-  p.square_at = section(p.square.size() * sizeof(Item));
-  p.update_at = section(p.update.size() * sizeof(Item));
+  p.sum_items_at = section(p.sums.size() * sizeof(Item));
+  p.load_at = section(p.load.size() * sizeof(Item));
+  for (int which = 0; which < kClasses; ++which) {
+    const Lists &l = p.lists[which];
+    p.tiles_at[which][0] = section(l.gram.size() * sizeof(Tile));
+    p.tiles_at[which][1] = section(l.square.size() * sizeof(Tile));
+    p.tiles_at[which][2] = section(l.update.size() * sizeof(Tile));
+  }
+  p.tickets_at = section(p.tickets * sizeof(uint32_t));
+  p.partial_at = section(static_cast<size_t>(p.partial_sums) * sizeof(float));
   p.arena_at = section(static_cast<size_t>(halves) * sizeof(uint16_t));
   p.total = off;
   return p;
 }
 
+// The largest of |f(s)| for singular values s up to `most`, with 2 % for what rounding adds.
+template <typename F>
+double largest(double most, F &&f) {
+  double v = 0.;
+  for (int i = 0; i <= 2048; ++i) v = std::max(v, std::fabs(f(most * i / 2048.)));
+  return 1.02 * v;
+}
+
+// The power of two that a half array of spectral norm `most` is held times.
+float power(double most) {
+  return static_cast<float>(std::min(8192., std::exp2(std::floor(std::log2(32768. / std::max(most, 1e-30))))));
+}
+
+// The steps as launches.  One step is A = X X^T, P = b A + c A A, X <- a X + P X.  Where X is much
+// longer than wide, two steps are one: with P0 from A0, the second step's A is (a0 + P0)^2 A0, a product of
+// n x n matrices too, and X <- a0 a1 X + Q X with Q = (a0 + P0)(a1 + P1) - a0 a1.  X is read and
+// written half as often, and of the products with X two of three per pair are left: 3 n n k + 5 n n n
+// for 6 n n k + 2 n n n.  (All n x n factors are polynomials of the same A, so that each product of
+// two is symmetric again.)  The last step is never one of a pair: rounding would show.
+// Returns an empty program if the coefficients let X outgrow a half.
+std::vector<Op> program(const Steps &steps, bool pairs, bool split) {
+  std::vector<Op> ops;
+  enum { kA, kP, kW, kQ };
+  auto symmetric = [&](Symmetric s) {
+    Op op{};
+    op.symmetric = s;
+    ops.push_back(op);
+  };
+  double most = 1.;   // of the singular values
+  int32_t from = 0;
+  for (int32_t t = 0; t < steps.count;) {
+    const bool two = pairs && steps.count - t >= 3;
+    const double a0 = steps.abc[t][0], b0 = steps.abc[t][1], c0 = steps.abc[t][2];
+    auto p0 = [=](double s) { return b0 * s * s + c0 * s * s * s * s; };
+    // Of single halves the last two steps' a goes to P's diagonal; the others' X enters as hi + lo.
+    // Pairs of halves have bits enough.
+    const bool carry = !split && (two || t < steps.count - 2);
+    const double keep0 = carry ? 0. : a0;
+    const float sa = power(largest(most, [&](double s) { return s * s; }));
+    const float sp = power(largest(most, [&](double s) { return p0(s) + (two ? 0. : keep0); }));
+    symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f});
+    symmetric({from, kA, kA, kA, -1, kP, static_cast<float>(c0 * sp / (double(sa) * sa)),
+               static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp)});
+    Op op{};
+    op.update = true;
+    op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0)};
+    double after = largest(most, [&](double s) { return s * (a0 + p0(s)); });
+    if (two) {
+      const double a1 = steps.abc[t + 1][0], b1 = steps.abc[t + 1][1], c1 = steps.abc[t + 1][2];
+      auto x1 = [=](double s) { return s * (a0 + p0(s)); };
+      auto p1 = [=](double s) { return b1 * x1(s) * x1(s) + c1 * std::pow(x1(s), 4.); };
+      const double keep = carry ? 0. : a0 * a1;
+      const float sw = power(largest(most, [&](double s) { return s * x1(s); }));
+      const float sa1 = power(largest(most, [&](double s) { return x1(s) * x1(s); }));
+      const float sp1 = power(largest(most, p1));
+      const float sq = power(largest(most, [&](double s) { return (a0 + p0(s)) * (a1 + p1(s)) - a0 * a1 + keep; }));
+      symmetric({from, kP, kA, kA, -1, kW, sw / (sp * sa), static_cast<float>(a0 * sw / sa), 0.f, 0.f});
+      symmetric({from, kW, kP, kW, -1, kA, sa1 / (sw * sp), static_cast<float>(a0 * sa1 / sw), 0.f, 0.f});
+      symmetric({from, kA, kA, kA, -1, kW, static_cast<float>(c1 * sp1 / (double(sa1) * sa1)),
+                 static_cast<float>(b1 * sp1 / sa1), 0.f, 0.f});
+      symmetric({from, kW, kP, kP, kW, kQ, sq / (sp1 * sp), static_cast<float>(a1 * sq / sp),
+                 static_cast<float>(a0 * sq / sp1), static_cast<float>(keep * sq)});
+      op.up.by = kQ;
+      op.up.alpha = 1.f / sq;
+      op.up.beta = static_cast<float>(a0 * a1);
+      if (after >= 7.9) return {};
+      after = largest(most, [&](double s) { return x1(s) * (a1 + p1(s)); });
+    }
+    if (after >= 7.9) return {};
+    most = std::max(after, 1e-3);
+    ops.push_back(op);
+    from = 1 - from;
+    t += two ? 2 : 1;
+  }
+  Update *next = nullptr;
+  for (auto op = ops.rbegin(); op != ops.rend(); ++op) {
+    if (!op->update) continue;
+    op->up.last = next == nullptr;
+    op->up.carry_next = next && next->carry;
+    next = &op->up;
+  }
+  return ops;
+}
+
 slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum, void *const *out, float mu,
                   int32_t nesterov, void *stream_) {
   const bool with_momentum = momentum != nullptr;
-  const size_t in_size = h->cfg.in_dtype == SLOWMO_BF16 ? 2 : 4, out_size = h->cfg.out_dtype == SLOWMO_BF16 ? 2 : 4;
-  const int32_t count = static_cast<int32_t>(h->matrices.size());
+  const size_t in_size = h->call.in_bf16 ? 2 : 4, out_size = h->call.out_bf16 ? 2 : 4;
+  const int32_t count = static_cast<int32_t>(h->index.size());
   for (int32_t i = 0; i < count; ++i) {
     const int32_t at = h->index[i];
     if (!in[at] || !out[at] || (with_momentum && !momentum[at]))
@@ -216,9 +406,9 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
   c.mu = mu;
   c.nesterov = nesterov;
   c.momentum = with_momentum;
-  const bool split = h->cfg.out_dtype == SLOWMO_F32;
   hipError_t e = hipSuccess;
   auto ok = [&](hipError_t got) { return (e = got) == hipSuccess; };
+  auto refused = [&] { return fail_thread_hip(e, "slowmo_orthogonalize (results may be partly written)"); };
   for (int32_t first = 0; first < count; first += kInline) {
     Few few{};
     const int32_t some = std::min(kInline, count - first);
@@ -226,23 +416,21 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
       const int32_t at = h->index[first + i];
       few.at[i] = {in[at], with_momentum ? momentum[at] : nullptr, out[at]};
     }
-    if (!ok(launch_addresses(c, few, first, some, s))) return fail_thread_hip(e, "slowmo_orthogonalize");
+    if (!ok(launch_addresses(c, few, first, some, s))) return refused();
   }
-  if (h->n_tiny && !ok(launch_tiny(c, h->steps, h->tiny, h->n_tiny, s)))
-    return fail_thread_hip(e, "slowmo_orthogonalize");
+  if (h->n_tiny && !ok(launch_tiny(c, h->steps, h->tiny, h->n_tiny, s))) return refused();
   if (h->n_tiny == count) return SLOWMO_OK;
-  if (!ok(launch_squares(c, h->patches, h->n_patches, s)) || !ok(launch_norms(c, count, s)) ||
-      !ok(launch_load(c, h->padded, h->n_padded, s)))
-    return fail_thread_hip(e, "slowmo_orthogonalize");
-  for (int32_t t = 0; t < h->steps.count; ++t) {
-    const float *k = h->steps.abc[t];
-    // Pairs of halves have bits enough; of single ones the last two steps, whose roundings grow no more.
-    auto carries = [&](int32_t step) { return !split && step < h->steps.count - 2; };
-    const Step st{k[0], k[1], k[2], t & 1, t + 1 == h->steps.count, carries(t), carries(t + 1)};
-    if (!ok(launch_products(c, h->tile, kGram, st, h->gram, h->n_gram, split, s)) ||
-        !ok(launch_products(c, h->tile, kPolynomial, st, h->square, h->n_square, split, s)) ||
-        !ok(launch_products(c, h->tile, kUpdate, st, h->update, h->n_update, split, s)))
-      return fail_thread_hip(e, "slowmo_orthogonalize");
+  if (!ok(launch_sums(c, h->sums, h->n_sums, s)) || !ok(launch_load(c, h->load, h->n_load, s))) return refused();
+  for (const Op &op : h->program) {
+    for (int which = 0; which < kClasses; ++which) {
+      const Device &d = h->tiles[which];
+      if (!d.n_update) continue;
+      const bool gram = op.symmetric.left < 0;
+      if (!ok(op.update ? launch_update(c, kTileOf[which], op.up, d.update, d.n_update, h->split, s)
+                        : launch_symmetric(c, kTileOf[which], op.symmetric, gram ? d.gram : d.square,
+                                           gram ? d.n_gram : d.n_square, h->split, s)))
+        return refused();
+    }
   }
   return SLOWMO_OK;
 }
@@ -251,11 +439,19 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
 
 extern "C" {
 
+// Reasons to refuse that both calls share.
+static const char *refusal(const slowmo_orth_config *cfg, int32_t n_matrices, const int64_t *rows,
+                           const int64_t *cols, const int64_t *ld) {
+  if (const char *bad = check(cfg, n_matrices, rows, cols, ld)) return bad;
+  if (program(steps_of(*cfg), false, false).empty()) return "the coefficients let singular values grow past 7";
+  return nullptr;
+}
+
 size_t slowmo_orth_bytes(const slowmo_orth_config *cfg, int32_t n_matrices, const int64_t *rows,
                          const int64_t *cols, const int64_t *ld) {
   size_t bytes = 0;
   walled([&]() -> slowmo_status {
-    if (const char *bad = check(cfg, n_matrices, rows, cols, ld)) return fail_thread(SLOWMO_ERR_ARG, bad);
+    if (const char *bad = refusal(cfg, n_matrices, rows, cols, ld)) return fail_thread(SLOWMO_ERR_ARG, bad);
     bytes = plan(*cfg, n_matrices, rows, cols, ld).total;
     return SLOWMO_OK;
   });
@@ -268,7 +464,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
   if (!out) return fail_thread(SLOWMO_ERR_ARG, "out is NULL");
   *out = nullptr;
   return walled([&]() -> slowmo_status {
-    if (const char *bad = check(cfg, n_matrices, rows, cols, ld)) return fail_thread(SLOWMO_ERR_ARG, bad);
+    if (const char *bad = refusal(cfg, n_matrices, rows, cols, ld)) return fail_thread(SLOWMO_ERR_ARG, bad);
     if (!workspace) return fail_thread(SLOWMO_ERR_ARG, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign)
       return fail_thread(SLOWMO_ERR_ALIGN, "workspace must be 256-byte aligned");
@@ -277,45 +473,39 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
       return fail_thread(SLOWMO_ERR_NOMEM, "workspace is smaller than slowmo_orth_bytes()");
     if (slowmo_status st = slowmo_check_device_range(workspace, p.total); st != SLOWMO_OK) return st;
     std::unique_ptr<slowmo_orth> h(new slowmo_orth);
-    h->cfg = *cfg;
-    h->cfg.coefficients = nullptr;
-    h->steps.count = cfg->steps;
-    for (int32_t t = 0; t < cfg->steps; ++t)
-      for (int i = 0; i < 3; ++i)
-        h->steps.abc[t][i] = cfg->coefficients ? cfg->coefficients[3 * t + i] : kDefault[i];
-    h->n_matrices = n_matrices;
-    h->tile = p.tile;
-    if (hipError_t e = prepare_products(p.tile, cfg->out_dtype == SLOWMO_F32); e != hipSuccess)
-      return fail_thread_hip(e, "slowmo_orth_create");
-    h->matrices = p.matrices;
+    h->split = cfg->out_dtype == SLOWMO_F32;
+    h->steps = steps_of(*cfg);
+    h->program = program(h->steps, p.pairs, h->split);
     h->index = p.index;
     char *base = static_cast<char *>(workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
-    auto put = [&](size_t at, const void *from, size_t bytes) {
-      if (bytes && e == hipSuccess) e = hipMemcpyAsync(base + at, from, bytes, hipMemcpyHostToDevice, s);
-    };
-    put(p.matrices_at, p.matrices.data(), p.matrices.size() * sizeof(Matrix));
-    auto items = [&](size_t at, const std::vector<Item> &v, const Item *&to, int32_t &count) {
-      put(at, v.data(), v.size() * sizeof(Item));
-      to = reinterpret_cast<const Item *>(base + at);
+    auto put = [&](size_t at, const auto &v, auto *&to, int32_t &count) {
+      if (!v.empty() && e == hipSuccess)
+        e = hipMemcpyAsync(base + at, v.data(), v.size() * sizeof(v[0]), hipMemcpyHostToDevice, s);
+      to = reinterpret_cast<std::remove_reference_t<decltype(to)>>(base + at);
       count = static_cast<int32_t>(v.size());
     };
-    put(p.tiny_at, p.tiny.data(), p.tiny.size() * sizeof(int32_t));
-    h->tiny = reinterpret_cast<const int32_t *>(base + p.tiny_at);
-    h->n_tiny = static_cast<int32_t>(p.tiny.size());
-    items(p.patches_at, p.patches, h->patches, h->n_patches);
-    items(p.padded_at, p.padded, h->padded, h->n_padded);
-    items(p.gram_at, p.gram, h->gram, h->n_gram);
-    items(p.square_at, p.square, h->square, h->n_square);
-    items(p.update_at, p.update, h->update, h->n_update);
-    hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here
+    int32_t n_matrices_here = 0;
+    put(p.matrices_at, p.matrices, h->call.matrices, n_matrices_here);
+    put(p.tiny_at, p.tiny, h->tiny, h->n_tiny);
+    put(p.sum_items_at, p.sums, h->sums, h->n_sums);
+    put(p.load_at, p.load, h->load, h->n_load);
+    for (int which = 0; which < kClasses; ++which) {
+      Device &d = h->tiles[which];
+      put(p.tiles_at[which][0], p.lists[which].gram, d.gram, d.n_gram);
+      put(p.tiles_at[which][1], p.lists[which].square, d.square, d.n_square);
+      put(p.tiles_at[which][2], p.lists[which].update, d.update, d.n_update);
+      if (d.n_update && e == hipSuccess) e = prepare_products(kTileOf[which], h->split);
+    }
+    if (p.tickets && e == hipSuccess) e = hipMemsetAsync(base + p.tickets_at, 0, p.tickets * sizeof(uint32_t), s);
+    const hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here
     if (e == hipSuccess) e = waited;
     if (e != hipSuccess) return fail_thread_hip(e, "slowmo_orth_create");
-    h->call.matrices = reinterpret_cast<const Matrix *>(base + p.matrices_at);
     h->call.addresses = reinterpret_cast<Addresses *>(base + p.addresses_at);
-    h->call.squares = reinterpret_cast<double *>(base + p.squares_at);
-    h->call.inverse = reinterpret_cast<float *>(base + p.inverse_at);
+    h->call.sums = reinterpret_cast<double *>(base + p.sums_at);
+    h->call.tickets = reinterpret_cast<uint32_t *>(base + p.tickets_at);
+    h->call.partial = reinterpret_cast<float *>(base + p.partial_at);
     h->call.arena = reinterpret_cast<_Float16 *>(base + p.arena_at);
     h->call.eps = cfg->eps;
     h->call.in_bf16 = cfg->in_dtype == SLOWMO_BF16;

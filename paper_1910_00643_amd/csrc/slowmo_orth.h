@@ -8,31 +8,44 @@
 namespace slowmo {
 namespace orth {
 
-// Halves are stored times a power of two that keeps them away from the subnormal range: X and A are
-// below 8 in size (their spectral norms are near 1), b A + c A A below 32.
-constexpr float kScaleX = 8192.f, kScaleA = 8192.f, kScaleP = 2048.f;
-
-constexpr int kPatch = 64;       // side of an elementwise kernel's patch
+constexpr int kDeep = 32;        // elements of the summed side in a step of a product
+constexpr int kPatch = 64;       // side of an elementwise kernel's patch; kPatches of them in a row per workgroup
+constexpr int kPatches = 4;
 constexpr int kInline = 64;      // matrices whose addresses travel with one launch
+constexpr int kMostSums = 1024;  // workgroups that share a matrix's sum of squares
+constexpr int kSquares = 4;      // n x n buffers of a matrix: A, P, W, Q
 
 // Matrices that one workgroup takes from load to store.
 constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
 
-// One matrix.  n <= k; X is n x k; np, kp: sides padded to whole tiles.  Offsets count halves from
-// the start of the arena; lo: the values' next 11 bits.
+// X is held as halves times this power of two: its elements are below 8 in size (checked on the
+// coefficients), and what of them is subnormal as a half is below 2^-27.
+constexpr float kScaleX = 8192.f;
+
+// One matrix.  n <= k; X is n x k; np, kp: sides padded to whole tiles.  X and the n x n buffers lie in
+// panels of kDeep columns, [column / kDeep][row][column mod kDeep].  Offsets count halves from the start
+// of the arena; lo: the values' next 11 bits.
 struct Matrix {
-  int64_t x[2], a, p;
-  int64_t x_lo[2], a_lo, p_lo;  // x_lo[1], a_lo, p_lo only where products are split
+  int64_t x[2], square[kSquares];
+  int64_t x_lo[2], square_lo[kSquares];  // x_lo[1], square_lo only where products are split
   int64_t ld;
   int32_t n, k, np, kp;
-  int32_t tall;                        // the caller's matrix is k x n
+  int32_t tall;                          // the caller's matrix is k x n
   float scale;
-  int32_t first_patch, patches;        // its patches in the list of them
+  int32_t first_sum, sums;               // its partial sums of squares
 };
 
-// One workgroup's share of a phase.
+// A workgroup's share of an elementwise phase: of a sum of squares (i of `j`), or the patches from
+// (i, j) on.
 struct Item {
   int32_t matrix, i, j, pad;
+};
+
+// A workgroup's share of a product: steps first..first + count - 1 of tile (i, j); where a tile is in
+// `pieces` > 1 shares, `slot` counts the places of their partial sums and `ticket` its counter.
+struct Tile {
+  int32_t matrix, i, j, first, count, piece, pieces, slot;
+  int32_t ticket, pad[3];
 };
 
 struct Addresses {
@@ -49,21 +62,25 @@ struct Few {
 struct Call {
   const Matrix *matrices;
   Addresses *addresses;
-  double *squares;     // one sum per patch
-  float *inverse;      // 1 / (|U|_F + eps) per matrix, NaN where the norm is not finite
+  double *sums;
   _Float16 *arena;
+  float *partial;        // partial sums of tiles
+  uint32_t *tickets;     // zero between calls
   float eps, mu;
   int32_t in_bf16, out_bf16, momentum, nesterov;
 };
 
-enum Phase { kGram = 0, kPolynomial = 1, kUpdate = 2 };
+// out = alpha * left * right (+ beta * first) (+ gamma * second) (+ delta on the diagonal), symmetric;
+// buffers are places in Matrix::square, left = -1: X X^T.  The factors hold the buffers' powers of two.
+struct Symmetric {
+  int32_t from, left, right, first, second, out;  // first, second: -1: none
+  float alpha, beta, gamma, delta;
+};
 
-struct Step {
-  float a, b, c;
-  int32_t from;        // which of x[2] is read
-  int32_t last;
-  int32_t carry;       // a X enters from hi + lo, and P is b A + c A A alone; else P has a on its diagonal
-  int32_t carry_next;  // the next step needs lo
+// x[1 - from] = alpha * square[by] x[from] (+ beta * (hi + lo of x[from])); or the caller's result.
+struct Update {
+  int32_t from, by, carry, carry_next, last;
+  float alpha, beta;
 };
 
 struct Steps {
@@ -73,12 +90,13 @@ struct Steps {
 
 hipError_t launch_tiny(const Call &c, const Steps &steps, const int32_t *list, int32_t count, hipStream_t s);
 hipError_t launch_addresses(const Call &c, const Few &few, int32_t first, int32_t count, hipStream_t s);
-hipError_t launch_squares(const Call &c, const Item *items, int32_t count, hipStream_t s);
-hipError_t launch_norms(const Call &c, int32_t matrices, hipStream_t s);
+hipError_t launch_sums(const Call &c, const Item *items, int32_t count, hipStream_t s);
 hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStream_t s);
 hipError_t prepare_products(int tile, bool split);
-hipError_t launch_products(const Call &c, int tile, Phase phase, const Step &step, const Item *items,
-                           int32_t count, bool split, hipStream_t s);
+hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const Tile *tiles, int32_t count,
+                            bool split, hipStream_t s);
+hipError_t launch_update(const Call &c, int tile, const Update &p, const Tile *tiles, int32_t count, bool split,
+                         hipStream_t s);
 
 }  // namespace orth
 }  // namespace slowmo

@@ -18,8 +18,7 @@ namespace orth {
 namespace {
 
 typedef _Float16 half;
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32;
@@ -48,46 +47,119 @@ __device__ __forceinline__ float load_input(const Call &c, const Addresses &at, 
                    : static_cast<const float *>(at.in)[e];
 }
 
-// The sum of squares of U over a patch, in 64 bits: squares of fp32 values neither overflow nor
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void load8(const float *p, float *v) {
+  const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+__device__ __forceinline__ void load8(const uint16_t *p, float *v) {
+  const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __builtin_bit_cast(float, a[i] << 16);
+    v[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+  }
+}
+
+// Eight neighbours of a row of the caller's matrix, zeros past its end; `wide`: loads of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void row8(const T *p, int left, bool wide, float *v) {
+  if (wide && left >= 8) {
+    load8(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = 0.f;
+      if (i < left) {
+        if constexpr (sizeof(T) == 2)
+          v[i] = widen_bf16(p[i]);
+        else
+          v[i] = p[i];
+      }
+    }
+  }
+}
+
+// Whether rows of a matrix at p, ld elements apart, all start at multiples of 16 bytes.
+template <typename T>
+__device__ __forceinline__ bool whole_rows(const T *p, int64_t ld) {
+  return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * sizeof(T))) & 15) == 0;
+}
+
+__device__ __forceinline__ double block_sum(double v, double *shared) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return shared[0] + shared[1] + shared[2] + shared[3];
+}
+
+// A workgroup's share of the sum of squares of U, in 64 bits: squares of fp32 values neither overflow nor
 // vanish there.  Updates the momentum on the way.
-__global__ __launch_bounds__(256) void k_squares(Call c, const Item *items) {
+__global__ __launch_bounds__(256) void k_sums(Call c, const Item *items) {
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
   const Addresses at = c.addresses[it.matrix];
-  const int rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k;
-  const int col = it.j * kPatch + (threadIdx.x & 63);
+  const u32 rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k, pieces = (cols + 7) / 8;
+  const u32 all = rows * pieces, each = (all + it.j - 1) / it.j;  // at most 2^29
+  const u32 last = min(all, (it.i + 1) * each);
   double sum = 0.;
-  for (int r = threadIdx.x >> 6; r < kPatch; r += 4) {
-    const int row = it.i * kPatch + r;
-    if (row >= rows || col >= cols) continue;
-    const int64_t e = row * m.ld + col;
-    float u = load_input(c, at, e);
-    if (c.momentum) {
-      const float h = fmaf(c.mu, at.momentum[e], u);
-      at.momentum[e] = h;
-      u = c.nesterov ? fmaf(c.mu, h, u) : h;
+  auto walk = [&](auto *in) {
+    const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
+#pragma unroll 2
+    for (u32 q = it.i * each + threadIdx.x; q < last; q += 256) {
+      const u32 row = q / pieces, col = (q - row * pieces) * 8;
+      const int64_t e = static_cast<int64_t>(row) * m.ld + col;
+      const int left = static_cast<int>(cols - col);
+      float u[8];
+      row8(in + e, left, wide, u);
+      if (c.momentum) {
+        float h[8];
+        row8(at.momentum + e, left, wide_m, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = fmaf(c.mu, h[i], u[i]);
+        float *to = at.momentum + e;
+        if (wide_m && left >= 8) {
+          *reinterpret_cast<f32x4 *>(to) = f32x4{h[0], h[1], h[2], h[3]};
+          *reinterpret_cast<f32x4 *>(to + 4) = f32x4{h[4], h[5], h[6], h[7]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < left) to[i] = h[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fma(static_cast<double>(u[i]), static_cast<double>(u[i]), sum);
     }
-    sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
-  }
-  __shared__ double sums[4];
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) c.squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+  };
+  if (c.in_bf16)
+    walk(static_cast<const uint16_t *>(at.in));
+  else
+    walk(static_cast<const float *>(at.in));
+  __shared__ double shared[4];
+  sum = block_sum(sum, shared);
+  if (threadIdx.x == 0) c.sums[m.first_sum + it.i] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_norms(Call c) {
-  const Matrix &m = c.matrices[blockIdx.x];
-  double sum = 0.;
-  for (int i = threadIdx.x; i < m.patches; i += 256) sum += c.squares[m.first_patch + i];
-  __shared__ double sums[4];
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x) return;
-  const double norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + static_cast<double>(c.eps);
+__device__ __forceinline__ double inverse_norm(double squares, float eps) {
+  const double norm = sqrt(squares) + static_cast<double>(eps);
   // a matrix of zeros (and eps 0): zeros; an infinity or NaN anywhere: NaN everywhere
-  c.inverse[blockIdx.x] = norm == 0. ? 0.f : norm < 1.7e308 ? static_cast<float>(1. / norm) : __builtin_nanf("");
+  return norm == 0. ? 0. : norm < 1.7e308 ? 1. / norm : __builtin_nan("");
+}
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ void split8(const float *v, half8 &hi, half8 &lo) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    half h, l;
+    split_half(v[e], h, l);
+    hi[e] = h;
+    lo[e] = l;
+  }
 }
 
 // X_0 (n x k, turned if the caller's matrix is tall) as halves hi and lo, with zeros in the padding (which
@@ -96,37 +168,67 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
   const Addresses at = c.addresses[it.matrix];
-  const int rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k;
+  const int rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k, across = m.tall ? m.np : m.kp;
   half *x = c.arena + m.x[0], *x_lo = c.arena + m.x_lo[0];
-  const float inverse = c.inverse[it.matrix];
   __shared__ float turn[kPatch][kPatch + 1];
-  const int lane = threadIdx.x & 63;
-  for (int r = threadIdx.x >> 6; r < kPatch; r += 4) {
-    const int row = it.i * kPatch + r, col = it.j * kPatch + lane;
-    float u = 0.f;
-    if (row < rows && col < cols) {
-      const int64_t e = row * m.ld + col;
-      if (c.momentum) {
-        const float h = at.momentum[e];
-        u = c.nesterov ? fmaf(c.mu, h, load_input(c, at, e)) : h;
-      } else {
-        u = load_input(c, at, e);
+  __shared__ double shared[4];
+  double squares = 0.;
+  for (int i = threadIdx.x; i < m.sums; i += 256) squares += c.sums[m.first_sum + i];
+  const float inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
+  auto walk = [&](auto *in) {
+    const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
+    for (int patch = it.j; patch < it.j + kPatches && patch * kPatch < across; ++patch) {
+#pragma unroll
+      for (int q = threadIdx.x; q < kPatch * kPatch / 8; q += 256) {
+        const int r = q >> 3, c8 = (q & 7) * 8, row = it.i * kPatch + r, col = patch * kPatch + c8;
+        float u[8] = {};
+        if (row < rows && col < cols) {
+          const int64_t e = row * m.ld + col;
+          row8(in + e, cols - col, wide, u);
+          if (c.momentum) {
+            float h[8];
+            row8(at.momentum + e, cols - col, wide_m, h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = u[i] * inverse * kScaleX;
+        if (m.tall) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) turn[r][c8 + i] = row < rows && col + i < cols ? u[i] : 0.f;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] = row < rows && col + i < cols ? u[i] : 0.f;
+          half8 hi, lo;
+          split8(u, hi, lo);
+          const int64_t to = (static_cast<int64_t>(col >> 5) * m.np + row) * kDeep + (col & 31);
+          *reinterpret_cast<half8 *>(x + to) = hi;
+          *reinterpret_cast<half8 *>(x_lo + to) = lo;
+        }
       }
-      u = u * inverse * kScaleX;
+      if (!m.tall) continue;
+      __syncthreads();
+#pragma unroll
+      for (int q = threadIdx.x; q < kPatch * kPatch / 8; q += 256) {
+        const int r = q >> 3, c8 = (q & 7) * 8;
+        float u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = turn[c8 + i][r];
+        half8 hi, lo;
+        split8(u, hi, lo);
+        const int n = patch * kPatch + r, k = it.i * kPatch + c8;
+        const int64_t to = (static_cast<int64_t>(k >> 5) * m.np + n) * kDeep + (k & 31);
+        *reinterpret_cast<half8 *>(x + to) = hi;
+        *reinterpret_cast<half8 *>(x_lo + to) = lo;
+      }
+      __syncthreads();
     }
-    if (m.tall) {
-      turn[r][lane] = u;
-    } else {
-      const int64_t to = static_cast<int64_t>(row) * m.kp + col;
-      split_half(u, x[to], x_lo[to]);
-    }
-  }
-  if (!m.tall) return;
-  __syncthreads();
-  for (int r = threadIdx.x >> 6; r < kPatch; r += 4) {
-    const int64_t to = static_cast<int64_t>(it.j * kPatch + r) * m.kp + it.i * kPatch + lane;
-    split_half(turn[lane][r], x[to], x_lo[to]);
-  }
+  };
+  if (c.in_bf16)
+    walk(static_cast<const uint16_t *>(at.in));
+  else
+    walk(static_cast<const float *>(at.in));
 }
 
 // 8 neighbouring results of one row of the caller's matrix (rows x cols, ld apart).
@@ -168,13 +270,17 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // registers before it issues the products of this 16, across the barrier of a step too, so that with
 // one wave per SIMD (T = 256: 256 accumulators a lane) the matrix cores go on.
 //
-// Rows of 32 halves (both factors contiguous along the summed side: X X^T, A A, and P of P X) are four
-// pieces of 16 bytes; piece p of row r lies at p xor (r / 4 mod 4), so that 16 lanes that read the same
-// piece of neighbouring rows meet all 64 banks once.  X of P X lies with the summed side across: its
-// rows are read turned (4 rows x 16 columns per 16 lanes), with piece p of row r at p xor 4 (r mod 4).
+// X and the n x n matrices lie in panels of 32 columns, [column / 32][row][column mod 32]: a step's share of a
+// factor is one piece of memory (P X's X: one per panel) and every cache line of it is used whole.  (Rows
+// after rows, a step's 64 bytes of each cost as many requests to L2 as 128, and L2 is what bounds the smaller
+// tiles.)  In shared memory a row's 64 bytes are four pieces; where a factor is read along its rows,
+// piece p of row r lies at p xor (r / 4 mod 4), so that 16 lanes that read the same piece of neighbouring
+// rows meet all 64 banks once.  X of P X has the summed side down its columns: it is read turned, 4 rows x
+// 16 columns per 16 lanes, which meets all banks as it lies.
 // Everything is padded to whole tiles; nothing is checked in the loop.
 
-constexpr int kDeep = 32, kRing = 4;
+template <int T>
+constexpr int kRing = T == 256 ? 4 : 3;  // 128 and 48 KB: one workgroup per CU, or three
 
 __device__ __forceinline__ void to_shared(u32 shared, u32 offset, const half *base) {
   // m0 is written and read within this block; the wait covers its hazard and that of a base that a
@@ -193,74 +299,79 @@ __device__ __forceinline__ void arrive() {
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
 
-template <int T, int PHASE, bool SPLIT>
-__global__ __launch_bounds__(256, T == 256 ? 1 : 2) void k_products(Call c, Step st, const Item *items) {
+// UPDATE: P X by Update, else a symmetric product by Symmetric.
+template <int T, bool UPDATE, bool SPLIT>
+__global__ __launch_bounds__(256, T == 256 ? 1 : 3) void k_products(
+    Call c, std::conditional_t<UPDATE, Update, Symmetric> st, const Tile *tiles) {
   extern __shared__ half ring[];
+  constexpr int kStages = kRing<T>;
   constexpr int kBlocks = T / 64;            // blocks of 32 x 32 along a side of a wave's share
   constexpr int kShare = T * kDeep;          // halves of one factor in a stage
   constexpr int kLoads = kShare * 2 / 1024 / 4;  // loads of a wave per factor and stage
   constexpr int kWide = T / 2;               // side of a wave's share
-  const Item it = items[blockIdx.x];
+  const Tile it = tiles[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave & 1, wb = wave >> 1;
   const int low = lane & 31, high = lane >> 5;
 
   // factor a: columns of the tile (j), factor b: rows (i).  The accumulators' four neighbours run along a.
-  const int depth = PHASE == kGram ? m.kp : m.np, steps = depth / kDeep;
-  const int64_t a_hi = PHASE == kPolynomial ? m.a : m.x[st.from];
-  const int64_t a_lo = PHASE == kPolynomial ? m.a_lo : m.x_lo[st.from];
-  const int64_t b_hi = PHASE == kUpdate ? m.p : a_hi, b_lo = PHASE == kUpdate ? m.p_lo : a_lo;
-  const int64_t a_at = PHASE == kUpdate ? static_cast<int64_t>(it.j) * T : static_cast<int64_t>(it.j) * T * depth;
-  const int64_t b_at = static_cast<int64_t>(it.i) * T * depth;
-  const int64_t a_step = PHASE == kUpdate ? static_cast<int64_t>(kDeep) * m.kp : kDeep;
-  const int total = SPLIT ? 3 * steps : steps;
-
-  u32 a_off[kLoads], b_off[kLoads];          // bytes
-#pragma unroll
-  for (int q = 0; q < kLoads; ++q) {
-    const int load = wave * kLoads + q;
-    const int row = load * 16 + (lane >> 2), piece = (lane & 3) ^ ((row >> 2) & 3);
-    b_off[q] = (row * depth + piece * 8) * 2;
-    if constexpr (PHASE == kUpdate) {
-      constexpr int kAcross = T / 8;         // pieces of a row
-      const int r = load * (64 / kAcross) + lane / kAcross, p = (lane % kAcross) ^ (4 * (r & 3));
-      a_off[q] = (r * m.kp + p * 8) * 2;
-    } else {
-      a_off[q] = b_off[q];
-    }
+  int64_t a_hi, a_lo, b_hi, b_lo;
+  int depth = m.np;
+  if constexpr (UPDATE) {
+    a_hi = m.x[st.from];
+    a_lo = m.x_lo[st.from];
+    b_hi = m.square[st.by];
+    b_lo = m.square_lo[st.by];
+  } else if (st.left < 0) {
+    depth = m.kp;
+    a_hi = b_hi = m.x[st.from];
+    a_lo = b_lo = m.x_lo[st.from];
+  } else {
+    a_hi = m.square[st.right];
+    a_lo = m.square_lo[st.right];
+    b_hi = m.square[st.left];
+    b_lo = m.square_lo[st.left];
   }
+  const int64_t panel = static_cast<int64_t>(m.np) * kDeep;
+  const int64_t a_at = UPDATE ? static_cast<int64_t>(it.j) * (T / kDeep) * panel : static_cast<int64_t>(it.j) * T * kDeep;
+  const int64_t a_step = UPDATE ? kDeep * kDeep : panel;
+  const int64_t b_at = static_cast<int64_t>(it.i) * T * kDeep;
+  const int steps = depth / kDeep;
+
+  // bytes of a lane's piece within a load's 1024: 16 rows of 4 pieces
+  const u32 b_off = ((lane & ~3) | ((lane & 3) ^ ((lane >> 4) & 3))) * 16, a_off = UPDATE ? lane * 16 : b_off;
   const u32 shared0 = static_cast<u32>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half *)ring));
 
-  auto fetch = [&](int t) {
+  const int total = it.count;
+  auto fetch = [&](int s, int slot) {
     // split: the small products first (hi lo, lo hi), while their sums are small, then hi hi
-    const int seg = SPLIT ? (t >= 2 * steps ? 2 : t >= steps ? 1 : 0) : 2;
+    const int t = it.first + s, seg = SPLIT ? (t >= 2 * steps ? 2 : t >= steps ? 1 : 0) : 2;
     const int at = SPLIT ? t - seg * steps : t;
     const half *a = c.arena + (seg == 1 ? a_lo : a_hi) + a_at + at * a_step;
-    const half *b = c.arena + (seg == 0 ? b_lo : b_hi) + b_at + static_cast<int64_t>(at) * kDeep;
-    const u32 slot = shared0 + (t % kRing) * (2 * kShare * 2) + wave * kLoads * 1024;
+    const half *b = c.arena + (seg == 0 ? b_lo : b_hi) + b_at + at * panel;
+    const u32 to = shared0 + slot * (2 * kShare * 2);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
-      to_shared(slot + q * 1024, a_off[q], a);
-      to_shared(slot + kShare * 2 + q * 1024, b_off[q], b);
+      const int load = wave * kLoads + q;  // two to a panel's 32 rows
+      to_shared(to + load * 1024, a_off, a + (UPDATE ? (load >> 1) * panel + (load & 1) * 512 : load * 512));
+      to_shared(to + kShare * 2 + load * 1024, b_off, b + load * 512);
     }
   };
 
   half8 fa[2][kBlocks], fb[2][kBlocks];
-  auto read = [&](int t, int kk, half8 *a, half8 *b) {
-    const half *sa = ring + (t % kRing) * 2 * kShare, *sb = sa + kShare;
+  auto read = [&](int slot, int kk, half8 *a, half8 *b) {
+    const half *sa = ring + slot * 2 * kShare, *sb = sa + kShare;
 #pragma unroll
     for (int x = 0; x < kBlocks; ++x) {
       const int rb = wb * kWide + x * 32 + low;
       b[x] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
-      if constexpr (PHASE == kUpdate) {
-        const int r = kk * 16 + high * 8 + ((lane >> 2) & 3);
-        const int col = wa * kWide + x * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const int piece = (col >> 3) ^ (4 * (r & 3));
-        const half *from = sa + r * T + piece * 8 + (col & 7);
+      if constexpr (UPDATE) {
+        const int r = kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        const half *from = sa + ((wa * kWide / 32 + x) * kDeep + r) * kDeep + col;
         typedef __attribute__((address_space(3))) short4v *shared4;
         const short4v lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from));
-        const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * T));
+        const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * kDeep));
         a[x] = __builtin_bit_cast(half8, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
       } else {
         const int ra = wa * kWide + x * 32 + low;
@@ -284,25 +395,74 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void k_products(Call c, Step
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
   };
 
-  constexpr int kPending = 2 * kLoads * (kRing - 2);
-  for (int t = 0; t < kRing && t < total; ++t) fetch(t);
-  if (total >= kRing)
+  constexpr int kPending = 2 * kLoads * (kStages - 2);
+  for (int s = 0; s < kStages && s < total; ++s) fetch(s, s);
+  if (total >= kStages)
     arrive<kPending + 2 * kLoads>();
   else
     arrive<0>();
   read(0, 0, fa[0], fb[0]);
-  for (int t = 0; t < total; ++t) {
-    read(t, 1, fa[1], fb[1]);
+  for (int s = 0, slot = 0; s < total; ++s) {
+    const int next = slot + 1 == kStages ? 0 : slot + 1;
+    read(slot, 1, fa[1], fb[1]);
     multiply(fa[0], fb[0]);
-    if (t + 1 < total) {
-      if (t + kRing <= total)
+    if (s + 1 < total) {
+      if (s + kStages <= total)
         arrive<kPending>();
       else
         arrive<0>();
-      if (t + kRing < total) fetch(t + kRing);  // where step t was: everybody has read it
-      read(t + 1, 0, fa[0], fb[0]);
+      if (s + kStages < total) fetch(s + kStages, slot);  // where step s was: everybody has read it
+      read(next, 0, fa[0], fb[0]);
     }
     multiply(fa[1], fb[1]);
+    slot = next;
+  }
+
+  // A tile in several shares: each leaves its sums in memory, and the one that comes last adds them all
+  // up, in their order whichever it is.  The sums pass the dies' separate L2 caches by themselves (8 bytes
+  // at a time, at the scope of the whole card); a fence would write all of L2 back, 120 us a launch.
+  if (it.pieces > 1) {
+    typedef unsigned long long two;
+    constexpr int64_t kTileSums = static_cast<int64_t>(T) * T / 2;
+    two *sums = reinterpret_cast<two *>(c.partial) + it.slot * kTileSums + threadIdx.x;
+#pragma unroll
+    for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+      for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+          __hip_atomic_store(sums + it.piece * kTileSums + ((x * kBlocks + y) * 8 + g) * 256,
+                             __builtin_bit_cast(two, f32x2{acc[x][y][2 * g], acc[x][y][2 * g + 1]}),
+                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they have reached memory
+    __syncthreads();
+    u32 *flag = reinterpret_cast<u32 *>(ring);
+    if (threadIdx.x == 0) {
+      const u32 before = __hip_atomic_fetch_add(c.tickets + it.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (before + 1 == static_cast<u32>(it.pieces))
+        __hip_atomic_store(c.tickets + it.ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      flag[0] = before;
+    }
+    __syncthreads();
+    if (flag[0] + 1 != static_cast<u32>(it.pieces)) return;
+#pragma unroll
+    for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+      for (int y = 0; y < kBlocks; ++y) {
+        f32x16 v;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = 0.f;
+        for (int p = 0; p < it.pieces; ++p)
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            const f32x2 w = __builtin_bit_cast(
+                f32x2, __hip_atomic_load(sums + p * kTileSums + ((x * kBlocks + y) * 8 + g) * 256, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT));
+            v[2 * g] += w[0];
+            v[2 * g + 1] += w[1];
+          }
+        acc[x][y] = v;
+      }
   }
   __syncthreads();
 
@@ -334,19 +494,43 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void k_products(Call c, Step
     for (int e = 0; e < 4; ++e) v[e] = p[e], v[4 + e] = q[e];
   };
   const int ai = it.j * T + wa * kWide, bi = it.i * T + wb * kWide;  // first place along each factor
+  // the 32 staged rows a panel's 16 rows at a time: 1024 bytes in a row of memory
+  auto panels = [&](int row0, int col0, auto &&f) {
+#pragma unroll
+    for (int q = 0; q < 2 * (kWide / kDeep); ++q) {
+      const int r = (q & 1) * 16 + (lane >> 2), col = (q >> 1) * kDeep + (lane & 3) * 8;
+      const f32x4 v0 = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + col),
+                  v1 = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + col + 4);
+      float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+      f(row0 + r, col0 + col, ((col0 + col) / kDeep) * panel + static_cast<int64_t>(row0 + r) * kDeep + (lane & 3) * 8, v);
+    }
+  };
 
-  if constexpr (PHASE == kUpdate) {
-    const Addresses at = c.addresses[it.matrix];
-    if (st.last && m.tall) {  // the caller's matrix is k x n: rows of factor a
-      const float scale = m.scale / (kScaleX * kScaleP);
+  if constexpr (UPDATE) {
+    if (st.last) {
+      const Addresses at = c.addresses[it.matrix];
+      const float scale = m.scale * st.alpha * (1.f / kScaleX);
+      if (m.tall) {  // the caller's matrix is k x n: rows of factor a
 #pragma unroll
-      for (int x = 0; x < kBlocks; ++x) {
-        turned(x);
+        for (int x = 0; x < kBlocks; ++x) {
+          turned(x);
 #pragma unroll
-        for (int r = 0; r < 32; r += kRows) {
-          float v[8];
-          take(r + sub, v);
-          write_out(c, at, m.ld, ai + x * 32 + r + sub, m.k, bi + c8, m.n, v, scale);
+          for (int r = 0; r < 32; r += kRows) {
+            float v[8];
+            take(r + sub, v);
+            write_out(c, at, m.ld, ai + x * 32 + r + sub, m.k, bi + c8, m.n, v, scale);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int y = 0; y < kBlocks; ++y) {
+          direct(y);
+#pragma unroll
+          for (int r = 0; r < 32; r += kRows) {
+            float v[8];
+            take(r + sub, v);
+            write_out(c, at, m.ld, bi + y * 32 + r + sub, m.n, ai + c8, m.k, v, scale);
+          }
         }
       }
       return;
@@ -354,75 +538,51 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 2) void k_products(Call c, Step
 #pragma unroll
     for (int y = 0; y < kBlocks; ++y) {
       direct(y);
-#pragma unroll
-      for (int r = 0; r < 32; r += kRows) {
-        const int row = bi + y * 32 + r + sub;
-        float v[8];
-        take(r + sub, v);
-        if (st.last) {
-          write_out(c, at, m.ld, row, m.n, ai + c8, m.k, v, m.scale / (kScaleX * kScaleP));
-          continue;
-        }
-        const int64_t pos = static_cast<int64_t>(row) * m.kp + ai + c8;
-        half8 nh, nl;
+      panels(bi + y * 32, ai, [&](int, int, int64_t pos, float *v) {
         if (st.carry) {
           const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.x[st.from] + pos);
           const half8 l = *reinterpret_cast<const half8 *>(c.arena + m.x_lo[0] + pos);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            v[e] = fmaf(st.a, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e] * (1.f / kScaleP));
+            v[e] = fmaf(st.beta, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e] * st.alpha);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= 1.f / kScaleP;
+          for (int e = 0; e < 8; ++e) v[e] *= st.alpha;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          half h, l;
-          split_half(v[e], h, l);
-          nh[e] = h;
-          nl[e] = l;
-        }
-        *reinterpret_cast<half8 *>(c.arena + m.x[1 - st.from] + pos) = nh;
+        half8 hi, lo;
+        split8(v, hi, lo);
+        *reinterpret_cast<half8 *>(c.arena + m.x[1 - st.from] + pos) = hi;
         if (SPLIT)
-          *reinterpret_cast<half8 *>(c.arena + m.x_lo[1 - st.from] + pos) = nl;
+          *reinterpret_cast<half8 *>(c.arena + m.x_lo[1 - st.from] + pos) = lo;
         else if (st.carry_next)
-          *reinterpret_cast<half8 *>(c.arena + m.x_lo[0] + pos) = nl;
-      }
+          *reinterpret_cast<half8 *>(c.arena + m.x_lo[0] + pos) = lo;
+      });
     }
   } else {
-    half *to_hi = c.arena + (PHASE == kGram ? m.a : m.p), *to_lo = c.arena + (PHASE == kGram ? m.a_lo : m.p_lo);
-    auto rows = [&](int row0, int col0) {  // 32 staged rows of the symmetric result
-#pragma unroll
-      for (int r = 0; r < 32; r += kRows) {
-        const int row = row0 + r + sub, col = col0 + c8;
-        const int64_t pos = static_cast<int64_t>(row) * m.np + col;
-        float v[8];
-        take(r + sub, v);
-        if constexpr (PHASE == kGram) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= kScaleA / (kScaleX * kScaleX);
-        } else {
-          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.a + pos);
+    auto rows = [&](int row0, int col0) {  // 32 staged rows of the result
+      panels(row0, col0, [&](int row, int col, int64_t pos, float *v) {
+        auto add = [&](int which, float by) {
+          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.square[which] + pos);
           half8 l;
-          if (SPLIT) l = *reinterpret_cast<const half8 *>(c.arena + m.a_lo + pos);
+          if (SPLIT) l = *reinterpret_cast<const half8 *>(c.arena + m.square_lo[which] + pos);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f);
-            v[e] = fmaf(st.b * (kScaleP / kScaleA), x, st.c * (kScaleP / (kScaleA * kScaleA)) * v[e]);
-            if (!st.carry && row == col + e) v[e] += st.a * kScaleP;
-          }
-        }
-        half8 nh, nl;
+          for (int e = 0; e < 8; ++e)
+            v[e] = fmaf(by, static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f), v[e]);
+        };
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          half h, l;
-          split_half(v[e], h, l);
-          nh[e] = h;
-          nl[e] = l;
+        for (int e = 0; e < 8; ++e) v[e] *= st.alpha;
+        if (st.first >= 0) add(st.first, st.beta);
+        if (st.second >= 0) add(st.second, st.gamma);
+        if (st.delta != 0.f) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (row == col + e) v[e] += st.delta;
         }
-        *reinterpret_cast<half8 *>(to_hi + pos) = nh;
-        if (SPLIT) *reinterpret_cast<half8 *>(to_lo + pos) = nl;
-      }
+        half8 hi, lo;
+        split8(v, hi, lo);
+        *reinterpret_cast<half8 *>(c.arena + m.square[st.out] + pos) = hi;
+        if (SPLIT) *reinterpret_cast<half8 *>(c.arena + m.square_lo[st.out] + pos) = lo;
+      });
     };
 #pragma unroll
     for (int y = 0; y < kBlocks; ++y) {
@@ -469,8 +629,7 @@ __global__ __launch_bounds__(kTinyThreads) void k_tiny(Call c, Steps steps, cons
   __syncthreads();
   sum = 0.;
   for (int w = 0; w < kTinyThreads / 64; ++w) sum += sums[w];
-  const double norm = sqrt(sum) + static_cast<double>(c.eps);
-  const double inverse = norm == 0. ? 0. : norm < 1.7e308 ? 1. / norm : __builtin_nan("");
+  const double inverse = inverse_norm(sum, c.eps);
   for (int e = tid; e < count; e += kTinyThreads) x[e] *= inverse;
   __syncthreads();
   // a group of lanes per element of A: few elements have long rows, many have short ones
@@ -529,13 +688,8 @@ hipError_t launch_addresses(const Call &c, const Few &few, int32_t first, int32_
   return hipGetLastError();
 }
 
-hipError_t launch_squares(const Call &c, const Item *items, int32_t count, hipStream_t s) {
-  k_squares<<<count, 256, 0, s>>>(c, items);
-  return hipGetLastError();
-}
-
-hipError_t launch_norms(const Call &c, int32_t matrices, hipStream_t s) {
-  k_norms<<<matrices, 256, 0, s>>>(c);
+hipError_t launch_sums(const Call &c, const Item *items, int32_t count, hipStream_t s) {
+  k_sums<<<count, 256, 0, s>>>(c, items);
   return hipGetLastError();
 }
 
@@ -545,43 +699,41 @@ hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStrea
 }
 
 namespace {
-template <int T>
-constexpr size_t shared_bytes() {
-  return sizeof(half) * kRing * 2 * T * kDeep;
-}
 
-template <typename F>
-hipError_t with_products(int tile, Phase phase, bool split, F &&f) {
+template <bool UPDATE, typename F>
+hipError_t with_products(int tile, bool split, F &&f) {
   auto sized = [&](auto t) {
     constexpr int T = t();
-    if (phase == kGram)
-      return split ? f(k_products<T, kGram, true>, shared_bytes<T>()) : f(k_products<T, kGram, false>, shared_bytes<T>());
-    if (phase == kPolynomial)
-      return split ? f(k_products<T, kPolynomial, true>, shared_bytes<T>())
-                   : f(k_products<T, kPolynomial, false>, shared_bytes<T>());
-    return split ? f(k_products<T, kUpdate, true>, shared_bytes<T>())
-                 : f(k_products<T, kUpdate, false>, shared_bytes<T>());
+    constexpr size_t bytes = sizeof(half) * kRing<T> * 2 * T * kDeep;
+    return split ? f(k_products<T, UPDATE, true>, bytes) : f(k_products<T, UPDATE, false>, bytes);
   };
   return tile == 256 ? sized(std::integral_constant<int, 256>{}) : sized(std::integral_constant<int, 128>{});
 }
+
 }  // namespace
 
 // More shared memory than a kernel may have unasked.
 hipError_t prepare_products(int tile, bool split) {
-  for (Phase p : {kGram, kPolynomial, kUpdate}) {
-    hipError_t e = with_products(tile, p, split, [](auto *k, size_t bytes) {
-      return hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                 static_cast<int>(bytes));
-    });
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  auto allow = [](auto *k, size_t bytes) {
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(bytes));
+  };
+  const hipError_t e = with_products<false>(tile, split, allow);
+  return e != hipSuccess ? e : with_products<true>(tile, split, allow);
 }
 
-hipError_t launch_products(const Call &c, int tile, Phase phase, const Step &st, const Item *items, int32_t count,
-                           bool split, hipStream_t s) {
-  return with_products(tile, phase, split, [&](auto *k, size_t bytes) {
-    k<<<count, 256, bytes, s>>>(c, st, items);
+hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const Tile *tiles, int32_t count,
+                            bool split, hipStream_t s) {
+  return with_products<false>(tile, split, [&](auto *k, size_t bytes) {
+    k<<<count, 256, bytes, s>>>(c, p, tiles);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_update(const Call &c, int tile, const Update &p, const Tile *tiles, int32_t count, bool split,
+                         hipStream_t s) {
+  return with_products<true>(tile, split, [&](auto *k, size_t bytes) {
+    k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
 }
