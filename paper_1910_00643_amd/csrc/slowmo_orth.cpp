@@ -230,15 +230,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   for (auto &list : of) {
     for (int32_t at : list) {
       Matrix &m = p.matrices[at];
-      const int64_t wide = static_cast<int64_t>(m.np) * m.kp, square = static_cast<int64_t>(m.np) * m.np;
-      const int32_t squares = p.pairs ? kSquares : 2;
-      for (int64_t &to : m.x) to = take(wide);
-      m.x_lo[0] = take(wide);
-      for (int32_t q = 0; q < squares; ++q) m.square[q] = take(square);
-      if (split) {
-        m.x_lo[1] = take(wide);
-        for (int32_t q = 0; q < squares; ++q) m.square_lo[q] = take(square);
-      }
+      m.at = take(Places(m.np, m.kp, p.pairs ? kSquares : 2).total(split));
       m.first_sum = sums;
       m.sums = static_cast<int32_t>(std::min<int64_t>(kMostSums, (static_cast<int64_t>(m.n) * m.k + 16383) / 16384));
       sums += m.sums;
@@ -258,7 +250,8 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     const int32_t tile = kTileOf[which], times = split ? 3 : 1;
     Lists &to = p.lists[which];
     auto put = [&](std::vector<Tile> &v, int32_t at, int32_t i, int32_t j, int32_t depth) {
-      v.push_back({at, i, j, 0, times * (depth / kDeep), 0, 1, 0, 0, {}});
+      const Matrix &m = p.matrices[at];
+      v.push_back({m.at, m.np, m.kp, i, j, 0, times * (depth / kDeep), 0, 1, 0, 0, at, {}});
     };
     for (int32_t at : grams) {
       const Matrix &m = p.matrices[at];
@@ -507,6 +500,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     h->call.tickets = reinterpret_cast<uint32_t *>(base + p.tickets_at);
     h->call.partial = reinterpret_cast<float *>(base + p.partial_at);
     h->call.arena = reinterpret_cast<_Float16 *>(base + p.arena_at);
+    h->call.buffers = p.pairs ? kSquares : 2;
     h->call.eps = cfg->eps;
     h->call.in_bf16 = cfg->in_dtype == SLOWMO_BF16;
     h->call.out_bf16 = cfg->out_dtype == SLOWMO_BF16;

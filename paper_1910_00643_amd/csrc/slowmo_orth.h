@@ -13,7 +13,7 @@ constexpr int kPatch = 64;       // side of an elementwise kernel's patch; kPatc
 constexpr int kPatches = 4;
 constexpr int kInline = 64;      // matrices whose addresses travel with one launch
 constexpr int kMostSums = 1024;  // workgroups that share a matrix's sum of squares
-constexpr int kSquares = 4;      // n x n buffers of a matrix: A, P, W, Q
+constexpr int kSquares = 4;      // n x n buffers of a matrix: A, P, W, Q (A, P where steps go one by one)
 
 // Matrices that one workgroup takes from load to store.
 constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
@@ -23,16 +23,26 @@ constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
 constexpr float kScaleX = 8192.f;
 
 // One matrix.  n <= k; X is n x k; np, kp: sides padded to whole tiles.  X and the n x n buffers lie in
-// panels of kDeep columns, [column / kDeep][row][column mod kDeep].  Offsets count halves from the start
-// of the arena; lo: the values' next 11 bits.
+// panels of kDeep columns, [column / kDeep][row][column mod kDeep].  From `at` on (halves from the start
+// of the arena): X, the X it is replaced by, X's lower halves (the values' next 11 bits), the n x n buffers;
+// where products are split, the other X's and the n x n buffers' lower halves after that.
 struct Matrix {
-  int64_t x[2], square[kSquares];
-  int64_t x_lo[2], square_lo[kSquares];  // x_lo[1], square_lo only where products are split
-  int64_t ld;
+  int64_t at, ld;
   int32_t n, k, np, kp;
   int32_t tall;                          // the caller's matrix is k x n
   float scale;
   int32_t first_sum, sums;               // its partial sums of squares
+};
+
+struct Places {
+  int64_t wide, square, squares;
+  __host__ __device__ Places(int64_t np, int64_t kp, int64_t buffers)
+      : wide(np * kp), square(np * np), squares(buffers) {}
+  __host__ __device__ int64_t x(int which) const { return which ? wide : 0; }
+  __host__ __device__ int64_t x_lo(int which) const { return which ? 3 * wide + squares * square : 2 * wide; }
+  __host__ __device__ int64_t buffer(int which) const { return 3 * wide + which * square; }
+  __host__ __device__ int64_t buffer_lo(int which) const { return 4 * wide + (squares + which) * square; }
+  __host__ __device__ int64_t total(bool split) const { return split ? buffer_lo(static_cast<int>(squares)) : buffer(static_cast<int>(squares)); }
 };
 
 // A workgroup's share of an elementwise phase: of a sum of squares (i of `j`), or the patches from
@@ -42,11 +52,16 @@ struct Item {
 };
 
 // A workgroup's share of a product: steps first..first + count - 1 of tile (i, j); where a tile is in
-// `pieces` > 1 shares, `slot` counts the places of their partial sums and `ticket` its counter.
+// `pieces` > 1 shares, `slot` counts the places of their partial sums and `ticket` its counter.  What it
+// needs of the matrix comes along: one load in front of the first of its data.
 struct Tile {
-  int32_t matrix, i, j, first, count, piece, pieces, slot;
-  int32_t ticket, pad[3];
+  int64_t at;                            // the matrix's first half in the arena
+  int32_t np, kp;
+  int32_t i, j, first, count;
+  int32_t piece, pieces, slot, ticket;
+  int32_t matrix, pad[3];
 };
+static_assert(sizeof(Tile) == 64, "one cache line's half");
 
 struct Addresses {
   const void *in;
@@ -68,16 +83,17 @@ struct Call {
   uint32_t *tickets;     // zero between calls
   float eps, mu;
   int32_t in_bf16, out_bf16, momentum, nesterov;
+  int32_t buffers;       // n x n buffers of a matrix
 };
 
 // out = alpha * left * right (+ beta * first) (+ gamma * second) (+ delta on the diagonal), symmetric;
-// buffers are places in Matrix::square, left = -1: X X^T.  The factors hold the buffers' powers of two.
+// buffers are numbered, left = -1: X X^T.  The factors hold the buffers' powers of two.
 struct Symmetric {
   int32_t from, left, right, first, second, out;  // first, second: -1: none
   float alpha, beta, gamma, delta;
 };
 
-// x[1 - from] = alpha * square[by] x[from] (+ beta * (hi + lo of x[from])); or the caller's result.
+// x[1 - from] = alpha * buffer[by] x[from] (+ beta * (hi + lo of x[from])); or the caller's result.
 struct Update {
   int32_t from, by, carry, carry_next, last;
   float alpha, beta;

@@ -18,6 +18,7 @@ namespace orth {
 namespace {
 
 typedef _Float16 half;
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -169,7 +170,8 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   const Matrix &m = c.matrices[it.matrix];
   const Addresses at = c.addresses[it.matrix];
   const int rows = m.tall ? m.k : m.n, cols = m.tall ? m.n : m.k, across = m.tall ? m.np : m.kp;
-  half *x = c.arena + m.x[0], *x_lo = c.arena + m.x_lo[0];
+  const Places places(m.np, m.kp, c.buffers);
+  half *x = c.arena + m.at, *x_lo = x + places.x_lo(0);
   __shared__ float turn[kPatch][kPatch + 1];
   __shared__ double shared[4];
   double squares = 0.;
@@ -265,8 +267,7 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // ---- products -----------------------------------------------------------------
 //
 // Tiles of T x T by 4 waves of T/2 x T/2.  Steps of 32 of the summed side go from memory straight to a
-// ring of kRing stages in shared memory (16 bytes a lane), kRing - 1 steps ahead of their use: memory's
-// latency is 0.7 us and a step's products take 0.25 us (T = 256).  A wave reads the next 16's factors into
+// ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead of their use.  A wave reads the next 16's factors into
 // registers before it issues the products of this 16, across the barrier of a step too, so that with
 // one wave per SIMD (T = 256: 256 accumulators a lane) the matrix cores go on.
 //
@@ -279,8 +280,6 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // 16 columns per 16 lanes, which meets all banks as it lies.
 // Everything is padded to whole tiles; nothing is checked in the loop.
 
-template <int T>
-constexpr int kRing = T == 256 ? 4 : 3;  // 128 and 48 KB: one workgroup per CU, or three
 
 __device__ __forceinline__ void to_shared(u32 shared, u32 offset, const half *base) {
   // m0 is written and read within this block; the wait covers its hazard and that of a base that a
@@ -300,40 +299,40 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
 
 // UPDATE: P X by Update, else a symmetric product by Symmetric.
-template <int T, bool UPDATE, bool SPLIT>
-__global__ __launch_bounds__(256, T == 256 ? 1 : 3) void k_products(
+template <int T, int STAGES, bool UPDATE, bool SPLIT>
+__global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 3) void k_products(
     Call c, std::conditional_t<UPDATE, Update, Symmetric> st, const Tile *tiles) {
   extern __shared__ half ring[];
-  constexpr int kStages = kRing<T>;
   constexpr int kBlocks = T / 64;            // blocks of 32 x 32 along a side of a wave's share
   constexpr int kShare = T * kDeep;          // halves of one factor in a stage
   constexpr int kLoads = kShare * 2 / 1024 / 4;  // loads of a wave per factor and stage
   constexpr int kWide = T / 2;               // side of a wave's share
   const Tile it = tiles[blockIdx.x];
-  const Matrix &m = c.matrices[it.matrix];
+  const Places places(it.np, it.kp, c.buffers);
+  half *const arena = c.arena + it.at;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave & 1, wb = wave >> 1;
   const int low = lane & 31, high = lane >> 5;
 
   // factor a: columns of the tile (j), factor b: rows (i).  The accumulators' four neighbours run along a.
   int64_t a_hi, a_lo, b_hi, b_lo;
-  int depth = m.np;
+  int depth = it.np;
   if constexpr (UPDATE) {
-    a_hi = m.x[st.from];
-    a_lo = m.x_lo[st.from];
-    b_hi = m.square[st.by];
-    b_lo = m.square_lo[st.by];
+    a_hi = places.x(st.from);
+    a_lo = places.x_lo(st.from);
+    b_hi = places.buffer(st.by);
+    b_lo = places.buffer_lo(st.by);
   } else if (st.left < 0) {
-    depth = m.kp;
-    a_hi = b_hi = m.x[st.from];
-    a_lo = b_lo = m.x_lo[st.from];
+    depth = it.kp;
+    a_hi = b_hi = places.x(st.from);
+    a_lo = b_lo = places.x_lo(st.from);
   } else {
-    a_hi = m.square[st.right];
-    a_lo = m.square_lo[st.right];
-    b_hi = m.square[st.left];
-    b_lo = m.square_lo[st.left];
+    a_hi = places.buffer(st.right);
+    a_lo = places.buffer_lo(st.right);
+    b_hi = places.buffer(st.left);
+    b_lo = places.buffer_lo(st.left);
   }
-  const int64_t panel = static_cast<int64_t>(m.np) * kDeep;
+  const int64_t panel = static_cast<int64_t>(it.np) * kDeep;
   const int64_t a_at = UPDATE ? static_cast<int64_t>(it.j) * (T / kDeep) * panel : static_cast<int64_t>(it.j) * T * kDeep;
   const int64_t a_step = UPDATE ? kDeep * kDeep : panel;
   const int64_t b_at = static_cast<int64_t>(it.i) * T * kDeep;
@@ -348,8 +347,8 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 3) void k_products(
     // split: the small products first (hi lo, lo hi), while their sums are small, then hi hi
     const int t = it.first + s, seg = SPLIT ? (t >= 2 * steps ? 2 : t >= steps ? 1 : 0) : 2;
     const int at = SPLIT ? t - seg * steps : t;
-    const half *a = c.arena + (seg == 1 ? a_lo : a_hi) + a_at + at * a_step;
-    const half *b = c.arena + (seg == 0 ? b_lo : b_hi) + b_at + at * panel;
+    const half *a = arena + (seg == 1 ? a_lo : a_hi) + a_at + at * a_step;
+    const half *b = arena + (seg == 0 ? b_lo : b_hi) + b_at + at * panel;
     const u32 to = shared0 + slot * (2 * kShare * 2);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
@@ -395,23 +394,23 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 3) void k_products(
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
   };
 
-  constexpr int kPending = 2 * kLoads * (kStages - 2);
-  for (int s = 0; s < kStages && s < total; ++s) fetch(s, s);
-  if (total >= kStages)
+  constexpr int kPending = 2 * kLoads * (STAGES - 2);
+  for (int s = 0; s < STAGES && s < total; ++s) fetch(s, s);
+  if (total >= STAGES)
     arrive<kPending + 2 * kLoads>();
   else
     arrive<0>();
   read(0, 0, fa[0], fb[0]);
   for (int s = 0, slot = 0; s < total; ++s) {
-    const int next = slot + 1 == kStages ? 0 : slot + 1;
+    const int next = slot + 1 == STAGES ? 0 : slot + 1;
     read(slot, 1, fa[1], fb[1]);
     multiply(fa[0], fb[0]);
     if (s + 1 < total) {
-      if (s + kStages <= total)
+      if (s + STAGES <= total)
         arrive<kPending>();
       else
         arrive<0>();
-      if (s + kStages < total) fetch(s + kStages, slot);  // where step s was: everybody has read it
+      if (s + STAGES < total) fetch(s + STAGES, slot);  // where step s was: everybody has read it
       read(next, 0, fa[0], fb[0]);
     }
     multiply(fa[1], fb[1]);
@@ -466,134 +465,153 @@ __global__ __launch_bounds__(256, T == 256 ? 1 : 3) void k_products(
   }
   __syncthreads();
 
-  // The results pass through shared memory, 32 rows of a wave's share at a time, to leave in whole rows.
-  constexpr int kPitch = kWide + 4, kLanes = kWide / 8, kRows = 64 / kLanes;
-  float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
-  const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
-  // rows y of factor b, along a
-  auto direct = [&](int y) {
-#pragma unroll
-    for (int x = 0; x < kBlocks; ++x)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4 *>(stage + low * kPitch + x * 32 + g * 8 + high * 4) =
-            f32x4{acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-  };
-  // rows x of factor a, along b
-  auto turned = [&](int x) {
-#pragma unroll
-    for (int y = 0; y < kBlocks; ++y)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        stage[((r >> 2) * 8 + high * 4 + (r & 3)) * kPitch + y * 32 + low] = acc[x][y][r];
-  };
-  auto take = [&](int r, float *v) {
-    const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + c8),
-                q = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + c8 + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = p[e], v[4 + e] = q[e];
-  };
   const int ai = it.j * T + wa * kWide, bi = it.i * T + wb * kWide;  // first place along each factor
-  // the 32 staged rows a panel's 16 rows at a time: 1024 bytes in a row of memory
-  auto panels = [&](int row0, int col0, auto &&f) {
-#pragma unroll
-    for (int q = 0; q < 2 * (kWide / kDeep); ++q) {
-      const int r = (q & 1) * 16 + (lane >> 2), col = (q >> 1) * kDeep + (lane & 3) * 8;
-      const f32x4 v0 = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + col),
-                  v1 = *reinterpret_cast<const f32x4 *>(stage + r * kPitch + col + 4);
-      float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-      f(row0 + r, col0 + col, ((col0 + col) / kDeep) * panel + static_cast<int64_t>(row0 + r) * kDeep + (lane & 3) * 8, v);
-    }
-  };
-
   if constexpr (UPDATE) {
     if (st.last) {
+      // The caller's rows: results pass through shared memory, 32 rows of a wave's share at a time.
+      constexpr int kPitch = kWide + 4, kLanes = kWide / 8, kRows = 64 / kLanes;
+      float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
+      const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
+      const Matrix &m = c.matrices[it.matrix];
       const Addresses at = c.addresses[it.matrix];
       const float scale = m.scale * st.alpha * (1.f / kScaleX);
-      if (m.tall) {  // the caller's matrix is k x n: rows of factor a
+      auto leave = [&](int row0, int rows, int col0, int cols) {
+#pragma unroll
+        for (int r = 0; r < 32; r += kRows) {
+          const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8),
+                      q = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8 + 4);
+          const float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+          write_out(c, at, m.ld, row0 + r + sub, rows, col0 + c8, cols, v, scale);
+        }
+      };
+      if (m.tall) {  // k x n: rows along factor a
 #pragma unroll
         for (int x = 0; x < kBlocks; ++x) {
-          turned(x);
 #pragma unroll
-          for (int r = 0; r < 32; r += kRows) {
-            float v[8];
-            take(r + sub, v);
-            write_out(c, at, m.ld, ai + x * 32 + r + sub, m.k, bi + c8, m.n, v, scale);
-          }
+          for (int y = 0; y < kBlocks; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              stage[((r >> 2) * 8 + high * 4 + (r & 3)) * kPitch + y * 32 + low] = acc[x][y][r];
+          leave(ai + x * 32, m.k, bi, m.n);
         }
       } else {
 #pragma unroll
         for (int y = 0; y < kBlocks; ++y) {
-          direct(y);
 #pragma unroll
-          for (int r = 0; r < 32; r += kRows) {
-            float v[8];
-            take(r + sub, v);
-            write_out(c, at, m.ld, bi + y * 32 + r + sub, m.n, ai + c8, m.k, v, scale);
-          }
+          for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *reinterpret_cast<f32x4 *>(stage + low * kPitch + x * 32 + g * 8 + high * 4) =
+                  f32x4{acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
+          leave(bi + y * 32, m.n, ai, m.k);
         }
       }
       return;
     }
+  }
+
+  // A block of 32 x 32 is 2 KB in one piece, row `low` of it 64 bytes of which a lane holds four times 8.
+  // It passes through shared memory to leave in stores of 1 KB; read turned there, it is its
+  // mirror image's block.  Pieces of 16 bytes are placed as the factors' are.
+  half *block = ring + wave * 2048;  // hi, lo
+  auto place = [&](int row, int col) { return row * kDeep + (((col >> 3) ^ ((row >> 2) & 3)) * 8) + (col & 7); };
+  auto where = [&](int row, int col) { return static_cast<int64_t>(col >> 5) * panel + static_cast<int64_t>(row) * kDeep; };
+  auto put = [&](int part, int g, const half4 &v) {
+    *reinterpret_cast<half4 *>(block + part * 1024 + place(low, g * 8 + high * 4)) = v;
+  };
+  auto leave = [&](int part, half *to) {
 #pragma unroll
-    for (int y = 0; y < kBlocks; ++y) {
-      direct(y);
-      panels(bi + y * 32, ai, [&](int, int, int64_t pos, float *v) {
-        if (st.carry) {
-          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.x[st.from] + pos);
-          const half8 l = *reinterpret_cast<const half8 *>(c.arena + m.x_lo[0] + pos);
+    for (int q = 0; q < 2; ++q) {
+      const int row = q * 16 + (lane >> 2), col = (lane & 3) * 8;
+      *reinterpret_cast<half8 *>(to + row * kDeep + col) =
+          *reinterpret_cast<const half8 *>(block + part * 1024 + place(row, col));
+    }
+  };
+  auto leave_turned = [&](int part, half *to) {
+    typedef __attribute__((address_space(3))) short4v *shared4;
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            v[e] = fmaf(st.beta, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e] * st.alpha);
+    for (int q = 0; q < 2; ++q) {  // column q * 16 + lane mod 16, rows (lane / 16) * 8 and on
+      const int row = (lane >> 4) * 8 + ((lane >> 2) & 3), col = q * 16 + (lane & 3) * 4;
+      const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(block + part * 1024 + place(row, col)));
+      const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(block + part * 1024 + place(row + 4, col)));
+      *reinterpret_cast<short8v *>(to + (q * 16 + (lane & 15)) * kDeep + (lane >> 4) * 8) =
+          __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  };
+  auto four = [&](const half *from, int g) { return *reinterpret_cast<const half4 *>(from + low * kDeep + g * 8 + high * 4); };
+#pragma unroll
+  for (int y = 0; y < kBlocks; ++y) {
+    // What is added to a row of blocks, all of it asked for before any of it is used.
+    constexpr int kMore = UPDATE || !SPLIT ? 2 : 4;
+    half4 more[kBlocks][kMore][4];
+    asm volatile("" ::: "memory");  // and no earlier: the registers would not hold it
+#pragma unroll
+    for (int x = 0; x < kBlocks; ++x) {
+      const int64_t pos = where(bi + y * 32, ai + x * 32);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if constexpr (UPDATE) {
+          if (st.carry) {
+            more[x][0][g] = four(arena + places.x(st.from) + pos, g);
+            more[x][1][g] = four(arena + places.x_lo(0) + pos, g);
+          }
         } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= st.alpha;
+          constexpr int kNext = SPLIT ? 2 : 1;
+          if (st.first >= 0) {
+            more[x][0][g] = four(arena + places.buffer(st.first) + pos, g);
+            if (SPLIT) more[x][1][g] = four(arena + places.buffer_lo(st.first) + pos, g);
+          }
+          if (st.second >= 0) {
+            more[x][kNext][g] = four(arena + places.buffer(st.second) + pos, g);
+            if (SPLIT) more[x][kNext + 1][g] = four(arena + places.buffer_lo(st.second) + pos, g);
+          }
         }
-        half8 hi, lo;
-        split8(v, hi, lo);
-        *reinterpret_cast<half8 *>(c.arena + m.x[1 - st.from] + pos) = hi;
-        if (SPLIT)
-          *reinterpret_cast<half8 *>(c.arena + m.x_lo[1 - st.from] + pos) = lo;
-        else if (st.carry_next)
-          *reinterpret_cast<half8 *>(c.arena + m.x_lo[0] + pos) = lo;
-      });
+      }
     }
-  } else {
-    auto rows = [&](int row0, int col0) {  // 32 staged rows of the result
-      panels(row0, col0, [&](int row, int col, int64_t pos, float *v) {
-        auto add = [&](int which, float by) {
-          const half8 h = *reinterpret_cast<const half8 *>(c.arena + m.square[which] + pos);
-          half8 l;
-          if (SPLIT) l = *reinterpret_cast<const half8 *>(c.arena + m.square_lo[which] + pos);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            v[e] = fmaf(by, static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f), v[e]);
-        };
+    for (int x = 0; x < kBlocks; ++x) {
+      const int row0 = bi + y * 32, col0 = ai + x * 32;
+      const int64_t pos = where(row0, col0);
+      half4 hi[4], lo[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= st.alpha;
-        if (st.first >= 0) add(st.first, st.beta);
-        if (st.second >= 0) add(st.second, st.gamma);
-        if (st.delta != 0.f) {
+      for (int g = 0; g < 4; ++g) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (row == col + e) v[e] += st.delta;
+        for (int e = 0; e < 4; ++e) {
+          float v = acc[x][y][4 * g + e] * st.alpha;
+          if constexpr (UPDATE) {
+            if (st.carry) v = fmaf(st.beta, static_cast<float>(more[x][0][g][e]) + static_cast<float>(more[x][1][g][e]), v);
+          } else {
+            auto value = [&](int which) {
+              const float h = static_cast<float>(more[x][which][g][e]);
+              return SPLIT ? h + static_cast<float>(more[x][which + 1][g][e]) : h;
+            };
+            if (st.first >= 0) v = fmaf(st.beta, value(0), v);
+            if (st.second >= 0) v = fmaf(st.gamma, value(SPLIT ? 2 : 1), v);
+            if (row0 + low == col0 + g * 8 + high * 4 + e) v += st.delta;
+          }
+          half h, l;
+          split_half(v, h, l);
+          hi[g][e] = h;
+          lo[g][e] = l;
         }
-        half8 hi, lo;
-        split8(v, hi, lo);
-        *reinterpret_cast<half8 *>(c.arena + m.square[st.out] + pos) = hi;
-        if (SPLIT) *reinterpret_cast<half8 *>(c.arena + m.square_lo[st.out] + pos) = lo;
-      });
-    };
+      }
+      const bool keep_lo = SPLIT || (UPDATE && [&] { if constexpr (UPDATE) return st.carry_next != 0; else return false; }());
 #pragma unroll
-    for (int y = 0; y < kBlocks; ++y) {
-      direct(y);
-      rows(bi + y * 32, ai);
-    }
-    if (it.i != it.j) {
-#pragma unroll
-      for (int x = 0; x < kBlocks; ++x) {
-        turned(x);
-        rows(ai + x * 32, bi);
+      for (int g = 0; g < 4; ++g) {
+        put(0, g, hi[g]);
+        if (keep_lo) put(1, g, lo[g]);
+      }
+      if constexpr (UPDATE) {
+        leave(0, arena + places.x(1 - st.from) + pos);
+        if (keep_lo) leave(1, arena + places.x_lo(SPLIT ? 1 - st.from : 0) + pos);
+      } else {
+        leave(0, arena + places.buffer(st.out) + pos);
+        if (SPLIT) leave(1, arena + places.buffer_lo(st.out) + pos);
+        if (it.i != it.j) {
+          const int64_t mirror = where(col0, row0);
+          leave_turned(0, arena + places.buffer(st.out) + mirror);
+          if (SPLIT) leave_turned(1, arena + places.buffer_lo(st.out) + mirror);
+        }
       }
     }
   }
@@ -700,14 +718,20 @@ hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStrea
 
 namespace {
 
+// Workgroups per CU there is room for: with few of them a deeper ring hides more of memory's latency.
+// Block of the Transformer-big shapes, 216 tiles a launch: 22 us with 3 stages, STAGES9 with 9.
 template <bool UPDATE, typename F>
-hipError_t with_products(int tile, bool split, F &&f) {
-  auto sized = [&](auto t) {
-    constexpr int T = t();
-    constexpr size_t bytes = sizeof(half) * kRing<T> * 2 * T * kDeep;
-    return split ? f(k_products<T, UPDATE, true>, bytes) : f(k_products<T, UPDATE, false>, bytes);
+hipError_t with_products(int tile, int32_t count, bool split, F &&f) {
+  auto sized = [&](auto t, auto stages) {
+    constexpr int T = t(), S = stages();
+    constexpr size_t bytes = sizeof(half) * S * 2 * T * kDeep;
+    return split ? f(k_products<T, S, UPDATE, true>, bytes) : f(k_products<T, S, UPDATE, false>, bytes);
   };
-  return tile == 256 ? sized(std::integral_constant<int, 256>{}) : sized(std::integral_constant<int, 128>{});
+  std::integral_constant<int, 128> small;
+  if (tile == 256) return sized(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  if (count <= 256) return sized(small, std::integral_constant<int, 9>{});
+  if (count <= 512) return sized(small, std::integral_constant<int, 5>{});
+  return sized(small, std::integral_constant<int, 3>{});
 }
 
 }  // namespace
@@ -718,13 +742,17 @@ hipError_t prepare_products(int tile, bool split) {
     return hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
                                static_cast<int>(bytes));
   };
-  const hipError_t e = with_products<false>(tile, split, allow);
-  return e != hipSuccess ? e : with_products<true>(tile, split, allow);
+  for (int32_t count : {256, 512, 768}) {
+    hipError_t e = with_products<false>(tile, count, split, allow);
+    if (e == hipSuccess) e = with_products<true>(tile, count, split, allow);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const Tile *tiles, int32_t count,
                             bool split, hipStream_t s) {
-  return with_products<false>(tile, split, [&](auto *k, size_t bytes) {
+  return with_products<false>(tile, count, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
@@ -732,7 +760,7 @@ hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const T
 
 hipError_t launch_update(const Call &c, int tile, const Update &p, const Tile *tiles, int32_t count, bool split,
                          hipStream_t s) {
-  return with_products<true>(tile, split, [&](auto *k, size_t bytes) {
+  return with_products<true>(tile, count, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
