@@ -12,6 +12,7 @@
 #include "slowmo_orth.h"
 
 #include <type_traits>
+#include <utility>
 
 namespace slowmo {
 namespace orth {
@@ -281,11 +282,10 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // Everything is padded to whole tiles; nothing is checked in the loop.
 
 
+// m0 is written and read within the block, with the one wait between that the two need; no vector register
+// is written.  `base` comes from scalar instructions.
 __device__ __forceinline__ void to_shared(u32 shared, u32 offset, const half *base) {
-  // m0 is written and read within this block; the wait covers its hazard and that of a base that a
-  // vector instruction has just brought to scalar registers.  No vector register is written.
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(shared), "v"(offset),
-               "s"(base)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(shared), "v"(offset), "s"(base)
                : "memory");
 }
 // All but the N newest loads of this wave have arrived, its reads of shared memory are done, and so it is
@@ -293,6 +293,11 @@ __device__ __forceinline__ void to_shared(u32 shared, u32 offset, const half *ba
 template <int N>
 __device__ __forceinline__ void arrive() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int... N, typename F>
+__device__ __forceinline__ void each(std::integer_sequence<int, N...>, F &&f) {
+  (f(std::integral_constant<int, N>{}), ...);
 }
 
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -342,19 +347,29 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
   const u32 b_off = ((lane & ~3) | ((lane & 3) ^ ((lane >> 4) & 3))) * 16, a_off = UPDATE ? lane * 16 : b_off;
   const u32 shared0 = static_cast<u32>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half *)ring));
 
+  // The next step to fetch.  Split: the small products first (hi lo, lo hi), while their sums are small, then
+  // hi hi; `left` steps until the next of the three.
   const int total = it.count;
-  auto fetch = [&](int s, int slot) {
-    // split: the small products first (hi lo, lo hi), while their sums are small, then hi hi
-    const int t = it.first + s, seg = SPLIT ? (t >= 2 * steps ? 2 : t >= steps ? 1 : 0) : 2;
-    const int at = SPLIT ? t - seg * steps : t;
-    const half *a = arena + (seg == 1 ? a_lo : a_hi) + a_at + at * a_step;
-    const half *b = arena + (seg == 0 ? b_lo : b_hi) + b_at + at * panel;
-    const u32 to = shared0 + slot * (2 * kShare * 2);
+  int segment = SPLIT ? it.first / steps : 2, left = steps;
+  const half *a_next, *b_next;
+  auto enter = [&](int at) {
+    a_next = arena + (segment == 1 ? a_lo : a_hi) + a_at + wave * kLoads * (UPDATE ? panel / 2 : 512) + at * a_step;
+    b_next = arena + (segment == 0 ? b_lo : b_hi) + b_at + wave * kLoads * 512 + at * panel;
+    left = steps - at;
+  };
+  enter(SPLIT ? it.first - segment * steps : it.first);
+  auto fetch = [&](int slot) {
+    const u32 to = shared0 + slot * (2 * kShare * 2) + wave * kLoads * 1024;
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {
-      const int load = wave * kLoads + q;  // two to a panel's 32 rows
-      to_shared(to + load * 1024, a_off, a + (UPDATE ? (load >> 1) * panel + (load & 1) * 512 : load * 512));
-      to_shared(to + kShare * 2 + load * 1024, b_off, b + load * 512);
+    for (int q = 0; q < kLoads; ++q) {  // of X for P X, two loads to a panel's 32 rows
+      to_shared(to + q * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
+      to_shared(to + kShare * 2 + q * 1024, b_off, b_next + q * 512);
+    }
+    a_next += a_step;
+    b_next += panel;
+    if (SPLIT && --left == 0 && segment < 2) {
+      ++segment;
+      enter(0);
     }
   };
 
@@ -394,28 +409,39 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
   };
 
-  constexpr int kPending = 2 * kLoads * (STAGES - 2);
-  for (int s = 0; s < STAGES && s < total; ++s) fetch(s, s);
+  constexpr int kStep = 2 * kLoads;  // loads of a wave in a step
+  for (int s = 0; s < STAGES && s < total; ++s) fetch(s);
   if (total >= STAGES)
-    arrive<kPending + 2 * kLoads>();
+    arrive<kStep * (STAGES - 1)>();
   else
     arrive<0>();
   read(0, 0, fa[0], fb[0]);
-  for (int s = 0, slot = 0; s < total; ++s) {
-    const int next = slot + 1 == STAGES ? 0 : slot + 1;
+  int s = 0, slot = 0;
+  auto after = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
+  for (; s + STAGES < total; ++s) {
     read(slot, 1, fa[1], fb[1]);
     multiply(fa[0], fb[0]);
-    if (s + 1 < total) {
-      if (s + STAGES <= total)
-        arrive<kPending>();
-      else
-        arrive<0>();
-      if (s + STAGES < total) fetch(s + STAGES, slot);  // where step s was: everybody has read it
-      read(next, 0, fa[0], fb[0]);
-    }
+    arrive<kStep * (STAGES - 2)>();
+    fetch(slot);  // where step s was: everybody has read it
+    slot = after(slot);
+    read(slot, 0, fa[0], fb[0]);
     multiply(fa[1], fb[1]);
-    slot = next;
   }
+  // nothing is left to fetch; what is on its way arrives one step after the other
+  auto drain = [&](auto pending) {
+    if (total - s != decltype(pending)::value / kStep + 2) return;
+    read(slot, 1, fa[1], fb[1]);
+    multiply(fa[0], fb[0]);
+    arrive<decltype(pending)::value>();
+    slot = after(slot);
+    read(slot, 0, fa[0], fb[0]);
+    multiply(fa[1], fb[1]);
+    ++s;
+  };
+  each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) { drain(std::integral_constant<int, kStep * (STAGES - 2 - n())>{}); });
+  read(slot, 1, fa[1], fb[1]);
+  multiply(fa[0], fb[0]);
+  multiply(fa[1], fb[1]);
 
   // A tile in several shares: each leaves its sums in memory, and the one that comes last adds them all
   // up, in their order whichever it is.  The sums pass the dies' separate L2 caches by themselves (8 bytes
