@@ -34,10 +34,6 @@ struct Device {
   int32_t n_gram = 0, n_square = 0, n_update = 0;
 };
 
-constexpr int kClasses = 2;
-constexpr int32_t kTileOf[kClasses] = {128, 256};
-constexpr int32_t kSlotsOf[kClasses] = {768, 256};  // workgroups that run at a time
-
 }  // namespace
 
 struct slowmo_orth {
@@ -49,7 +45,7 @@ struct slowmo_orth {
   const Item *sums = nullptr, *load = nullptr;
   const int32_t *tiny = nullptr;
   int32_t n_tiny = 0, n_sums = 0, n_load = 0;
-  Device tiles[kClasses];
+  Device tiles[kKinds];
 };
 
 namespace {
@@ -66,11 +62,11 @@ struct Plan {
   std::vector<Matrix> matrices;
   std::vector<int32_t> index, tiny;
   std::vector<Item> sums, load;
-  Lists lists[kClasses];
+  Lists lists[kKinds];
   int64_t partial_sums = 0;   // floats
   int32_t tickets = 0;
   size_t matrices_at = 0, addresses_at = 0, sums_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
-         tiles_at[kClasses][3] = {}, tickets_at = 0, partial_at = 0, arena_at = 0, total = 0;
+         tiles_at[kKinds][3] = {}, tickets_at = 0, partial_at = 0, arena_at = 0, total = 0;
 };
 
 const char *check(const slowmo_orth_config *c, int32_t n, const int64_t *rows, const int64_t *cols,
@@ -95,16 +91,18 @@ const char *check(const slowmo_orth_config *c, int32_t n, const int64_t *rows, c
   return nullptr;
 }
 
-// Tiles of a grid in blocks of 4 x 8, which 32 neighbouring workgroups share factors in.
+// Tiles of a grid in bands of 8 rows, down each column of a band: neighbours share the columns' factor,
+// which for P X is the long one.
 template <typename F>
 void walk(int32_t down, int32_t across, F &&f) {
-  for (int32_t a0 = 0; a0 < down; a0 += 4)
-    for (int32_t b0 = 0; b0 < across; b0 += 8)
-      for (int32_t a = a0; a < std::min(down, a0 + 4); ++a)
-        for (int32_t b = b0; b < std::min(across, b0 + 8); ++b) f(a, b);
+  for (int32_t a0 = 0; a0 < down; a0 += 8)
+    for (int32_t b = 0; b < across; ++b)
+      for (int32_t a = a0; a < std::min(down, a0 + 8); ++a) f(a, b);
 }
 
-// Workgroups go to the 8 dies in turn: of every 256, each die gets 32 neighbours of the list.
+// Workgroups go to the 8 dies in turn, each with an L2 of its own: of every 256, each die gets 32
+// neighbours of the list.  (96, all that a die runs at once, gave one die the list's longest sums:
+// 1.10-1.15 of a call's time on ResNet lists.)
 std::vector<Tile> spread(const std::vector<Tile> &v) {
   std::vector<Tile> out(v.size());
   for (size_t base = 0; base < v.size(); base += 256) {
@@ -121,7 +119,8 @@ std::vector<Tile> spread(const std::vector<Tile> &v) {
 // for the length of its longest tile: its tiles are cut along the summed side into shares of about equal
 // length, as many as there are slots.  Shares are no shorter than 32 steps and no more than 16 to
 // a tile, since the last one adds the others' sums up.
-void balance(std::vector<Tile> &v, int32_t slots, int64_t tile, Plan &p) {
+void balance(std::vector<Tile> &v, int kind, Plan &p) {
+  const int32_t slots = kSlotsOf[kind];
   const size_t whole = v.size() / slots * slots;
   if (whole == v.size()) return;
   int32_t longest = 0;
@@ -161,7 +160,7 @@ void balance(std::vector<Tile> &v, int32_t slots, int64_t tile, Plan &p) {
     slot += pieces;
     ++ticket;
   }
-  p.partial_sums = std::max(p.partial_sums, slot * tile * tile);
+  p.partial_sums = std::max(p.partial_sums, slot * kRowsOf[kind] * kColsOf[kind]);
   p.tickets = std::max(p.tickets, ticket);
   v.swap(out);
 }
@@ -172,6 +171,9 @@ void balance(std::vector<Tile> &v, int32_t slots, int64_t tile, Plan &p) {
 bool large_tiles(const Matrix &m) {
   return m.n >= 2048 && static_cast<int64_t>(m.n) * m.k >= int64_t(256) * 256 * 256;
 }
+
+// Rows of 256 for P X: three quarters of the traffic per product, two workgroups per CU.
+bool wide_tiles(const Matrix &m) { return m.n >= 256 && m.kp % 256 == 0; }
 
 float factor(const slowmo_orth_config &c, int64_t rows, int64_t cols) {
   const double r = static_cast<double>(rows), k = static_cast<double>(cols);
@@ -193,7 +195,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   Plan p;
   const bool split = c.out_dtype == SLOWMO_F32;
   double one_by_one = 0., by_pairs = 0.;
-  std::vector<int32_t> of[kClasses];
+  std::vector<int32_t> of[2];  // matrices in small and in large tiles
   for (int32_t i = 0; i < n_matrices; ++i) {
     if (!rows[i] || !cols[i]) continue;
     Matrix m{};
@@ -208,8 +210,8 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     } else {
       const int which = large_tiles(m);
       of[which].push_back(at);
-      m.np = static_cast<int32_t>(up(m.n, kTileOf[which]));
-      m.kp = static_cast<int32_t>(up(m.k, kTileOf[which]));
+      m.np = static_cast<int32_t>(up(m.n, kRowsOf[which]));
+      m.kp = static_cast<int32_t>(up(m.k, kRowsOf[which]));
       const double n = m.np, k = m.kp;
       one_by_one += 6. * n * n * k + 2. * n * n * n;
       by_pairs += 3. * n * n * k + 5. * n * n * n;
@@ -240,34 +242,49 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
         for (int32_t b = 0; b < across; b += kPatches) p.load.push_back({at, a, b, 0});
     }
   }
-  for (int which = 0; which < kClasses; ++which) {
+  for (int which : {kSmall, kLarge}) {
     auto grams = of[which], updates = of[which];
     auto by = [&](auto side) {
       return [&p, side](int32_t a, int32_t b) { return p.matrices[a].*side > p.matrices[b].*side; };
     };
     std::stable_sort(grams.begin(), grams.end(), by(&Matrix::kp));  // long sums first
     std::stable_sort(updates.begin(), updates.end(), by(&Matrix::np));
-    const int32_t tile = kTileOf[which], times = split ? 3 : 1;
-    Lists &to = p.lists[which];
+    const int32_t side = kRowsOf[which], times = split ? 3 : 1;
     auto put = [&](std::vector<Tile> &v, int32_t at, int32_t i, int32_t j, int32_t depth) {
       const Matrix &m = p.matrices[at];
       v.push_back({m.at, m.np, m.kp, i, j, 0, times * (depth / kDeep), 0, 1, 0, 0, at, {}});
     };
+    Lists &to = p.lists[which];
     for (int32_t at : grams) {
       const Matrix &m = p.matrices[at];
-      walk(m.np / tile, m.np / tile, [&](int32_t i, int32_t j) {
+      walk(m.np / side, m.np / side, [&](int32_t i, int32_t j) {
         if (j <= i) put(to.gram, at, i, j, m.kp);
       });
     }
     for (int32_t at : updates) {
       const Matrix &m = p.matrices[at];
-      walk(m.np / tile, m.np / tile, [&](int32_t i, int32_t j) {
+      walk(m.np / side, m.np / side, [&](int32_t i, int32_t j) {
         if (j <= i) put(to.square, at, i, j, m.np);
       });
-      walk(m.np / tile, m.kp / tile, [&](int32_t i, int32_t j) { put(to.update, at, i, j, m.np); });
+      const int kind = which == kSmall && wide_tiles(m) ? kWide : which;
+      walk(m.np / side, m.kp / kColsOf[kind], [&](int32_t i, int32_t j) { put(p.lists[kind].update, at, i, j, m.np); });
     }
-    for (std::vector<Tile> *v : {&to.gram, &to.square, &to.update}) {
-      balance(*v, kSlotsOf[which], tile, p);
+  }
+  if (p.lists[kWide].update.size() < 512) {  // too few to fill the card: as small ones
+    for (const Tile &t : p.lists[kWide].update)
+      for (int32_t half : {0, 1}) {
+        Tile s = t;
+        s.j = 2 * t.j + half;
+        p.lists[kSmall].update.push_back(s);
+      }
+    p.lists[kWide].update.clear();
+    std::stable_sort(p.lists[kSmall].update.begin(), p.lists[kSmall].update.end(),
+                     [](const Tile &a, const Tile &b) { return a.count > b.count; });
+  }
+  for (int kind = 0; kind < kKinds; ++kind) {
+    Lists &l = p.lists[kind];
+    for (std::vector<Tile> *v : {&l.gram, &l.square, &l.update}) {
+      balance(*v, kind, p);
       *v = spread(*v);
     }
   }
@@ -283,7 +300,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.tiny_at = section(p.tiny.size() * sizeof(int32_t));
   p.sum_items_at = section(p.sums.size() * sizeof(Item));
   p.load_at = section(p.load.size() * sizeof(Item));
-  for (int which = 0; which < kClasses; ++which) {
+  for (int which = 0; which < kKinds; ++which) {
     const Lists &l = p.lists[which];
     p.tiles_at[which][0] = section(l.gram.size() * sizeof(Tile));
     p.tiles_at[which][1] = section(l.square.size() * sizeof(Tile));
@@ -415,13 +432,13 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
   if (h->n_tiny == count) return SLOWMO_OK;
   if (!ok(launch_sums(c, h->sums, h->n_sums, s)) || !ok(launch_load(c, h->load, h->n_load, s))) return refused();
   for (const Op &op : h->program) {
-    for (int which = 0; which < kClasses; ++which) {
+    for (int which = 0; which < kKinds; ++which) {
       const Device &d = h->tiles[which];
-      if (!d.n_update) continue;
       const bool gram = op.symmetric.left < 0;
-      if (!ok(op.update ? launch_update(c, kTileOf[which], op.up, d.update, d.n_update, h->split, s)
-                        : launch_symmetric(c, kTileOf[which], op.symmetric, gram ? d.gram : d.square,
-                                           gram ? d.n_gram : d.n_square, h->split, s)))
+      const int32_t tiles = op.update ? d.n_update : gram ? d.n_gram : d.n_square;
+      if (!tiles) continue;
+      if (!ok(op.update ? launch_update(c, which, op.up, d.update, tiles, h->split, s)
+                        : launch_symmetric(c, which, op.symmetric, gram ? d.gram : d.square, tiles, h->split, s)))
         return refused();
     }
   }
@@ -484,13 +501,13 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     put(p.tiny_at, p.tiny, h->tiny, h->n_tiny);
     put(p.sum_items_at, p.sums, h->sums, h->n_sums);
     put(p.load_at, p.load, h->load, h->n_load);
-    for (int which = 0; which < kClasses; ++which) {
+    for (int which = 0; which < kKinds; ++which) {
       Device &d = h->tiles[which];
       put(p.tiles_at[which][0], p.lists[which].gram, d.gram, d.n_gram);
       put(p.tiles_at[which][1], p.lists[which].square, d.square, d.n_square);
       put(p.tiles_at[which][2], p.lists[which].update, d.update, d.n_update);
-      if (d.n_update && e == hipSuccess) e = prepare_products(kTileOf[which], h->split);
     }
+    if (e == hipSuccess) e = prepare_products(h->split);
     if (p.tickets && e == hipSuccess) e = hipMemsetAsync(base + p.tickets_at, 0, p.tickets * sizeof(uint32_t), s);
     const hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here
     if (e == hipSuccess) e = waited;

@@ -15,6 +15,11 @@ constexpr int kInline = 64;      // matrices whose addresses travel with one lau
 constexpr int kMostSums = 1024;  // workgroups that share a matrix's sum of squares
 constexpr int kSquares = 4;      // n x n buffers of a matrix: A, P, W, Q (A, P where steps go one by one)
 
+// Kinds of tiles: 128 x 128, 256 x 256, and, for P X, 128 rows of 256.
+enum Kind { kSmall = 0, kLarge = 1, kWide = 2, kKinds = 3 };
+constexpr int32_t kRowsOf[kKinds] = {128, 256, 128}, kColsOf[kKinds] = {128, 256, 256};
+constexpr int32_t kSlotsOf[kKinds] = {768, 256, 512};  // workgroups that run at a time
+
 // Matrices that one workgroup takes from load to store.
 constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
 
@@ -108,10 +113,10 @@ hipError_t launch_tiny(const Call &c, const Steps &steps, const int32_t *list, i
 hipError_t launch_addresses(const Call &c, const Few &few, int32_t first, int32_t count, hipStream_t s);
 hipError_t launch_sums(const Call &c, const Item *items, int32_t count, hipStream_t s);
 hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStream_t s);
-hipError_t prepare_products(int tile, bool split);
-hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const Tile *tiles, int32_t count,
+hipError_t prepare_products(bool split);
+hipError_t launch_symmetric(const Call &c, int kind, const Symmetric &p, const Tile *tiles, int32_t count,
                             bool split, hipStream_t s);
-hipError_t launch_update(const Call &c, int tile, const Update &p, const Tile *tiles, int32_t count, bool split,
+hipError_t launch_update(const Call &c, int kind, const Update &p, const Tile *tiles, int32_t count, bool split,
                          hipStream_t s);
 
 }  // namespace orth

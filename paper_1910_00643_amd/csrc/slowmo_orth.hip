@@ -267,7 +267,7 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 
 // ---- products -----------------------------------------------------------------
 //
-// Tiles of T x T by 4 waves of T/2 x T/2.  Steps of 32 of the summed side go from memory straight to a
+// Tiles of B x A by 4 waves of B/2 x A/2, where A runs along the result's rows.  Steps of 32 of the summed side go from memory straight to a
 // ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead of their use.  A wave reads the next 16's factors into
 // registers before it issues the products of this 16, across the barrier of a step too, so that with
 // one wave per SIMD (T = 256: 256 accumulators a lane) the matrix cores go on.
@@ -304,14 +304,14 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
 
 // UPDATE: P X by Update, else a symmetric product by Symmetric.
-template <int T, int STAGES, bool UPDATE, bool SPLIT>
-__global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 3) void k_products(
+template <int A, int B, int STAGES, bool UPDATE, bool SPLIT>
+__global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGES > 3 ? 2 : 3) void k_products(
     Call c, std::conditional_t<UPDATE, Update, Symmetric> st, const Tile *tiles) {
   extern __shared__ half ring[];
-  constexpr int kBlocks = T / 64;            // blocks of 32 x 32 along a side of a wave's share
-  constexpr int kShare = T * kDeep;          // halves of one factor in a stage
-  constexpr int kLoads = kShare * 2 / 1024 / 4;  // loads of a wave per factor and stage
-  constexpr int kWide = T / 2;               // side of a wave's share
+  constexpr int kBlocksA = A / 64, kBlocksB = B / 64;  // blocks of 32 x 32 along the sides of a wave's share
+  constexpr int kShareA = A * kDeep, kStage = (A + B) * kDeep;  // halves of a stage
+  constexpr int kLoadsA = A / 64, kLoadsB = B / 64;    // loads of a wave per stage
+  constexpr int kWideA = A / 2, kWideB = B / 2;        // sides of a wave's share
   const Tile it = tiles[blockIdx.x];
   const Places places(it.np, it.kp, c.buffers);
   half *const arena = c.arena + it.at;
@@ -338,9 +338,9 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
     b_lo = places.buffer_lo(st.left);
   }
   const int64_t panel = static_cast<int64_t>(it.np) * kDeep;
-  const int64_t a_at = UPDATE ? static_cast<int64_t>(it.j) * (T / kDeep) * panel : static_cast<int64_t>(it.j) * T * kDeep;
+  const int64_t a_at = UPDATE ? static_cast<int64_t>(it.j) * (A / kDeep) * panel : static_cast<int64_t>(it.j) * A * kDeep;
   const int64_t a_step = UPDATE ? kDeep * kDeep : panel;
-  const int64_t b_at = static_cast<int64_t>(it.i) * T * kDeep;
+  const int64_t b_at = static_cast<int64_t>(it.i) * B * kDeep;
   const int steps = depth / kDeep;
 
   // bytes of a lane's piece within a load's 1024: 16 rows of 4 pieces
@@ -353,18 +353,19 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
   int segment = SPLIT ? it.first / steps : 2, left = steps;
   const half *a_next, *b_next;
   auto enter = [&](int at) {
-    a_next = arena + (segment == 1 ? a_lo : a_hi) + a_at + wave * kLoads * (UPDATE ? panel / 2 : 512) + at * a_step;
-    b_next = arena + (segment == 0 ? b_lo : b_hi) + b_at + wave * kLoads * 512 + at * panel;
+    a_next = arena + (segment == 1 ? a_lo : a_hi) + a_at + wave * kLoadsA * (UPDATE ? panel / 2 : 512) + at * a_step;
+    b_next = arena + (segment == 0 ? b_lo : b_hi) + b_at + wave * kLoadsB * 512 + at * panel;
     left = steps - at;
   };
   enter(SPLIT ? it.first - segment * steps : it.first);
   auto fetch = [&](int slot) {
-    const u32 to = shared0 + slot * (2 * kShare * 2) + wave * kLoads * 1024;
+    const u32 to = shared0 + slot * (kStage * 2), to_a = to + wave * kLoadsA * 1024,
+              to_b = to + kShareA * 2 + wave * kLoadsB * 1024;
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {  // of X for P X, two loads to a panel's 32 rows
-      to_shared(to + q * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
-      to_shared(to + kShare * 2 + q * 1024, b_off, b_next + q * 512);
-    }
+    for (int q = 0; q < kLoadsA; ++q)  // of X for P X, two loads to a panel's 32 rows
+      to_shared(to_a + q * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
+#pragma unroll
+    for (int q = 0; q < kLoadsB; ++q) to_shared(to_b + q * 1024, b_off, b_next + q * 512);
     a_next += a_step;
     b_next += panel;
     if (SPLIT && --left == 0 && segment < 2) {
@@ -373,43 +374,46 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
     }
   };
 
-  half8 fa[2][kBlocks], fb[2][kBlocks];
+  half8 fa[2][kBlocksA], fb[2][kBlocksB];
   auto read = [&](int slot, int kk, half8 *a, half8 *b) {
-    const half *sa = ring + slot * 2 * kShare, *sb = sa + kShare;
+    const half *sa = ring + slot * kStage, *sb = sa + kShareA;
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x) {
-      const int rb = wb * kWide + x * 32 + low;
-      b[x] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+    for (int y = 0; y < kBlocksB; ++y) {
+      const int rb = wb * kWideB + y * 32 + low;
+      b[y] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+    }
+#pragma unroll
+    for (int x = 0; x < kBlocksA; ++x) {
       if constexpr (UPDATE) {
         const int r = kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const half *from = sa + ((wa * kWide / 32 + x) * kDeep + r) * kDeep + col;
+        const half *from = sa + ((wa * kWideA / 32 + x) * kDeep + r) * kDeep + col;
         typedef __attribute__((address_space(3))) short4v *shared4;
         const short4v lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from));
         const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * kDeep));
         a[x] = __builtin_bit_cast(half8, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
       } else {
-        const int ra = wa * kWide + x * 32 + low;
+        const int ra = wa * kWideA + x * 32 + low;
         a[x] = *reinterpret_cast<const half8 *>(sa + ra * kDeep + (((kk * 2 + high) ^ ((ra >> 2) & 3)) * 8));
       }
     }
   };
 
-  f32x16 acc[kBlocks][kBlocks];
+  f32x16 acc[kBlocksA][kBlocksB];
 #pragma unroll
-  for (int x = 0; x < kBlocks; ++x)
+  for (int x = 0; x < kBlocksA; ++x)
 #pragma unroll
-    for (int y = 0; y < kBlocks; ++y)
+    for (int y = 0; y < kBlocksB; ++y)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
   auto multiply = [&](const half8 *a, const half8 *b) {
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x)
+    for (int x = 0; x < kBlocksA; ++x)
 #pragma unroll
-      for (int y = 0; y < kBlocks; ++y)
+      for (int y = 0; y < kBlocksB; ++y)
         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
   };
 
-  constexpr int kStep = 2 * kLoads;  // loads of a wave in a step
+  constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a step
   for (int s = 0; s < STAGES && s < total; ++s) fetch(s);
   if (total >= STAGES)
     arrive<kStep * (STAGES - 1)>();
@@ -448,15 +452,15 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
   // at a time, at the scope of the whole card); a fence would write all of L2 back, 120 us a launch.
   if (it.pieces > 1) {
     typedef unsigned long long two;
-    constexpr int64_t kTileSums = static_cast<int64_t>(T) * T / 2;
+    constexpr int64_t kTileSums = static_cast<int64_t>(A) * B / 2;
     two *sums = reinterpret_cast<two *>(c.partial) + it.slot * kTileSums + threadIdx.x;
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x)
+    for (int x = 0; x < kBlocksA; ++x)
 #pragma unroll
-      for (int y = 0; y < kBlocks; ++y)
+      for (int y = 0; y < kBlocksB; ++y)
 #pragma unroll
         for (int g = 0; g < 8; ++g)
-          __hip_atomic_store(sums + it.piece * kTileSums + ((x * kBlocks + y) * 8 + g) * 256,
+          __hip_atomic_store(sums + it.piece * kTileSums + ((x * kBlocksB + y) * 8 + g) * 256,
                              __builtin_bit_cast(two, f32x2{acc[x][y][2 * g], acc[x][y][2 * g + 1]}),
                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they have reached memory
@@ -471,9 +475,9 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
     __syncthreads();
     if (flag[0] + 1 != static_cast<u32>(it.pieces)) return;
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x)
+    for (int x = 0; x < kBlocksA; ++x)
 #pragma unroll
-      for (int y = 0; y < kBlocks; ++y) {
+      for (int y = 0; y < kBlocksB; ++y) {
         f32x16 v;
 #pragma unroll
         for (int r = 0; r < 16; ++r) v[r] = 0.f;
@@ -481,7 +485,7 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
 #pragma unroll
           for (int g = 0; g < 8; ++g) {
             const f32x2 w = __builtin_bit_cast(
-                f32x2, __hip_atomic_load(sums + p * kTileSums + ((x * kBlocks + y) * 8 + g) * 256, __ATOMIC_RELAXED,
+                f32x2, __hip_atomic_load(sums + p * kTileSums + ((x * kBlocksB + y) * 8 + g) * 256, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_AGENT));
             v[2 * g] += w[0];
             v[2 * g + 1] += w[1];
@@ -491,17 +495,18 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
   }
   __syncthreads();
 
-  const int ai = it.j * T + wa * kWide, bi = it.i * T + wb * kWide;  // first place along each factor
+  const int ai = it.j * A + wa * kWideA, bi = it.i * B + wb * kWideB;  // first place along each factor
   if constexpr (UPDATE) {
     if (st.last) {
       // The caller's rows: results pass through shared memory, 32 rows of a wave's share at a time.
-      constexpr int kPitch = kWide + 4, kLanes = kWide / 8, kRows = 64 / kLanes;
+      constexpr int kPitch = (kWideA > kWideB ? kWideA : kWideB) + 4;
       float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
-      const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
       const Matrix &m = c.matrices[it.matrix];
       const Addresses at = c.addresses[it.matrix];
       const float scale = m.scale * st.alpha * (1.f / kScaleX);
-      auto leave = [&](int row0, int rows, int col0, int cols) {
+      auto leave = [&](auto wide, int row0, int rows, int col0, int cols) {
+        constexpr int kLanes = decltype(wide)::value / 8, kRows = 64 / kLanes;
+        const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
 #pragma unroll
         for (int r = 0; r < 32; r += kRows) {
           const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8),
@@ -512,24 +517,24 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
       };
       if (m.tall) {  // k x n: rows along factor a
 #pragma unroll
-        for (int x = 0; x < kBlocks; ++x) {
+        for (int x = 0; x < kBlocksA; ++x) {
 #pragma unroll
-          for (int y = 0; y < kBlocks; ++y)
+          for (int y = 0; y < kBlocksB; ++y)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               stage[((r >> 2) * 8 + high * 4 + (r & 3)) * kPitch + y * 32 + low] = acc[x][y][r];
-          leave(ai + x * 32, m.k, bi, m.n);
+          leave(std::integral_constant<int, kWideB>{}, ai + x * 32, m.k, bi, m.n);
         }
       } else {
 #pragma unroll
-        for (int y = 0; y < kBlocks; ++y) {
+        for (int y = 0; y < kBlocksB; ++y) {
 #pragma unroll
-          for (int x = 0; x < kBlocks; ++x)
+          for (int x = 0; x < kBlocksA; ++x)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
               *reinterpret_cast<f32x4 *>(stage + low * kPitch + x * 32 + g * 8 + high * 4) =
                   f32x4{acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-          leave(bi + y * 32, m.n, ai, m.k);
+          leave(std::integral_constant<int, kWideA>{}, bi + y * 32, m.n, ai, m.k);
         }
       }
       return;
@@ -566,13 +571,13 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
   };
   auto four = [&](const half *from, int g) { return *reinterpret_cast<const half4 *>(from + low * kDeep + g * 8 + high * 4); };
 #pragma unroll
-  for (int y = 0; y < kBlocks; ++y) {
+  for (int y = 0; y < kBlocksB; ++y) {
     // What is added to a row of blocks, all of it asked for before any of it is used.
     constexpr int kMore = UPDATE || !SPLIT ? 2 : 4;
-    half4 more[kBlocks][kMore][4];
+    half4 more[kBlocksA][kMore][4];
     asm volatile("" ::: "memory");  // and no earlier: the registers would not hold it
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x) {
+    for (int x = 0; x < kBlocksA; ++x) {
       const int64_t pos = where(bi + y * 32, ai + x * 32);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -595,7 +600,7 @@ __global__ __launch_bounds__(256, T == 256 || STAGES > 5 ? 1 : STAGES > 3 ? 2 : 
       }
     }
 #pragma unroll
-    for (int x = 0; x < kBlocks; ++x) {
+    for (int x = 0; x < kBlocksA; ++x) {
       const int row0 = bi + y * 32, col0 = ai + x * 32;
       const int64_t pos = where(row0, col0);
       half4 hi[4], lo[4];
@@ -744,49 +749,55 @@ hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStrea
 
 namespace {
 
-// Workgroups per CU there is room for: with few of them a deeper ring hides more of memory's latency.
-// Block of the Transformer-big shapes, 216 tiles a launch: 22 us with 3 stages, STAGES9 with 9.
+// The kernel for a kind of tiles.  Of small ones, `count` decides how many workgroups share a CU: few leave
+// shared memory for a deeper ring, which hides more of memory's latency.  Block of the Transformer-big shapes,
+// 216 tiles a launch: 19.4 us with 9 stages, 22.2 with 3.
 template <bool UPDATE, typename F>
-hipError_t with_products(int tile, int32_t count, bool split, F &&f) {
-  auto sized = [&](auto t, auto stages) {
-    constexpr int T = t(), S = stages();
-    constexpr size_t bytes = sizeof(half) * S * 2 * T * kDeep;
-    return split ? f(k_products<T, S, UPDATE, true>, bytes) : f(k_products<T, S, UPDATE, false>, bytes);
+hipError_t with_products(int kind, int32_t count, bool split, F &&f) {
+  auto sized = [&](auto a, auto b, auto stages) {
+    constexpr int A = a(), B = b(), S = stages();
+    constexpr size_t bytes = sizeof(half) * S * (A + B) * kDeep;
+    return split ? f(k_products<A, B, S, UPDATE, true>, bytes) : f(k_products<A, B, S, UPDATE, false>, bytes);
   };
   std::integral_constant<int, 128> small;
-  if (tile == 256) return sized(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
-  if (count <= 256) return sized(small, std::integral_constant<int, 9>{});
-  if (count <= 512) return sized(small, std::integral_constant<int, 5>{});
-  return sized(small, std::integral_constant<int, 3>{});
+  std::integral_constant<int, 256> large;
+  if (kind == kLarge) return sized(large, large, std::integral_constant<int, 4>{});
+  if constexpr (UPDATE)
+    if (kind == kWide) return sized(large, small, std::integral_constant<int, 3>{});
+  if (count <= 256) return sized(small, small, std::integral_constant<int, 9>{});
+  if (count <= 512) return sized(small, small, std::integral_constant<int, 5>{});
+  return sized(small, small, std::integral_constant<int, 3>{});
 }
 
 }  // namespace
 
 // More shared memory than a kernel may have unasked.
-hipError_t prepare_products(int tile, bool split) {
+hipError_t prepare_products(bool split) {
   auto allow = [](auto *k, size_t bytes) {
     return hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize,
                                static_cast<int>(bytes));
   };
-  for (int32_t count : {256, 512, 768}) {
-    hipError_t e = with_products<false>(tile, count, split, allow);
-    if (e == hipSuccess) e = with_products<true>(tile, count, split, allow);
-    if (e != hipSuccess) return e;
+  for (int kind : {kSmall, kLarge, kWide}) {
+    for (int32_t count : {256, 512, 768}) {
+      hipError_t e = with_products<false>(kind, count, split, allow);
+      if (e == hipSuccess) e = with_products<true>(kind, count, split, allow);
+      if (e != hipSuccess) return e;
+    }
   }
   return hipSuccess;
 }
 
-hipError_t launch_symmetric(const Call &c, int tile, const Symmetric &p, const Tile *tiles, int32_t count,
+hipError_t launch_symmetric(const Call &c, int kind, const Symmetric &p, const Tile *tiles, int32_t count,
                             bool split, hipStream_t s) {
-  return with_products<false>(tile, count, split, [&](auto *k, size_t bytes) {
+  return with_products<false>(kind, count, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_update(const Call &c, int tile, const Update &p, const Tile *tiles, int32_t count, bool split,
+hipError_t launch_update(const Call &c, int kind, const Update &p, const Tile *tiles, int32_t count, bool split,
                          hipStream_t s) {
-  return with_products<true>(tile, count, split, [&](auto *k, size_t bytes) {
+  return with_products<true>(kind, count, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
