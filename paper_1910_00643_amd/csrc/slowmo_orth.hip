@@ -268,9 +268,9 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // ---- products -----------------------------------------------------------------
 //
 // Tiles of B x A by 4 waves of B/2 x A/2, where A runs along the result's rows.  Steps of 32 of the summed side go from memory straight to a
-// ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead of their use.  A wave reads the next 16's factors into
-// registers before it issues the products of this 16, across the barrier of a step too, so that with
-// one wave per SIMD (T = 256: 256 accumulators a lane) the matrix cores go on.
+// ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead of their use.  A wave reads the next step's factors into
+// registers before it issues the products of this one, so that the matrix cores go on with one wave per SIMD
+// too (B = 256: 256 accumulators a lane).
 //
 // X and the n x n matrices lie in panels of 32 columns, [column / 32][row][column mod 32]: a step's share of a
 // factor is one piece of memory (P X's X: one per panel) and every cache line of it is used whole.  (Rows
@@ -374,8 +374,8 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     }
   };
 
-  half8 fa[2][kBlocksA], fb[2][kBlocksB];
-  auto read = [&](int slot, int kk, half8 *a, half8 *b) {
+  half8 fa[2][2][kBlocksA], fb[2][2][kBlocksB];  // of this step and of the next, 16 deep each
+  auto read_half = [&](int slot, int kk, half8 *a, half8 *b) {
     const half *sa = ring + slot * kStage, *sb = sa + kShareA;
 #pragma unroll
     for (int y = 0; y < kBlocksB; ++y) {
@@ -398,6 +398,11 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     }
   };
 
+  auto read = [&](int slot, int which) {
+    read_half(slot, 0, fa[which][0], fb[which][0]);
+    read_half(slot, 1, fa[which][1], fb[which][1]);
+  };
+
   f32x16 acc[kBlocksA][kBlocksB];
 #pragma unroll
   for (int x = 0; x < kBlocksA; ++x)
@@ -405,12 +410,14 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     for (int y = 0; y < kBlocksB; ++y)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
-  auto multiply = [&](const half8 *a, const half8 *b) {
+  auto multiply = [&](int which) {
 #pragma unroll
-    for (int x = 0; x < kBlocksA; ++x)
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int y = 0; y < kBlocksB; ++y)
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[x], b[y], acc[x][y], 0, 0, 0);
+      for (int x = 0; x < kBlocksA; ++x)
+#pragma unroll
+        for (int y = 0; y < kBlocksB; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[which][kk][x], fb[which][kk][y], acc[x][y], 0, 0, 0);
   };
 
   constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a step
@@ -419,33 +426,38 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     arrive<kStep * (STAGES - 1)>();
   else
     arrive<0>();
-  read(0, 0, fa[0], fb[0]);
-  int s = 0, slot = 0;
-  auto after = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
-  for (; s + STAGES < total; ++s) {
-    read(slot, 1, fa[1], fb[1]);
-    multiply(fa[0], fb[0]);
-    arrive<kStep * (STAGES - 2)>();
-    fetch(slot);  // where step s was: everybody has read it
-    slot = after(slot);
-    read(slot, 0, fa[0], fb[0]);
-    multiply(fa[1], fb[1]);
-  }
-  // nothing is left to fetch; what is on its way arrives one step after the other
-  auto drain = [&](auto pending) {
-    if (total - s != decltype(pending)::value / kStep + 2) return;
-    read(slot, 1, fa[1], fb[1]);
-    multiply(fa[0], fb[0]);
+  int left_steps = total, slot = 0;  // the factors of a step with r left are in registers r mod 2
+  if (total & 1)
+    read(0, 1);
+  else
+    read(0, 0);
+  // One step: the next one's factors go to registers while this one's are multiplied.  `pending` loads may
+  // still be on their way when the next step's have arrived.
+  auto step = [&](auto odd, auto pending, auto more) {
+    constexpr int kThis = decltype(odd)::value;
     arrive<decltype(pending)::value>();
-    slot = after(slot);
-    read(slot, 0, fa[0], fb[0]);
-    multiply(fa[1], fb[1]);
-    ++s;
+    if constexpr (decltype(more)::value) fetch(slot);  // where this step was: everybody has read it
+    slot = slot + 1 == STAGES ? 0 : slot + 1;
+    read(slot, 1 - kThis);
+    multiply(kThis);
+    --left_steps;
   };
-  each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) { drain(std::integral_constant<int, kStep * (STAGES - 2 - n())>{}); });
-  read(slot, 1, fa[1], fb[1]);
-  multiply(fa[0], fb[0]);
-  multiply(fa[1], fb[1]);
+  std::integral_constant<int, 0> even;
+  std::integral_constant<int, 1> odd;
+  std::integral_constant<int, kStep * (STAGES - 2)> full;
+  if (left_steps > STAGES && (left_steps & 1)) step(odd, full, std::true_type{});
+  while (left_steps - 1 > STAGES) {
+    step(even, full, std::true_type{});
+    step(odd, full, std::true_type{});
+  }
+  if (left_steps > STAGES) step(even, full, std::true_type{});
+  // nothing is left to fetch; what is on its way arrives one step after the other
+  each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) {
+    constexpr int kLeft = STAGES - decltype(n)::value;
+    if (left_steps == kLeft)
+      step(std::integral_constant<int, (kLeft & 1)>{}, std::integral_constant<int, kStep * (kLeft - 2)>{}, std::false_type{});
+  });
+  multiply(1);
 
   // A tile in several shares: each leaves its sums in memory, and the one that comes last adds them all
   // up, in their order whichever it is.  The sums pass the dies' separate L2 caches by themselves (8 bytes
