@@ -358,14 +358,15 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     left = steps - at;
   };
   enter(SPLIT ? it.first - segment * steps : it.first);
-  auto fetch = [&](int slot) {
-    const u32 to = shared0 + slot * (kStage * 2), to_a = to + wave * kLoadsA * 1024,
-              to_b = to + kShareA * 2 + wave * kLoadsB * 1024;
-#pragma unroll
-    for (int q = 0; q < kLoadsA; ++q)  // of X for P X, two loads to a panel's 32 rows
-      to_shared(to_a + q * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
-#pragma unroll
-    for (int q = 0; q < kLoadsB; ++q) to_shared(to_b + q * 1024, b_off, b_next + q * 512);
+  constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a step
+  auto fetch_one = [&](int slot, int q) {
+    const u32 to = shared0 + slot * (kStage * 2);
+    if (q < kLoadsA)  // of X for P X, two loads to a panel's 32 rows
+      to_shared(to + (wave * kLoadsA + q) * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
+    else
+      to_shared(to + kShareA * 2 + (wave * kLoadsB + q - kLoadsA) * 1024, b_off, b_next + (q - kLoadsA) * 512);
+  };
+  auto fetched = [&] {
     a_next += a_step;
     b_next += panel;
     if (SPLIT && --left == 0 && segment < 2) {
@@ -375,32 +376,27 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
   };
 
   half8 fa[2][2][kBlocksA], fb[2][2][kBlocksB];  // of this step and of the next, 16 deep each
-  auto read_half = [&](int slot, int kk, half8 *a, half8 *b) {
+  constexpr int kReads = 2 * (kBlocksA + kBlocksB);
+  auto read_one = [&](int slot, int which, int q) {
+    const int kk = q / (kBlocksA + kBlocksB), f = q % (kBlocksA + kBlocksB);
     const half *sa = ring + slot * kStage, *sb = sa + kShareA;
-#pragma unroll
-    for (int y = 0; y < kBlocksB; ++y) {
-      const int rb = wb * kWideB + y * 32 + low;
-      b[y] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+    if (f < kBlocksB) {
+      const int rb = wb * kWideB + f * 32 + low;
+      fb[which][kk][f] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+      return;
     }
-#pragma unroll
-    for (int x = 0; x < kBlocksA; ++x) {
-      if constexpr (UPDATE) {
-        const int r = kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-        const half *from = sa + ((wa * kWideA / 32 + x) * kDeep + r) * kDeep + col;
-        typedef __attribute__((address_space(3))) short4v *shared4;
-        const short4v lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from));
-        const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * kDeep));
-        a[x] = __builtin_bit_cast(half8, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
-      } else {
-        const int ra = wa * kWideA + x * 32 + low;
-        a[x] = *reinterpret_cast<const half8 *>(sa + ra * kDeep + (((kk * 2 + high) ^ ((ra >> 2) & 3)) * 8));
-      }
+    const int x = f - kBlocksB;
+    if constexpr (UPDATE) {
+      const int r = kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+      const half *from = sa + ((wa * kWideA / 32 + x) * kDeep + r) * kDeep + col;
+      typedef __attribute__((address_space(3))) short4v *shared4;
+      const short4v lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from));
+      const short4v hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + 4 * kDeep));
+      fa[which][kk][x] = __builtin_bit_cast(half8, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int ra = wa * kWideA + x * 32 + low;
+      fa[which][kk][x] = *reinterpret_cast<const half8 *>(sa + ra * kDeep + (((kk * 2 + high) ^ ((ra >> 2) & 3)) * 8));
     }
-  };
-
-  auto read = [&](int slot, int which) {
-    read_half(slot, 0, fa[which][0], fb[which][0]);
-    read_half(slot, 1, fa[which][1], fb[which][1]);
   };
 
   f32x16 acc[kBlocksA][kBlocksB];
@@ -410,36 +406,50 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     for (int y = 0; y < kBlocksB; ++y)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
-  auto multiply = [&](int which) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int x = 0; x < kBlocksA; ++x)
-#pragma unroll
-        for (int y = 0; y < kBlocksB; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[which][kk][x], fb[which][kk][y], acc[x][y], 0, 0, 0);
+  constexpr int kProducts = 2 * kBlocksA * kBlocksB;
+  auto multiply_one = [&](int which, int q) {
+    const int kk = q / (kBlocksA * kBlocksB), x = q / kBlocksB % kBlocksA, y = q % kBlocksB;
+    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[which][kk][x], fb[which][kk][y], acc[x][y], 0, 0, 0);
   };
 
-  constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a step
-  for (int s = 0; s < STAGES && s < total; ++s) fetch(s);
+  for (int s = 0; s < STAGES && s < total; ++s) {
+#pragma unroll
+    for (int q = 0; q < kStep; ++q) fetch_one(s, q);
+    fetched();
+  }
   if (total >= STAGES)
     arrive<kStep * (STAGES - 1)>();
   else
     arrive<0>();
   int left_steps = total, slot = 0;  // the factors of a step with r left are in registers r mod 2
-  if (total & 1)
-    read(0, 1);
-  else
-    read(0, 0);
+#pragma unroll
+  for (int q = 0; q < kReads; ++q) {
+    if (total & 1)
+      read_one(0, 1, q);
+    else
+      read_one(0, 0, q);
+  }
   // One step: the next one's factors go to registers while this one's are multiplied.  `pending` loads may
-  // still be on their way when the next step's have arrived.
+  // still be on their way when the next step's have arrived.  Reads and loads are issued one by one between
+  // products: a wave issues in order, and in a row they hold it up for as long as the products take.
   auto step = [&](auto odd, auto pending, auto more) {
     constexpr int kThis = decltype(odd)::value;
-    arrive<decltype(pending)::value>();
-    if constexpr (decltype(more)::value) fetch(slot);  // where this step was: everybody has read it
+    const int here = slot;
     slot = slot + 1 == STAGES ? 0 : slot + 1;
-    read(slot, 1 - kThis);
-    multiply(kThis);
+    __builtin_amdgcn_sched_barrier(0);  // the products before run on while this wave waits
+    arrive<decltype(pending)::value>();
+    each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+      constexpr int I = decltype(i)::value;
+#pragma unroll
+      for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q) read_one(slot, 1 - kThis, q);
+      if constexpr (decltype(more)::value) {  // to where this step was: everybody has read it
+#pragma unroll
+        for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, q);
+      }
+      multiply_one(kThis, I);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (decltype(more)::value) fetched();
     --left_steps;
   };
   std::integral_constant<int, 0> even;
@@ -457,7 +467,7 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     if (left_steps == kLeft)
       step(std::integral_constant<int, (kLeft & 1)>{}, std::integral_constant<int, kStep * (kLeft - 2)>{}, std::false_type{});
   });
-  multiply(1);
+  each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) { multiply_one(1, decltype(i)::value); });
 
   // A tile in several shares: each leaves its sums in memory, and the one that comes last adds them all
   // up, in their order whichever it is.  The sums pass the dies' separate L2 caches by themselves (8 bytes
