@@ -100,17 +100,29 @@ void walk(int32_t down, int32_t across, F &&f) {
       for (int32_t a = a0; a < std::min(down, a0 + 8); ++a) f(a, b);
 }
 
-// Workgroups go to the 8 dies in turn, each with an L2 of its own: of every 256, each die gets 32
-// neighbours of the list.  (96, all that a die runs at once, gave one die the list's longest sums:
-// 1.10-1.15 of a call's time on ResNet lists.)
+// Workgroups go to the 8 dies in turn, each with an L2 of its own.  The list in bundles -- a matrix's tiles,
+// or 32 neighbours of a large one's -- goes to the dies whole, each to the one with the fewest steps so far, so
+// that a factor is fetched into one L2 and no die gets all of the longest sums.
 std::vector<Tile> spread(const std::vector<Tile> &v) {
-  std::vector<Tile> out(v.size());
-  for (size_t base = 0; base < v.size(); base += 256) {
-    const size_t count = std::min<size_t>(256, v.size() - base), each = count / 8, more = count % 8;
-    for (size_t b = 0; b < count; ++b) {
-      const size_t die = b % 8;
-      out[base + b] = v[base + die * each + std::min(die, more) + b / 8];
+  int64_t steps[8] = {};
+  std::vector<Tile> queue[8], out;
+  for (size_t at = 0; at < v.size();) {
+    size_t end = at;
+    while (end < v.size() && v[end].matrix == v[at].matrix && v[end].pieces == v[at].pieces) ++end;
+    if (end - at > 32 && (end - at) * 16 > v.size()) end = at + 32;
+    const auto die = std::min_element(steps, steps + 8) - steps;
+    for (; at < end; ++at) {
+      queue[die].push_back(v[at]);
+      steps[die] += v[at].count;
     }
+  }
+  size_t next[8] = {};
+  while (out.size() < v.size()) {
+    size_t die = out.size() % 8;
+    if (next[die] == queue[die].size())  // it has run out: the one with the most left gives
+      for (size_t d = 0; d < 8; ++d)
+        if (queue[d].size() - next[d] > queue[die].size() - next[die]) die = d;
+    out.push_back(queue[die][next[die]++]);
   }
   return out;
 }
