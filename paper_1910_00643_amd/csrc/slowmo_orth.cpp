@@ -37,7 +37,7 @@ struct Device {
 }  // namespace
 
 struct slowmo_orth {
-  bool split = false;
+  bool split = false, small = false;
   Steps steps{};
   std::vector<Op> program;
   std::vector<int32_t> index;       // places in the caller's list of the matrices that are not empty
@@ -59,6 +59,7 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // Everything a handle needs, laid out from the configuration and the shapes alone.
 struct Plan {
   bool pairs = false;
+  bool small = false;         // every matrix goes by one workgroup from load to store
   std::vector<Matrix> matrices;
   std::vector<int32_t> index, tiny;
   std::vector<Item> sums, load;
@@ -219,6 +220,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     const int32_t at = static_cast<int32_t>(p.matrices.size());
     if (m.n <= kTinySide && static_cast<int64_t>(m.n) * m.k <= kTinyElements) {
       p.tiny.push_back(at);
+      m.tiny = 1;
     } else {
       const int which = large_tiles(m);
       of[which].push_back(at);
@@ -231,8 +233,14 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     p.matrices.push_back(m);
     p.index.push_back(i);
   }
+  // Small matrices alone (beside tiny ones): one workgroup each.
+  int32_t side = split ? kSmallSideSplit : kSmallSide, small = 0;
+  for (const Matrix &m : p.matrices) small += m.n <= side && m.k <= kSmallLength;
+  p.small = p.tiny.size() < p.matrices.size() && small == static_cast<int32_t>(p.matrices.size());
+  if (p.small)
+    for (auto &list : of) list.clear();
   // Two steps at a time, on n x n matrices: see program().
-  p.pairs = c.steps >= 3 && by_pairs < 0.93 * one_by_one;
+  p.pairs = !p.small && c.steps >= 3 && by_pairs < 0.93 * one_by_one;
 
   int64_t halves = 0;
   auto take = [&](int64_t count) {
@@ -282,7 +290,8 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
       walk(m.np / side, m.kp / kColsOf[kind], [&](int32_t i, int32_t j) { put(p.lists[kind].update, at, i, j, m.np); });
     }
   }
-  if (p.lists[kWide].update.size() < 512) {  // too few to fill the card: as small ones
+  // Too few to fill the card, or beside small ones, whose launch would come on top: as small ones.
+  if (p.lists[kWide].update.size() < (p.lists[kSmall].update.empty() ? 512u : 2048u)) {
     for (const Tile &t : p.lists[kWide].update)
       for (int32_t half : {0, 1}) {
         Tile s = t;
@@ -344,8 +353,8 @@ float power(double most) {
 // written half as often, and of the products with X two of three per pair are left: 3 n n k + 5 n n n
 // for 6 n n k + 2 n n n.  (All n x n factors are polynomials of the same A, so that each product of
 // two is symmetric again.)  The last step is never one of a pair: rounding would show.
-// Returns an empty program if the coefficients let X outgrow a half.
-std::vector<Op> program(const Steps &steps, bool pairs, bool split) {
+// Leaves the powers of two with the steps.  Returns an empty program if the coefficients let X outgrow a half.
+std::vector<Op> program(Steps &steps, bool pairs, bool split) {
   std::vector<Op> ops;
   enum { kA, kP, kW, kQ };
   auto symmetric = [&](Symmetric s) {
@@ -365,6 +374,9 @@ std::vector<Op> program(const Steps &steps, bool pairs, bool split) {
     const double keep0 = carry ? 0. : a0;
     const float sa = power(largest(most, [&](double s) { return s * s; }));
     const float sp = power(largest(most, [&](double s) { return p0(s) + (two ? 0. : keep0); }));
+    steps.a_power[t] = sa;
+    steps.p_power[t] = sp;
+    steps.carry[t] = carry;
     symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f});
     symmetric({from, kA, kA, kA, -1, kP, static_cast<float>(c0 * sp / (double(sa) * sa)),
                static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp)});
@@ -432,16 +444,17 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
   auto ok = [&](hipError_t got) { return (e = got) == hipSuccess; };
   auto refused = [&] { return fail_thread_hip(e, "slowmo_orthogonalize (results may be partly written)"); };
   for (int32_t first = 0; first < count; first += kInline) {
-    Few few{};
+    Few few{};  // travels with the launch
     const int32_t some = std::min(kInline, count - first);
     for (int32_t i = 0; i < some; ++i) {
       const int32_t at = h->index[first + i];
       few.at[i] = {in[at], with_momentum ? momentum[at] : nullptr, out[at]};
     }
-    if (!ok(launch_addresses(c, few, first, some, s))) return refused();
+    if (h->small && !ok(launch_small(c, h->steps, few, first, some, h->split, s))) return refused();
+    if ((!h->small || h->n_tiny) && !ok(launch_addresses(c, few, first, some, s))) return refused();
   }
   if (h->n_tiny && !ok(launch_tiny(c, h->steps, h->tiny, h->n_tiny, s))) return refused();
-  if (h->n_tiny == count) return SLOWMO_OK;
+  if (h->small || h->n_tiny == count) return SLOWMO_OK;
   if (!ok(launch_sums(c, h->sums, h->n_sums, s)) || !ok(launch_load(c, h->load, h->n_load, s))) return refused();
   for (const Op &op : h->program) {
     for (int which = 0; which < kKinds; ++which) {
@@ -465,7 +478,8 @@ extern "C" {
 static const char *refusal(const slowmo_orth_config *cfg, int32_t n_matrices, const int64_t *rows,
                            const int64_t *cols, const int64_t *ld) {
   if (const char *bad = check(cfg, n_matrices, rows, cols, ld)) return bad;
-  if (program(steps_of(*cfg), false, false).empty()) return "the coefficients let singular values grow past 7";
+  Steps steps = steps_of(*cfg);
+  if (program(steps, false, false).empty()) return "the coefficients let singular values grow past 7";
   return nullptr;
 }
 
@@ -497,6 +511,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     std::unique_ptr<slowmo_orth> h(new slowmo_orth);
     h->split = cfg->out_dtype == SLOWMO_F32;
     h->steps = steps_of(*cfg);
+    h->small = p.small;
     h->program = program(h->steps, p.pairs, h->split);
     h->index = p.index;
     char *base = static_cast<char *>(workspace);
@@ -519,7 +534,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
       put(p.tiles_at[which][1], p.lists[which].square, d.square, d.n_square);
       put(p.tiles_at[which][2], p.lists[which].update, d.update, d.n_update);
     }
-    if (e == hipSuccess) e = prepare_products(h->split);
+    if (e == hipSuccess) e = h->small ? prepare_small() : prepare_products(h->split);
     if (p.tickets && e == hipSuccess) e = hipMemsetAsync(base + p.tickets_at, 0, p.tickets * sizeof(uint32_t), s);
     const hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here
     if (e == hipSuccess) e = waited;

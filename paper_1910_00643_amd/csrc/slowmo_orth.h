@@ -27,6 +27,10 @@ constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
 // coefficients), and what of them is subnormal as a half is below 2^-27.
 constexpr float kScaleX = 8192.f;
 
+// A list of small matrices alone goes by one workgroup each too: n up to 128 and k up to 256 for products
+// of halves, n up to 64 for those of pairs of halves (X, A and P fill shared memory).
+constexpr int kSmallSide = 128, kSmallSideSplit = 64, kSmallLength = 256;
+
 // One matrix.  n <= k; X is n x k; np, kp: sides padded to whole tiles.  X and the n x n buffers lie in
 // panels of kDeep columns, [column / kDeep][row][column mod kDeep].  From `at` on (halves from the start
 // of the arena): X, the X it is replaced by, X's lower halves (the values' next 11 bits), the n x n buffers;
@@ -34,7 +38,7 @@ constexpr float kScaleX = 8192.f;
 struct Matrix {
   int64_t at, ld;
   int32_t n, k, np, kp;
-  int32_t tall;                          // the caller's matrix is k x n
+  int32_t tall, tiny;                    // the caller's matrix is k x n; it is k_tiny's
   float scale;
   int32_t first_sum, sums;               // its partial sums of squares
 };
@@ -106,10 +110,16 @@ struct Update {
 
 struct Steps {
   float abc[16][3];
+  float a_power[16], p_power[16];  // the powers of two that A and P are held times in step by step products
+  int32_t carry[16];
   int32_t count;
 };
 
 hipError_t launch_tiny(const Call &c, const Steps &steps, const int32_t *list, int32_t count, hipStream_t s);
+// Matrices first..first + count - 1, all of them small or tiny (which are left out).
+hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, bool split,
+                        hipStream_t s);
+hipError_t prepare_small();
 hipError_t launch_addresses(const Call &c, const Few &few, int32_t first, int32_t count, hipStream_t s);
 hipError_t launch_sums(const Call &c, const Item *items, int32_t count, hipStream_t s);
 hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStream_t s);

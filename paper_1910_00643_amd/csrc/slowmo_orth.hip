@@ -747,10 +747,257 @@ __global__ __launch_bounds__(kTinyThreads) void k_tiny(Call c, Steps steps, cons
   }
 }
 
+// A small matrix from its load to its store: one workgroup, all steps, X, A and P as halves in shared
+// memory, in panels of 32 columns as the products' factors lie there.  A call is one launch instead of 17:
+// launches, each with its way to memory and back, are all that such a call takes.  N: 128, or 64 for pairs of
+// halves, and the side of the tiles of X that are replaced one after the other; 4 waves have a quarter of
+// a tile each.
+template <int N, bool SPLIT>
+__global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, int32_t first) {
+  extern __shared__ half memory[];
+  constexpr int kBlocks = N / 64, kParts = SPLIT ? 2 : 1, kMostTiles = kSmallLength / N;
+  constexpr int kXs = N * kSmallLength, kAs = N * N;
+  half *const x[2] = {memory, memory + kXs};  // hi, lo (lo: while loading only, unless SPLIT)
+  half *const gram[2] = {memory + kParts * kXs, memory + kParts * kXs + kAs};
+  half *const poly[2] = {gram[0] + kParts * kAs, gram[0] + kParts * kAs + kAs};
+  __shared__ double shared[4];
+  const Matrix &m = c.matrices[first + blockIdx.x];
+  if (m.tiny) return;
+  const Addresses at = few.at[blockIdx.x];
+  const int n = m.n, k = m.k, tiles = (k + N - 1) / N, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wa = wave & 1, wb = wave >> 1;
+  const int low = lane & 31, high = lane >> 5;
+  // where column `col`, of a multiple of 4, of row `row` is
+  auto place = [&](int row, int col) {
+    return ((col >> 5) * N + row) * kDeep + ((((col >> 3) & 3) ^ ((row >> 2) & 3)) * 8) + (col & 7);
+  };
+
+  const int rows = m.tall ? k : n, cols = m.tall ? n : k;
+  double squares = 0.;
+  auto walk = [&](auto *in, auto &&f) {
+    const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
+    const int pieces = (cols + 7) / 8;
+    for (int q = tid; q < rows * pieces; q += 256) {
+      const int row = q / pieces, col = (q - row * pieces) * 8;
+      const int64_t e = row * m.ld + col;
+      float u[8], h[8];
+      row8(in + e, cols - col, wide, u);
+      if (c.momentum) row8(at.momentum + e, cols - col, wide_m, h);
+      f(row, col, e, u, h);
+    }
+  };
+  auto first_look = [&](int, int col, int64_t e, float *u, float *h) {
+    if (c.momentum) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        h[i] = fmaf(c.mu, h[i], u[i]);
+        if (col + i < cols) at.momentum[e + i] = h[i];
+        u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) squares = fma(static_cast<double>(u[i]), static_cast<double>(u[i]), squares);
+  };
+  // zeros where the padding is
+  for (int q = tid; q < N * tiles * N / 8; q += 256) {
+    const half8 none = {};
+    *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
+    *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
+  }
+  if (c.in_bf16)
+    walk(static_cast<const uint16_t *>(at.in), first_look);
+  else
+    walk(static_cast<const float *>(at.in), first_look);
+  const float inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
+  auto second_look = [&](int row, int col, int64_t, float *u, float *h) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (c.momentum) u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
+      if (col + i >= cols) continue;
+      const int to = m.tall ? place(col + i, row & ~3) + (row & 3) : place(row, (col + i) & ~3) + ((col + i) & 3);
+      split_half(u[i] * inverse * kScaleX, x[0][to], x[1][to]);
+    }
+  };
+  if (c.in_bf16)
+    walk(static_cast<const uint16_t *>(at.in), second_look);
+  else
+    walk(static_cast<const float *>(at.in), second_look);
+  __syncthreads();
+
+  // this wave's quarter of tile t: rows wb * N / 2 + y * 32 + low, columns t * N + wa * N / 2 + x * 32 + g * 8 + high * 4
+  half4 lower[kMostTiles][kBlocks][kBlocks][4];
+  auto mine = [&](int t, int xb, int yb, int g) {
+    return place(wb * (N / 2) + yb * 32 + low, t * N + wa * (N / 2) + xb * 32 + g * 8 + high * 4);
+  };
+  if constexpr (!SPLIT) {
+#pragma unroll
+    for (int t = 0; t < kMostTiles; ++t)
+#pragma unroll
+      for (int q = 0; q < kBlocks * kBlocks * 4; ++q)
+        if (t < tiles)
+          lower[t][q / (4 * kBlocks)][q / 4 % kBlocks][q % 4] =
+              *reinterpret_cast<const half4 *>(x[1] + mine(t, q / (4 * kBlocks), q / 4 % kBlocks, q % 4));
+    __syncthreads();  // what lay there makes room for A and P
+  }
+
+  f32x16 acc[kBlocks][kBlocks];
+  auto along = [&](const half *from, int row0, int panel, int kk) {
+    const int r = row0 + low;
+    return *reinterpret_cast<const half8 *>(from + (panel * N + r) * kDeep + (((kk * 2 + high) ^ ((r >> 2) & 3)) * 8));
+  };
+  auto down = [&](const half *from, int panel_row, int panel, int kk) {  // columns of `panel`, rows panel_row * 32 and on
+    typedef __attribute__((address_space(3))) short4v *shared4;
+    const int r = panel_row * 32 + kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+    const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + place(r, panel * 32 + col)));
+    const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + place(r + 4, panel * 32 + col)));
+    return __builtin_bit_cast(half8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // acc = sum over `depth` of a and b, small products of pairs first
+  auto product = [&](int depth, auto &&a, auto &&b) {
+#pragma unroll
+    for (int xb = 0; xb < kBlocks; ++xb)
+#pragma unroll
+      for (int yb = 0; yb < kBlocks; ++yb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[xb][yb][r] = 0.f;
+#pragma unroll
+    for (int pass = SPLIT ? 0 : 2; pass < 3; ++pass)
+      for (int s = 0; s < depth / kDeep; ++s)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          half8 fa[kBlocks], fb[kBlocks];
+#pragma unroll
+          for (int q = 0; q < kBlocks; ++q) {
+            fa[q] = a(pass == 1, q, s, kk);
+            fb[q] = b(pass == 0, q, s, kk);
+          }
+#pragma unroll
+          for (int xb = 0; xb < kBlocks; ++xb)
+#pragma unroll
+            for (int yb = 0; yb < kBlocks; ++yb)
+              acc[xb][yb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[xb], fb[yb], acc[xb][yb], 0, 0, 0);
+        }
+  };
+  auto each_four = [&](auto &&f) {
+#pragma unroll
+    for (int xb = 0; xb < kBlocks; ++xb)
+#pragma unroll
+      for (int yb = 0; yb < kBlocks; ++yb)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) f(xb, yb, g);
+  };
+  auto keep = [&](half *const to[2], int pos, const float *v) {
+    half4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      half h, l;
+      split_half(v[e], h, l);
+      hi[e] = h;
+      lo[e] = l;
+    }
+    *reinterpret_cast<half4 *>(to[0] + pos) = hi;
+    if (SPLIT) *reinterpret_cast<half4 *>(to[1] + pos) = lo;
+    return lo;
+  };
+
+  for (int s = 0; s < steps.count; ++s) {
+    const float sa = steps.a_power[s], sp = steps.p_power[s], a0 = steps.abc[s][0];
+    const bool carry = !SPLIT && steps.carry[s], last = s + 1 == steps.count;
+    product(tiles * N, [&](bool lo, int q, int d, int kk) { return along(x[lo], wa * (N / 2) + q * 32, d, kk); },
+            [&](bool lo, int q, int d, int kk) { return along(x[lo], wb * (N / 2) + q * 32, d, kk); });
+    each_four([&](int xb, int yb, int g) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (sa / (kScaleX * kScaleX));
+      keep(gram, mine(0, xb, yb, g), v);
+    });
+    __syncthreads();
+    product(N, [&](bool lo, int q, int d, int kk) { return along(gram[lo], wa * (N / 2) + q * 32, d, kk); },
+            [&](bool lo, int q, int d, int kk) { return along(gram[lo], wb * (N / 2) + q * 32, d, kk); });
+    each_four([&](int xb, int yb, int g) {
+      const int pos = mine(0, xb, yb, g);
+      const half4 h = *reinterpret_cast<const half4 *>(gram[0] + pos);
+      half4 l;
+      if (SPLIT) l = *reinterpret_cast<const half4 *>(gram[1] + pos);
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float value = static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f);
+        v[e] = fmaf(steps.abc[s][1] * (sp / sa), value, acc[xb][yb][4 * g + e] * (steps.abc[s][2] * (sp / (sa * sa))));
+        if (!carry && wb * (N / 2) + yb * 32 + low == wa * (N / 2) + xb * 32 + g * 8 + high * 4 + e) v[e] += a0 * sp;
+      }
+      keep(poly, pos, v);
+    });
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kMostTiles; ++t) {
+      if (t >= tiles) break;
+      product(N, [&](bool lo, int q, int d, int kk) { return down(x[lo], d, (t * N + wa * (N / 2)) / 32 + q, kk); },
+              [&](bool lo, int q, int d, int kk) { return along(poly[lo], wb * (N / 2) + q * 32, d, kk); });
+      if (!last) __syncthreads();  // everybody has read this tile of X
+      each_four([&](int xb, int yb, int g) {
+        const int pos = mine(t, xb, yb, g);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (1.f / sp);
+        if (carry) {
+          const half4 h = *reinterpret_cast<const half4 *>(x[0] + pos);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = fmaf(a0, static_cast<float>(h[e]) + static_cast<float>(lower[t][xb][yb][g][e]), v[e]);
+        }
+        if (!last) {
+          lower[t][xb][yb][g] = keep(x, pos, v);
+          return;
+        }
+        const int row = wb * (N / 2) + yb * 32 + low, col = t * N + wa * (N / 2) + xb * 32 + g * 8 + high * 4;
+        if (row >= n) return;
+        const float scale = m.scale * (1.f / kScaleX);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (col + e >= k) continue;
+          const int64_t to = m.tall ? (col + e) * m.ld + row : row * m.ld + col + e;
+          if (c.out_bf16)
+            static_cast<uint16_t *>(at.out)[to] = narrow_bf16(v[e] * scale);
+          else
+            static_cast<float *>(at.out)[to] = v[e] * scale;
+        }
+      });
+    }
+    __syncthreads();
+  }
+}
+
+template <int N, bool SPLIT>
+constexpr size_t small_bytes() {  // while loading, X's lower halves lie where A and P come to be
+  const size_t parts = SPLIT ? 2 : 1;
+  return sizeof(half) * (parts * N * kSmallLength + (SPLIT || 2 * N > kSmallLength ? 2 * parts * N * N : N * kSmallLength));
+}
+static_assert(small_bytes<128, false>() <= 160 * 1024 - 64 && small_bytes<64, true>() <= 160 * 1024 - 64, "shared memory");
+static_assert(2 * kSmallSide * kSmallSide >= kSmallSide * kSmallLength, "X's lower halves fit where A and P lie");
+
 }  // namespace
 
 hipError_t launch_tiny(const Call &c, const Steps &steps, const int32_t *list, int32_t count, hipStream_t s) {
   k_tiny<<<count, kTinyThreads, 0, s>>>(c, steps, list);
+  return hipGetLastError();
+}
+
+hipError_t prepare_small() {
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_small<kSmallSide, false>),
+                                     hipFuncAttributeMaxDynamicSharedMemorySize, small_bytes<kSmallSide, false>());
+  if (e == hipSuccess)
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_small<kSmallSideSplit, true>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, small_bytes<kSmallSideSplit, true>());
+  return e;
+}
+
+hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, bool split,
+                        hipStream_t s) {
+  if (split)
+    k_small<kSmallSideSplit, true><<<count, 256, small_bytes<kSmallSideSplit, true>(), s>>>(c, steps, few, first);
+  else
+    k_small<kSmallSide, false><<<count, 256, small_bytes<kSmallSide, false>(), s>>>(c, steps, few, first);
   return hipGetLastError();
 }
 
