@@ -529,7 +529,7 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
       auto leave = [&](auto wide, int row0, int rows, int col0, int cols) {
         constexpr int kLanes = decltype(wide)::value / 8, kRows = 64 / kLanes;
         const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
-#pragma unroll
+#pragma unroll 1  // code that runs once comes slowly: short is fast
         for (int r = 0; r < 32; r += kRows) {
           const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8),
                       q = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8 + 4);
@@ -757,7 +757,7 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   extern __shared__ half memory[];
   constexpr int kBlocks = N / 64, kParts = SPLIT ? 2 : 1, kMostTiles = kSmallLength / N;
   constexpr int kXs = N * kSmallLength, kAs = N * N;
-  half *const x[2] = {memory, memory + kXs};  // hi, lo (lo: while loading only, unless SPLIT)
+  half *const x[2] = {memory, memory + kXs};  // hi, lo (lo: only at both ends, unless SPLIT)
   half *const gram[2] = {memory + kParts * kXs, memory + kParts * kXs + kAs};
   half *const poly[2] = {gram[0] + kParts * kAs, gram[0] + kParts * kAs + kAs};
   __shared__ double shared[4];
@@ -773,55 +773,59 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   };
 
   const int rows = m.tall ? k : n, cols = m.tall ? n : k;
+  // Twice over U, 8 neighbours of a row at a time.  Code that runs once comes slowly from memory, so that
+  // loops here are kept short rather than unrolled.
+  const int pieces = (cols + 7) / 8, units = rows * pieces;
   double squares = 0.;
-  auto walk = [&](auto *in, auto &&f) {
+  float inverse = 0.f;
+  auto walk = [&](auto *in) {
     const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
-    const int pieces = (cols + 7) / 8;
-    for (int q = tid; q < rows * pieces; q += 256) {
-      const int row = q / pieces, col = (q - row * pieces) * 8;
-      const int64_t e = row * m.ld + col;
-      float u[8], h[8];
-      row8(in + e, cols - col, wide, u);
-      if (c.momentum) row8(at.momentum + e, cols - col, wide_m, h);
-      f(row, col, e, u, h);
-    }
-  };
-  auto first_look = [&](int, int col, int64_t e, float *u, float *h) {
-    if (c.momentum) {
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 2
+      for (int q = tid; q < units; q += 256) {
+        const int row = q / pieces, col = (q - row * pieces) * 8;
+        const int64_t from = row * m.ld + col;
+        float u[8];
+        row8(in + from, cols - col, wide, u);
+        if (c.momentum) {
+          float h[8];
+          row8(at.momentum + from, cols - col, wide_m, h);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        h[i] = fmaf(c.mu, h[i], u[i]);
-        if (col + i < cols) at.momentum[e + i] = h[i];
-        u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
+          for (int e = 0; e < 8; ++e) {
+            if (pass == 0) {
+              h[e] = fmaf(c.mu, h[e], u[e]);
+              if (col + e < cols) at.momentum[from + e] = h[e];
+            }
+            u[e] = c.nesterov ? fmaf(c.mu, h[e], u[e]) : h[e];
+          }
+        }
+        if (pass == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) squares = fma(static_cast<double>(u[e]), static_cast<double>(u[e]), squares);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (col + e >= cols) continue;
+            const int to = m.tall ? place(col + e, row & ~3) + (row & 3) : place(row, (col + e) & ~3) + ((col + e) & 3);
+            split_half(u[e] * inverse * kScaleX, x[0][to], x[1][to]);
+          }
+        }
+      }
+      if (pass == 0) {
+        for (int q = tid; q < N * tiles * N / 8; q += 256) {  // zeros where the padding is
+          const half8 none = {};
+          *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
+          *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
+        }
+        inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
       }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) squares = fma(static_cast<double>(u[i]), static_cast<double>(u[i]), squares);
-  };
-  // zeros where the padding is
-  for (int q = tid; q < N * tiles * N / 8; q += 256) {
-    const half8 none = {};
-    *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
-    *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
-  }
-  if (c.in_bf16)
-    walk(static_cast<const uint16_t *>(at.in), first_look);
-  else
-    walk(static_cast<const float *>(at.in), first_look);
-  const float inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
-  auto second_look = [&](int row, int col, int64_t, float *u, float *h) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (c.momentum) u[i] = c.nesterov ? fmaf(c.mu, h[i], u[i]) : h[i];
-      if (col + i >= cols) continue;
-      const int to = m.tall ? place(col + i, row & ~3) + (row & 3) : place(row, (col + i) & ~3) + ((col + i) & 3);
-      split_half(u[i] * inverse * kScaleX, x[0][to], x[1][to]);
-    }
   };
   if (c.in_bf16)
-    walk(static_cast<const uint16_t *>(at.in), second_look);
+    walk(static_cast<const uint16_t *>(at.in));
   else
-    walk(static_cast<const float *>(at.in), second_look);
+    walk(static_cast<const float *>(at.in));
   __syncthreads();
 
   // this wave's quarter of tile t: rows wb * N / 2 + y * 32 + low, columns t * N + wa * N / 2 + x * 32 + g * 8 + high * 4
@@ -852,32 +856,34 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
     const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((shared4)(from + place(r + 4, panel * 32 + col)));
     return __builtin_bit_cast(half8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  // acc = sum over `depth` of a and b, small products of pairs first
-  auto product = [&](int depth, auto &&a, auto &&b) {
+  // acc += a b over N of the summed side, of pairs the products of `pass`: hi lo, lo hi, hi hi
+  auto clear = [&] {
 #pragma unroll
     for (int xb = 0; xb < kBlocks; ++xb)
 #pragma unroll
       for (int yb = 0; yb < kBlocks; ++yb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[xb][yb][r] = 0.f;
-#pragma unroll
-    for (int pass = SPLIT ? 0 : 2; pass < 3; ++pass)
-      for (int s = 0; s < depth / kDeep; ++s)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          half8 fa[kBlocks], fb[kBlocks];
-#pragma unroll
-          for (int q = 0; q < kBlocks; ++q) {
-            fa[q] = a(pass == 1, q, s, kk);
-            fb[q] = b(pass == 0, q, s, kk);
-          }
-#pragma unroll
-          for (int xb = 0; xb < kBlocks; ++xb)
-#pragma unroll
-            for (int yb = 0; yb < kBlocks; ++yb)
-              acc[xb][yb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[xb], fb[yb], acc[xb][yb], 0, 0, 0);
-        }
   };
+  auto product = [&](int pass, auto &&a, auto &&b) {
+#pragma unroll
+    for (int s = 0; s < N / kDeep; ++s)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        half8 fa[kBlocks], fb[kBlocks];
+#pragma unroll
+        for (int q = 0; q < kBlocks; ++q) {
+          fa[q] = a(pass == 1, q, s, kk);
+          fb[q] = b(pass == 0, q, s, kk);
+        }
+#pragma unroll
+        for (int xb = 0; xb < kBlocks; ++xb)
+#pragma unroll
+          for (int yb = 0; yb < kBlocks; ++yb)
+            acc[xb][yb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[xb], fb[yb], acc[xb][yb], 0, 0, 0);
+      }
+  };
+  constexpr int kFirstPass = SPLIT ? 0 : 2;
   auto each_four = [&](auto &&f) {
 #pragma unroll
     for (int xb = 0; xb < kBlocks; ++xb)
@@ -902,9 +908,14 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
 
   for (int s = 0; s < steps.count; ++s) {
     const float sa = steps.a_power[s], sp = steps.p_power[s], a0 = steps.abc[s][0];
-    const bool carry = !SPLIT && steps.carry[s], last = s + 1 == steps.count;
-    product(tiles * N, [&](bool lo, int q, int d, int kk) { return along(x[lo], wa * (N / 2) + q * 32, d, kk); },
-            [&](bool lo, int q, int d, int kk) { return along(x[lo], wb * (N / 2) + q * 32, d, kk); });
+    const bool carry = !SPLIT && steps.carry[s];
+    clear();
+#pragma unroll
+    for (int pass = kFirstPass; pass < 3; ++pass)
+      for (int t = 0; t < tiles; ++t)
+        product(pass,
+                [&](bool lo, int q, int d, int kk) { return along(x[lo], wa * (N / 2) + q * 32, t * (N / kDeep) + d, kk); },
+                [&](bool lo, int q, int d, int kk) { return along(x[lo], wb * (N / 2) + q * 32, t * (N / kDeep) + d, kk); });
     each_four([&](int xb, int yb, int g) {
       float v[4];
 #pragma unroll
@@ -912,8 +923,11 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
       keep(gram, mine(0, xb, yb, g), v);
     });
     __syncthreads();
-    product(N, [&](bool lo, int q, int d, int kk) { return along(gram[lo], wa * (N / 2) + q * 32, d, kk); },
-            [&](bool lo, int q, int d, int kk) { return along(gram[lo], wb * (N / 2) + q * 32, d, kk); });
+    clear();
+#pragma unroll
+    for (int pass = kFirstPass; pass < 3; ++pass)
+      product(pass, [&](bool lo, int q, int d, int kk) { return along(gram[lo], wa * (N / 2) + q * 32, d, kk); },
+              [&](bool lo, int q, int d, int kk) { return along(gram[lo], wb * (N / 2) + q * 32, d, kk); });
     each_four([&](int xb, int yb, int g) {
       const int pos = mine(0, xb, yb, g);
       const half4 h = *reinterpret_cast<const half4 *>(gram[0] + pos);
@@ -932,9 +946,12 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
 #pragma unroll
     for (int t = 0; t < kMostTiles; ++t) {
       if (t >= tiles) break;
-      product(N, [&](bool lo, int q, int d, int kk) { return down(x[lo], d, (t * N + wa * (N / 2)) / 32 + q, kk); },
-              [&](bool lo, int q, int d, int kk) { return along(poly[lo], wb * (N / 2) + q * 32, d, kk); });
-      if (!last) __syncthreads();  // everybody has read this tile of X
+      clear();
+#pragma unroll
+      for (int pass = kFirstPass; pass < 3; ++pass)
+        product(pass, [&](bool lo, int q, int d, int kk) { return down(x[lo], d, (t * N + wa * (N / 2)) / 32 + q, kk); },
+                [&](bool lo, int q, int d, int kk) { return along(poly[lo], wb * (N / 2) + q * 32, d, kk); });
+      __syncthreads();  // everybody has read this tile of X
       each_four([&](int xb, int yb, int g) {
         const int pos = mine(t, xb, yb, g);
         float v[4];
@@ -946,30 +963,33 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
           for (int e = 0; e < 4; ++e)
             v[e] = fmaf(a0, static_cast<float>(h[e]) + static_cast<float>(lower[t][xb][yb][g][e]), v[e]);
         }
-        if (!last) {
-          lower[t][xb][yb][g] = keep(x, pos, v);
-          return;
-        }
-        const int row = wb * (N / 2) + yb * 32 + low, col = t * N + wa * (N / 2) + xb * 32 + g * 8 + high * 4;
-        if (row >= n) return;
-        const float scale = m.scale * (1.f / kScaleX);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (col + e >= k) continue;
-          const int64_t to = m.tall ? (col + e) * m.ld + row : row * m.ld + col + e;
-          if (c.out_bf16)
-            static_cast<uint16_t *>(at.out)[to] = narrow_bf16(v[e] * scale);
-          else
-            static_cast<float *>(at.out)[to] = v[e] * scale;
-        }
+        lower[t][xb][yb][g] = keep(x, pos, v);
       });
     }
     __syncthreads();
   }
+  // The result, hi + lo, in the caller's rows.
+  if constexpr (!SPLIT) {
+#pragma unroll
+    for (int t = 0; t < kMostTiles; ++t)
+      if (t < tiles) each_four([&](int xb, int yb, int g) { *reinterpret_cast<half4 *>(x[1] + mine(t, xb, yb, g)) = lower[t][xb][yb][g]; });
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int q = tid; q < units; q += 256) {
+    const int row = q / pieces, col = (q - row * pieces) * 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int from = m.tall ? place(min(col + e, cols - 1), row & ~3) + (row & 3) : place(row, (col + e) & ~3) + ((col + e) & 3);
+      v[e] = static_cast<float>(x[0][from]) + static_cast<float>(x[1][from]);
+    }
+    write_out(c, at, m.ld, row, rows, col, cols, v, m.scale * (1.f / kScaleX));
+  }
 }
 
 template <int N, bool SPLIT>
-constexpr size_t small_bytes() {  // while loading, X's lower halves lie where A and P come to be
+constexpr size_t small_bytes() {  // at both ends X's lower halves lie where A and P do in between
   const size_t parts = SPLIT ? 2 : 1;
   return sizeof(half) * (parts * N * kSmallLength + (SPLIT || 2 * N > kSmallLength ? 2 * parts * N * N : N * kSmallLength));
 }
