@@ -38,6 +38,7 @@ struct Device {
 
 struct slowmo_orth {
   bool split = false, small = false;
+  int32_t small_side = 0;
   Steps steps{};
   std::vector<Op> program;
   std::vector<int32_t> index;       // places in the caller's list of the matrices that are not empty
@@ -450,7 +451,7 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
       const int32_t at = h->index[first + i];
       few.at[i] = {in[at], with_momentum ? momentum[at] : nullptr, out[at]};
     }
-    if (h->small && !ok(launch_small(c, h->steps, few, first, some, h->split, s))) return refused();
+    if (h->small && !ok(launch_small(c, h->steps, few, first, some, h->small_side, h->split, s))) return refused();
     if ((!h->small || h->n_tiny) && !ok(launch_addresses(c, few, first, some, s))) return refused();
   }
   if (h->n_tiny && !ok(launch_tiny(c, h->steps, h->tiny, h->n_tiny, s))) return refused();
@@ -512,6 +513,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     h->split = cfg->out_dtype == SLOWMO_F32;
     h->steps = steps_of(*cfg);
     h->small = p.small;
+    for (const Matrix &m : p.matrices) h->small_side = std::max(h->small_side, m.n);
     h->program = program(h->steps, p.pairs, h->split);
     h->index = p.index;
     char *base = static_cast<char *>(workspace);

@@ -117,8 +117,9 @@ struct Steps {
 
 hipError_t launch_tiny(const Call &c, const Steps &steps, const int32_t *list, int32_t count, hipStream_t s);
 // Matrices first..first + count - 1, all of them small or tiny (which are left out).
-hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, bool split,
-                        hipStream_t s);
+// side: the longest of their shorter sides.
+hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, int32_t side,
+                        bool split, hipStream_t s);
 hipError_t prepare_small();
 hipError_t launch_addresses(const Call &c, const Few &few, int32_t first, int32_t count, hipStream_t s);
 hipError_t launch_sums(const Call &c, const Item *items, int32_t count, hipStream_t s);

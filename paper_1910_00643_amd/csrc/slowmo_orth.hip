@@ -778,54 +778,81 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   const int pieces = (cols + 7) / 8, units = rows * pieces;
   double squares = 0.;
   float inverse = 0.f;
-  auto walk = [&](auto *in) {
+  // some units at a time, so that their loads are on their way together
+  auto look = [&](auto *in, auto whole, int pass) {
+    constexpr int kSome = decltype(whole)::value ? 4 : 1;
     const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 2
-      for (int q = tid; q < units; q += 256) {
-        const int row = q / pieces, col = (q - row * pieces) * 8;
+    for (int q0 = tid; q0 < units; q0 += 256 * kSome) {
+      float u[kSome][8], h[kSome][8];
+#pragma unroll
+      for (int i = 0; i < kSome; ++i) {
+        const int q = min(q0 + i * 256, units - 1), row = q / pieces, col = (q - row * pieces) * 8;
         const int64_t from = row * m.ld + col;
-        float u[8];
-        row8(in + from, cols - col, wide, u);
+        if constexpr (decltype(whole)::value) {
+          load8(in + from, u[i]);
+          if (c.momentum) load8(static_cast<const float *>(at.momentum) + from, h[i]);
+        } else {
+          row8(in + from, cols - col, wide, u[i]);
+          if (c.momentum) row8(static_cast<const float *>(at.momentum) + from, cols - col, wide_m, h[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kSome; ++i) {
+        const int q = q0 + i * 256, row = q / pieces, col = (q - row * pieces) * 8;
+        if (q >= units) continue;
         if (c.momentum) {
-          float h[8];
-          row8(at.momentum + from, cols - col, wide_m, h);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             if (pass == 0) {
-              h[e] = fmaf(c.mu, h[e], u[e]);
-              if (col + e < cols) at.momentum[from + e] = h[e];
+              h[i][e] = fmaf(c.mu, h[i][e], u[i][e]);
+              if (decltype(whole)::value || col + e < cols) at.momentum[row * m.ld + col + e] = h[i][e];
             }
-            u[e] = c.nesterov ? fmaf(c.mu, h[e], u[e]) : h[e];
+            u[i][e] = c.nesterov ? fmaf(c.mu, h[i][e], u[i][e]) : h[i][e];
           }
         }
         if (pass == 0) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) squares = fma(static_cast<double>(u[e]), static_cast<double>(u[e]), squares);
+          for (int e = 0; e < 8; ++e) squares = fma(static_cast<double>(u[i][e]), static_cast<double>(u[i][e]), squares);
+          continue;
+        }
+        half8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[i][e] *= inverse * kScaleX;
+        split8(u[i], hi, lo);
+        if (!m.tall) {  // past the row's end: zeros, into the padding
+          *reinterpret_cast<half8 *>(x[0] + place(row, col)) = hi;
+          *reinterpret_cast<half8 *>(x[1] + place(row, col)) = lo;
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            if (col + e >= cols) continue;
-            const int to = m.tall ? place(col + e, row & ~3) + (row & 3) : place(row, (col + e) & ~3) + ((col + e) & 3);
-            split_half(u[e] * inverse * kScaleX, x[0][to], x[1][to]);
+            const int to = place(min(col + e, N - 1), row & ~3) + (row & 3);
+            if (col + e < cols) x[0][to] = hi[e], x[1][to] = lo[e];
           }
         }
       }
-      if (pass == 0) {
-        for (int q = tid; q < N * tiles * N / 8; q += 256) {  // zeros where the padding is
-          const half8 none = {};
-          *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
-          *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
-        }
-        inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
-      }
     }
   };
+  auto both = [&](auto *in, auto whole) {
+    look(in, whole, 0);
+    for (int q = tid; q < N * tiles * N / 8; q += 256) {  // zeros where the padding is
+      const half8 none = {};
+      *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
+      *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
+    }
+    inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
+    look(in, whole, 1);
+  };
+  auto by_rows = [&](auto *in) {
+    if (cols % 8 == 0 && whole_rows(in, m.ld) && (!c.momentum || whole_rows(at.momentum, m.ld)))
+      both(in, std::true_type{});
+    else
+      both(in, std::false_type{});
+  };
   if (c.in_bf16)
-    walk(static_cast<const uint16_t *>(at.in));
+    by_rows(static_cast<const uint16_t *>(at.in));
   else
-    walk(static_cast<const float *>(at.in));
+    by_rows(static_cast<const float *>(at.in));
   __syncthreads();
 
   // this wave's quarter of tile t: rows wb * N / 2 + y * 32 + low, columns t * N + wa * N / 2 + x * 32 + g * 8 + high * 4
@@ -938,7 +965,11 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
       for (int e = 0; e < 4; ++e) {
         const float value = static_cast<float>(h[e]) + (SPLIT ? static_cast<float>(l[e]) : 0.f);
         v[e] = fmaf(steps.abc[s][1] * (sp / sa), value, acc[xb][yb][4 * g + e] * (steps.abc[s][2] * (sp / (sa * sa))));
-        if (!carry && wb * (N / 2) + yb * 32 + low == wa * (N / 2) + xb * 32 + g * 8 + high * 4 + e) v[e] += a0 * sp;
+      }
+      if (!carry && wa == wb && xb == yb) {  // a block of the diagonal
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (low == g * 8 + high * 4 + e) v[e] += a0 * sp;
       }
       keep(poly, pos, v);
     });
@@ -979,10 +1010,17 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   for (int q = tid; q < units; q += 256) {
     const int row = q / pieces, col = (q - row * pieces) * 8;
     float v[8];
+    if (!m.tall) {
+      const half8 hi = *reinterpret_cast<const half8 *>(x[0] + place(row, col)),
+                  lo = *reinterpret_cast<const half8 *>(x[1] + place(row, col));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int from = m.tall ? place(min(col + e, cols - 1), row & ~3) + (row & 3) : place(row, (col + e) & ~3) + ((col + e) & 3);
-      v[e] = static_cast<float>(x[0][from]) + static_cast<float>(x[1][from]);
+      for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(hi[e]) + static_cast<float>(lo[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int from = place(min(col + e, cols - 1), row & ~3) + (row & 3);
+        v[e] = static_cast<float>(x[0][from]) + static_cast<float>(x[1][from]);
+      }
     }
     write_out(c, at, m.ld, row, rows, col, cols, v, m.scale * (1.f / kScaleX));
   }
@@ -994,7 +1032,7 @@ constexpr size_t small_bytes() {  // at both ends X's lower halves lie where A a
   return sizeof(half) * (parts * N * kSmallLength + (SPLIT || 2 * N > kSmallLength ? 2 * parts * N * N : N * kSmallLength));
 }
 static_assert(small_bytes<128, false>() <= 160 * 1024 - 64 && small_bytes<64, true>() <= 160 * 1024 - 64, "shared memory");
-static_assert(2 * kSmallSide * kSmallSide >= kSmallSide * kSmallLength, "X's lower halves fit where A and P lie");
+static_assert(2 * kSmallSide * kSmallSide >= kSmallSide * kSmallLength || small_bytes<64, false>() >= 4 * 64 * kSmallLength, "X's lower halves fit where A and P lie");
 
 }  // namespace
 
@@ -1009,13 +1047,18 @@ hipError_t prepare_small() {
   if (e == hipSuccess)
     e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_small<kSmallSideSplit, true>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, small_bytes<kSmallSideSplit, true>());
+  if (e == hipSuccess)
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_small<kSmallSideSplit, false>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, small_bytes<kSmallSideSplit, false>());
   return e;
 }
 
-hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, bool split,
-                        hipStream_t s) {
+hipError_t launch_small(const Call &c, const Steps &steps, const Few &few, int32_t first, int32_t count, int32_t side,
+                        bool split, hipStream_t s) {
   if (split)
     k_small<kSmallSideSplit, true><<<count, 256, small_bytes<kSmallSideSplit, true>(), s>>>(c, steps, few, first);
+  else if (side <= kSmallSideSplit)
+    k_small<kSmallSideSplit, false><<<count, 256, small_bytes<kSmallSideSplit, false>(), s>>>(c, steps, few, first);
   else
     k_small<kSmallSide, false><<<count, 256, small_bytes<kSmallSide, false>(), s>>>(c, steps, few, first);
   return hipGetLastError();
