@@ -3,9 +3,10 @@
 //
 // Memory bounds both: a pass reads and writes every element once (forward 2 accesses an element,
 // backward 3).  A head's row lies in the registers of one group of lanes from its load to its
-// store: every lane holds both elements of 8 pairs, so that the rotation needs no other lane and
-// the mean of squares is the only exchange; the angles of a token are fetched once and serve all
-// of its heads.
+// store: every lane holds both elements of its pairs, so that the rotation needs no other lane and
+// the mean of squares is the only exchange.  A wave has queries or keys only -- one weight and one
+// sum for its gradient in registers -- and, where a token has enough heads, one token at a time, whose
+// angles are fetched once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,10 +24,21 @@ constexpr int kWaves = 4;                      // waves per workgroup
 constexpr int kThreads = 64 * kWaves;
 constexpr int kPairs = SLOWMO_MAX_HEAD_DIM / 2;
 constexpr int kFill = 8192;                    // waves that fill the card: 256 CUs, 8 waves per SIMD
+constexpr int kWalks = 768;                    // workgroups of a backward pass: all run at once, 3 per CU
 
 struct Rows {
   void *data;
   int64_t token, head;
+};
+
+// Queries or keys.  A turn of a wave takes `groups` rows: heads of one token, or, where it has fewer
+// heads than there are groups, all heads of `together` tokens.
+struct Side {
+  Rows x, g, y;          // inputs; backward: gradients of the outputs; outputs
+  const float *weight;
+  int64_t units;         // blocks of `together` tokens times `parts`
+  int32_t heads, together;
+  int32_t parts;         // waves that share a token's heads
 };
 
 struct HeadArgs {
@@ -34,18 +46,15 @@ struct HeadArgs {
   const float *table;
   const int64_t *positions;
   int64_t table_rows, position_stride;
-  Rows q, k;            // inputs
-  Rows gq, gk;          // backward: gradients of the outputs
-  Rows yq, yk;          // outputs
-  const float *wq, *wk;
+  Side side[2];
   const int64_t *slots;
   int64_t slot_rows;
-  float *partial;       // backward: [waves][2][D] sums for the weights' gradients
-  int32_t hq, heads;    // query heads, query and key heads together
+  float *partial;        // backward: [workgroups][2][D] sums for the weights' gradients
   int32_t dim, rot;
-  int32_t chunks;       // pieces of 2V elements in a row
-  int32_t lanes_log2;   // a row is spread over 1 << lanes_log2 lanes
-  int32_t parts;        // waves that share a token's heads
+  int32_t chunks;        // pieces of 2V elements in a row
+  int32_t lanes, groups; // lanes of a row, rows of a wave
+  int32_t lanes_log2;    // with the norm: lanes is a power of two
+  int32_t q_blocks;      // backward: workgroups of the queries, the keys' come after them
   int32_t axes;
   float eps;
   uint32_t pair_axis[kPairs / 16];  // 2 bits a pair
@@ -72,35 +81,57 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// A vector's load and store; NT: past the caches, for rows that nobody reads again soon.
+template <bool NT, typename V>
+__device__ __forceinline__ V fetch(const void *p) {
+  if constexpr (NT)
+    return __builtin_nontemporal_load(static_cast<const V *>(p));
+  else
+    return *static_cast<const V *>(p);
+}
+template <bool NT, typename V>
+__device__ __forceinline__ void leave(void *p, V v) {
+  if constexpr (NT)
+    __builtin_nontemporal_store(v, static_cast<V *>(p));
+  else
+    *static_cast<V *>(p) = v;
+}
+
 template <typename T, int V>
 struct Piece;  // V neighbouring elements
 
 template <>
 struct Piece<float, 8> {
+  template <bool NT = false>
   static __device__ __forceinline__ void load(const float *p, float *o) {
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+    const f32x4 a = fetch<NT, f32x4>(p), b = fetch<NT, f32x4>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = a[i], o[4 + i] = b[i];
   }
+  template <bool NT = false>
   static __device__ __forceinline__ void store(float *p, const float *o) {
-    *reinterpret_cast<f32x4 *>(p) = f32x4{o[0], o[1], o[2], o[3]};
-    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{o[4], o[5], o[6], o[7]};
+    leave<NT>(p, f32x4{o[0], o[1], o[2], o[3]});
+    leave<NT>(p + 4, f32x4{o[4], o[5], o[6], o[7]});
   }
 };
 template <>
 struct Piece<float, 4> {
+  template <bool NT = false>
   static __device__ __forceinline__ void load(const float *p, float *o) {
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p);
+    const f32x4 a = fetch<NT, f32x4>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = a[i];
   }
+  template <bool NT = false>
   static __device__ __forceinline__ void store(float *p, const float *o) {
-    *reinterpret_cast<f32x4 *>(p) = f32x4{o[0], o[1], o[2], o[3]};
+    leave<NT>(p, f32x4{o[0], o[1], o[2], o[3]});
   }
 };
 template <typename T>
 struct Piece<T, 1> {
+  template <bool NT = false>
   static __device__ __forceinline__ void load(const T *p, float *o) { o[0] = widen(*p); }
+  template <bool NT = false>
   static __device__ __forceinline__ void store(T *p, const float *o) {
     if constexpr (sizeof(T) == 4)
       *p = o[0];
@@ -110,31 +141,34 @@ struct Piece<T, 1> {
 };
 template <>
 struct Piece<uint16_t, 8> {
+  template <bool NT = false>
   static __device__ __forceinline__ void load(const uint16_t *p, float *o) {
-    const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+    const u32x4 a = fetch<NT, u32x4>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       o[2 * i] = __builtin_bit_cast(float, a[i] << 16);
       o[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
     }
   }
+  template <bool NT = false>
   static __device__ __forceinline__ void store(uint16_t *p, const float *o) {
-    *reinterpret_cast<u32x4 *>(p) =
-        u32x4{narrow2(o[0], o[1]), narrow2(o[2], o[3]), narrow2(o[4], o[5]), narrow2(o[6], o[7])};
+    leave<NT>(p, u32x4{narrow2(o[0], o[1]), narrow2(o[2], o[3]), narrow2(o[4], o[5]), narrow2(o[6], o[7])});
   }
 };
 template <>
 struct Piece<uint16_t, 4> {
+  template <bool NT = false>
   static __device__ __forceinline__ void load(const uint16_t *p, float *o) {
-    const u32x2 a = *reinterpret_cast<const u32x2 *>(p);
+    const u32x2 a = fetch<NT, u32x2>(p);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       o[2 * i] = __builtin_bit_cast(float, a[i] << 16);
       o[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
     }
   }
+  template <bool NT = false>
   static __device__ __forceinline__ void store(uint16_t *p, const float *o) {
-    *reinterpret_cast<u32x2 *>(p) = u32x2{narrow2(o[0], o[1]), narrow2(o[2], o[3])};
+    leave<NT>(p, u32x2{narrow2(o[0], o[1]), narrow2(o[2], o[3])});
   }
 };
 
@@ -232,7 +266,7 @@ __device__ __forceinline__ int shared_axis(const HeadArgs &a, const Place &p) {
 // Turns a lane's pairs by the angle (DIR 1) or back (DIR -1).  Past the rotated part c = 1, s = 0,
 // whichever two elements are taken as a pair.
 template <int V, bool INTER, int DIR>
-__device__ __forceinline__ void turn(float *u, float *v, const float *c, const float *s) {
+__device__ __forceinline__ void turn_pairs(float *u, float *v, const float *c, const float *s) {
   if constexpr (INTER && V > 1) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {  // pair i: elements 2i, 2i + 1 of u followed by v
@@ -251,22 +285,22 @@ __device__ __forceinline__ void turn(float *u, float *v, const float *c, const f
   }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool NT>
 __device__ __forceinline__ void load_row(const Rows &r, int64_t t, int64_t h, const Place &p, float *u,
                                          float *v) {
   const T *x = static_cast<const T *>(r.data) + t * r.token + h * r.head;
-  Piece<T, V>::load(x + p.u, u);
+  Piece<T, V>::template load<NT>(x + p.u, u);
   if (p.both)
-    Piece<T, V>::load(x + p.v, v);
+    Piece<T, V>::template load<NT>(x + p.v, v);
   else
     v[0] = 0.f;
 }
-template <typename T, int V>
+template <typename T, int V, bool NT>
 __device__ __forceinline__ void store_row(const Rows &r, int64_t t, int64_t h, const Place &p,
                                           const float *u, const float *v) {
   T *x = static_cast<T *>(r.data) + t * r.token + h * r.head;
-  Piece<T, V>::store(x + p.u, u);
-  if (p.both) Piece<T, V>::store(x + p.v, v);
+  Piece<T, V>::template store<NT>(x + p.u, u);
+  if (p.both) Piece<T, V>::template store<NT>(x + p.v, v);
 }
 
 template <int V>
@@ -278,125 +312,143 @@ __device__ __forceinline__ void load_weight(const float *w, const Place &p, floa
   }
 }
 
-// A wave takes one token and a share of its heads, 64 >> lanes_log2 heads at a time.  NCH: pieces
-// of a row per lane (more than one only in the element-by-element variant).
-template <typename T, int V, int NCH, bool INTER, bool NORM>
+// A row of a turn: which token and head lane group g has.
+struct Row {
+  int64_t t;
+  int32_t h;
+  bool live;
+};
+__device__ __forceinline__ Row row_of(const HeadArgs &a, const Side &s, int64_t block, int turn, int g) {
+  Row r;
+  if (s.together > 1) {
+    const int ahead = g / s.heads;
+    r.t = block * s.together + ahead;
+    r.h = g - ahead * s.heads;
+    r.live = ahead < s.together && r.t < a.tokens;
+  } else {
+    r.t = block;
+    r.h = turn * a.groups + g;
+    r.live = g < a.groups && r.h < s.heads;
+  }
+  if (!r.live) r.t = min(r.t, a.tokens - 1);  // read for its angles all the same
+  return r;
+}
+
+// NCH: pieces of a row per lane (more than one only in the element-by-element variant).
+template <typename T, int V, int NCH, bool INTER, bool NORM, bool NT>
 __global__ __launch_bounds__(kThreads) void k_head_forward(HeadArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t t = unit / a.parts;
-  if (t >= a.tokens) return;
-  const int part = static_cast<int>(unit - t * a.parts);
-  const int lanes = 1 << a.lanes_log2, groups = 64 >> a.lanes_log2;
-  const int l = lane & (lanes - 1), g = lane >> a.lanes_log2;
+  int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool key = unit >= a.side[0].units;
+  const Side &s = a.side[key];
+  if (key) unit -= a.side[0].units;
+  if (unit >= s.units) return;
+  const int64_t block = unit / s.parts;
+  const int part = static_cast<int>(unit - block * s.parts);
+  const int g = lane / a.lanes, l = lane - g * a.lanes;
 
+  Row row = row_of(a, s, block, part, g);
   Place p[NCH];
-  float c[NCH][V], s[NCH][V], wq[NCH][2 * V], wk[NCH][2 * V];
+  float c[NCH][V], sn[NCH][V], w[NCH][2 * V];
 #pragma unroll
   for (int j = 0; j < NCH; ++j) {
-    p[j] = place<V, INTER>(a, l + lanes * j);
-    angles<V>(a, p[j], shared_axis<V>(a, p[j]), t, c[j], s[j]);
-    if constexpr (NORM) {
-      load_weight<V>(a.wq, p[j], wq[j], wq[j] + V);
-      load_weight<V>(a.wk, p[j], wk[j], wk[j] + V);
-    }
-  }
-  int64_t slot = t;
-  if (a.slots) {
-    slot = a.slots[t];
-    if (slot < 0 || slot >= a.slot_rows) slot = -1;
+    p[j] = place<V, INTER>(a, l + a.lanes * j);
+    angles<V>(a, p[j], shared_axis<V>(a, p[j]), row.t, c[j], sn[j]);
+    if constexpr (NORM) load_weight<V>(s.weight, p[j], w[j], w[j] + V);
   }
   const float inv_dim = 1.f / static_cast<float>(a.dim);
-  for (int h0 = part * groups; h0 < a.heads; h0 += a.parts * groups) {
-    const int h = h0 + g;
-    const bool key = h >= a.hq, live = h < a.heads;
+  for (int turn = part; turn * a.groups < s.heads; turn += s.parts) {
+    row = row_of(a, s, block, turn, g);
     float u[NCH][V], v[NCH][V], sq = 0.f;
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
 #pragma unroll
       for (int i = 0; i < V; ++i) u[j][i] = v[j][i] = 0.f;
-      if (live && p[j].here) load_row<T, V>(key ? a.k : a.q, t, key ? h - a.hq : h, p[j], u[j], v[j]);
+      if (row.live && p[j].here) load_row<T, V, NT>(s.x, row.t, row.h, p[j], u[j], v[j]);
       if constexpr (NORM) {
 #pragma unroll
         for (int i = 0; i < V; ++i) sq = fmaf(u[j][i], u[j][i], fmaf(v[j][i], v[j][i], sq));
       }
     }
     if constexpr (NORM) {
-      const float mean = group_sum(sq, a.lanes_log2) * inv_dim;
-      const float r = 1.f / sqrtf(mean + a.eps);
+      const float r = rsqrtf(group_sum(sq, a.lanes_log2) * inv_dim + a.eps);
 #pragma unroll
       for (int j = 0; j < NCH; ++j) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          u[j][i] *= r * (key ? wk[j][i] : wq[j][i]);
-          v[j][i] *= r * (key ? wk[j][V + i] : wq[j][V + i]);
+          u[j][i] *= r * w[j][i];
+          v[j][i] *= r * w[j][V + i];
         }
       }
     }
+    int64_t to = row.t;
+    bool store = row.live;
+    if (key && a.slots && store) {
+      to = a.slots[row.t];
+      store = to >= 0 && to < a.slot_rows;
+    }
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-      turn<V, INTER, 1>(u[j], v[j], c[j], s[j]);
-      if (live && p[j].here && (!key || slot >= 0))
-        store_row<T, V>(key ? a.yk : a.yq, key ? slot : t, key ? h - a.hq : h, p[j], u[j], v[j]);
+      turn_pairs<V, INTER, 1>(u[j], v[j], c[j], sn[j]);
+      if (store && p[j].here) store_row<T, V, NT>(s.y, to, row.h, p[j], u[j], v[j]);
     }
   }
 }
 
-// The gradient.  Waves walk over (token, share of its heads); the sums for the weights' gradients
-// stay in registers over the whole walk and are joined over the wave's groups, then over the
-// workgroup, and written once: k_head_weights adds them up in a fixed order.
-template <typename T, int V, int NCH, bool INTER, bool NORM>
+// The gradient.  Waves walk over their side's units; the sums for the weight's gradient stay in registers
+// over the whole walk and are joined over the wave's groups, then over the workgroup, and written once:
+// k_head_weights adds them up in a fixed order.
+template <typename T, int V, int NCH, bool INTER, bool NORM, bool NT>
 __global__ __launch_bounds__(kThreads) void k_head_backward(HeadArgs a) {
-  extern __shared__ float joined[];  // [kWaves][2][dim]
+  extern __shared__ float joined[];  // [kWaves][dim]
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lanes = 1 << a.lanes_log2, groups = 64 >> a.lanes_log2;
-  const int l = lane & (lanes - 1), g = lane >> a.lanes_log2;
+  const bool key = static_cast<int>(blockIdx.x) >= a.q_blocks;
+  const Side &s = a.side[key];
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) - (key ? a.q_blocks : 0)) * kWaves + wave;
+  const int64_t step = static_cast<int64_t>(key ? gridDim.x - a.q_blocks : a.q_blocks) * kWaves;
+  const int g = lane / a.lanes, l = lane - g * a.lanes;
 
   Place p[NCH];
   int axis[NCH];
-  float wq[NCH][2 * V], wk[NCH][2 * V], dwq[NCH][2 * V], dwk[NCH][2 * V];
+  float w[NCH][2 * V], dw[NCH][2 * V];
 #pragma unroll
   for (int j = 0; j < NCH; ++j) {
-    p[j] = place<V, INTER>(a, l + lanes * j);
+    p[j] = place<V, INTER>(a, l + a.lanes * j);
     axis[j] = shared_axis<V>(a, p[j]);
     if constexpr (NORM) {
-      load_weight<V>(a.wq, p[j], wq[j], wq[j] + V);
-      load_weight<V>(a.wk, p[j], wk[j], wk[j] + V);
+      load_weight<V>(s.weight, p[j], w[j], w[j] + V);
 #pragma unroll
-      for (int i = 0; i < 2 * V; ++i) dwq[j][i] = dwk[j][i] = 0.f;
+      for (int i = 0; i < 2 * V; ++i) dw[j][i] = 0.f;
     }
   }
   const float inv_dim = 1.f / static_cast<float>(a.dim);
-  const int64_t units = a.tokens * a.parts, step = static_cast<int64_t>(gridDim.x) * kWaves;
-  for (int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + wave; unit < units; unit += step) {
-    const int64_t t = unit / a.parts;
-    const int part = static_cast<int>(unit - t * a.parts);
-    float c[NCH][V], s[NCH][V];
+  for (int64_t unit = first; unit < s.units; unit += step) {
+    const int64_t block = unit / s.parts;
+    const int part = static_cast<int>(unit - block * s.parts);
+    Row row = row_of(a, s, block, part, g);
+    float c[NCH][V], sn[NCH][V];
 #pragma unroll
-    for (int j = 0; j < NCH; ++j) angles<V>(a, p[j], axis[j], t, c[j], s[j]);
-    for (int h0 = part * groups; h0 < a.heads; h0 += a.parts * groups) {
-      const int h = h0 + g;
-      const bool key = h >= a.hq, live = h < a.heads;
-      const int64_t at = key ? h - a.hq : h;
+    for (int j = 0; j < NCH; ++j) angles<V>(a, p[j], axis[j], row.t, c[j], sn[j]);
+    for (int turn = part; turn * a.groups < s.heads; turn += s.parts) {
+      row = row_of(a, s, block, turn, g);
       float u[NCH][V], v[NCH][V], xu[NCH][V], xv[NCH][V], sq = 0.f;
 #pragma unroll
       for (int j = 0; j < NCH; ++j) {
 #pragma unroll
         for (int i = 0; i < V; ++i) u[j][i] = v[j][i] = xu[j][i] = xv[j][i] = 0.f;
-        if (live && p[j].here) {
-          load_row<T, V>(key ? a.gk : a.gq, t, at, p[j], u[j], v[j]);
-          if constexpr (NORM) load_row<T, V>(key ? a.k : a.q, t, at, p[j], xu[j], xv[j]);
+        if (row.live && p[j].here) {
+          load_row<T, V, NT>(s.g, row.t, row.h, p[j], u[j], v[j]);
+          if constexpr (NORM) load_row<T, V, NT>(s.x, row.t, row.h, p[j], xu[j], xv[j]);
         }
-        turn<V, INTER, -1>(u[j], v[j], c[j], s[j]);
+        turn_pairs<V, INTER, -1>(u[j], v[j], c[j], sn[j]);
         if constexpr (NORM) {
 #pragma unroll
           for (int i = 0; i < V; ++i) sq = fmaf(xu[j][i], xu[j][i], fmaf(xv[j][i], xv[j][i], sq));
         }
       }
       if constexpr (NORM) {
-        const float r = 1.f / sqrtf(group_sum(sq, a.lanes_log2) * inv_dim + a.eps);
+        const float r = rsqrtf(group_sum(sq, a.lanes_log2) * inv_dim + a.eps);
         float dot = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
@@ -405,13 +457,11 @@ __global__ __launch_bounds__(kThreads) void k_head_backward(HeadArgs a) {
             xu[j][i] *= r;
             xv[j][i] *= r;
             const float pu = u[j][i] * xu[j][i], pv = v[j][i] * xv[j][i];
-            // no select on the sums alone: 0 * NaN of a dead row never enters
-            dwq[j][i] += live && !key ? pu : 0.f;
-            dwq[j][V + i] += live && !key ? pv : 0.f;
-            dwk[j][i] += live && key ? pu : 0.f;
-            dwk[j][V + i] += live && key ? pv : 0.f;
-            u[j][i] *= key ? wk[j][i] : wq[j][i];
-            v[j][i] *= key ? wk[j][V + i] : wq[j][V + i];
+            // a row that is not there has x = 0 and, where its angles are none, NaN for g: not 0 of it
+            dw[j][i] += row.live ? pu : 0.f;
+            dw[j][V + i] += row.live ? pv : 0.f;
+            u[j][i] *= w[j][i];
+            v[j][i] *= w[j][V + i];
             dot = fmaf(u[j][i], xu[j][i], fmaf(v[j][i], xv[j][i], dot));
           }
         }
@@ -427,7 +477,7 @@ __global__ __launch_bounds__(kThreads) void k_head_backward(HeadArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < NCH; ++j)
-        if (live && p[j].here) store_row<T, V>(key ? a.yk : a.yq, t, at, p[j], u[j], v[j]);
+        if (row.live && p[j].here) store_row<T, V, NT>(s.y, row.t, row.h, p[j], u[j], v[j]);
     }
   }
   if constexpr (NORM) {
@@ -436,50 +486,48 @@ __global__ __launch_bounds__(kThreads) void k_head_backward(HeadArgs a) {
     for (int j = 0; j < NCH; ++j) {
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) {
-        for (int o = lanes; o < 64; o <<= 1) {
-          dwq[j][i] += __shfl_xor(dwq[j][i], o);
-          dwk[j][i] += __shfl_xor(dwk[j][i], o);
-        }
+        for (int o = a.lanes; o < 64; o <<= 1) dw[j][i] += __shfl_xor(dw[j][i], o);
         const int e = i < V ? p[j].u + i : p[j].v + i - V;
-        if (g == 0 && p[j].here && (i < V || p[j].both)) {
-          joined[(2 * wave) * a.dim + e] = dwq[j][i];
-          joined[(2 * wave + 1) * a.dim + e] = dwk[j][i];
-        }
+        if (g == 0 && p[j].here && (i < V || p[j].both)) joined[wave * a.dim + e] = dw[j][i];
       }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.dim; e += kThreads) {
+    for (int e = threadIdx.x; e < a.dim; e += kThreads) {
       float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) sum += joined[2 * w * a.dim + e];
-      a.partial[static_cast<int64_t>(blockIdx.x) * 2 * a.dim + e] = sum;
+      for (int i = 0; i < kWaves; ++i) sum += joined[i * a.dim + e];
+      a.partial[static_cast<int64_t>(blockIdx.x) * a.dim + e] = sum;
     }
   }
 }
 
-// Adds the workgroups' sums: 16 columns a workgroup, 16 lanes down each.
-__global__ __launch_bounds__(256) void k_head_weights(const float *partial, int32_t blocks, int32_t dim,
-                                                      float *dq, float *dk) {
-  __shared__ float sums[16][17];
+// Adds the workgroups' sums: 16 columns of the queries' or the keys' a workgroup, 64 lanes down each.
+__global__ __launch_bounds__(1024) void k_head_weights(const float *partial, int32_t q_blocks, int32_t blocks,
+                                                       int32_t dim, float *dq, float *dk) {
+  __shared__ float sums[64][17];
   const int col = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int e = blockIdx.x * 16 + col;
+  const bool key = blockIdx.y != 0;
   float sum = 0.f;
-  if (e < 2 * dim)
-    for (int b = row; b < blocks; b += 16) sum += partial[static_cast<int64_t>(b) * 2 * dim + e];
+  if (e < dim) {
+#pragma unroll 4
+    for (int b = (key ? q_blocks : 0) + row; b < (key ? blocks : q_blocks); b += 64)
+      sum += partial[static_cast<int64_t>(b) * dim + e];
+  }
   sums[row][col] = sum;
   __syncthreads();
-  if (row != 0 || e >= 2 * dim) return;
+  float *to = key ? dk : dq;
+  if (row != 0 || e >= dim || !to) return;
   float all = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) all += sums[r][col];
-  float *to = e < dim ? dq : dk;
-  if (to) to[e < dim ? e : e - dim] = all;
+#pragma unroll 8
+  for (int r = 0; r < 64; ++r) all += sums[r][col];
+  to[e] = all;
 }
 
 // ---- host -------------------------------------------------------------------
 
 struct Shape {
-  int v, nch, lanes_log2, chunks;
+  int v, nch, lanes, lanes_log2, chunks;
 };
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -505,6 +553,8 @@ Shape shape_of(const slowmo_head_config &c, const slowmo_heads *const *every, in
   s.chunks = s.v > 1 ? c.head_dim / (2 * s.v) : (c.head_dim + 1) / 2;
   s.nch = s.v > 1 ? 1 : 4;
   while ((s.nch << s.lanes_log2) < s.chunks) ++s.lanes_log2;
+  // the mean is exchanged among a power of two; without it lanes need not be left over
+  s.lanes = c.norm ? 1 << s.lanes_log2 : (s.chunks + s.nch - 1) / s.nch;
   return s;
 }
 
@@ -595,30 +645,35 @@ void fill(HeadArgs &a, const slowmo_head_config &c, int64_t tokens, const slowmo
   a.positions = c.positions;
   a.table_rows = c.rotary_dim ? c.table_rows : 0;
   a.position_stride = c.position_stride;
-  a.q = rows_of(q);
-  a.k = rows_of(k);
-  a.wq = c.q_weight;
-  a.wk = c.k_weight;
-  a.hq = q.heads;
-  a.heads = q.heads + k.heads;
   a.dim = c.head_dim;
   a.rot = c.rotary_dim;
   a.chunks = s.chunks;
+  a.lanes = s.lanes;
   a.lanes_log2 = s.lanes_log2;
+  a.groups = 64 / s.lanes;
   a.axes = c.n_axes;
   a.eps = c.eps;
   if (c.pair_axis)
     for (int i = 0; i < c.rotary_dim / 2; ++i)
       a.pair_axis[i >> 4] |= static_cast<uint32_t>(c.pair_axis[i]) << (2 * (i & 15));
-  // few tokens: their heads go to several waves, down to one turn of the wave's groups each
-  const int64_t groups = 64 >> s.lanes_log2, turns = (a.heads + groups - 1) / groups;
-  a.parts = static_cast<int32_t>(
-      std::max<int64_t>(1, std::min<int64_t>(turns, kFill / std::max<int64_t>(tokens, 1))));
+  for (int key = 0; key < 2; ++key) {
+    Side &d = a.side[key];
+    const slowmo_heads &h = key ? k : q;
+    d.x = rows_of(h);
+    d.weight = key ? c.k_weight : c.q_weight;
+    d.heads = h.heads;
+    d.together = std::max(1, h.heads ? a.groups / h.heads : 1);
+    // few tokens: their heads go to several waves, down to one turn each
+    const int64_t blocks = (tokens + d.together - 1) / d.together, turns = (h.heads + a.groups - 1) / a.groups;
+    d.parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(turns, kFill / std::max<int64_t>(blocks, 1))));
+    d.units = h.heads ? blocks * d.parts : 0;
+  }
 }
 
-// Workgroups of the backward kernel: enough to fill the card, no more than there is work.
-int32_t backward_blocks(int64_t units) {
-  return static_cast<int32_t>(std::min<int64_t>((units + kWaves - 1) / kWaves, kFill / kWaves));
+// Workgroups of a side of the backward kernel: enough to fill the card, no more than there is work.
+int32_t backward_blocks(int64_t units, double share) {
+  return static_cast<int32_t>(std::min<int64_t>((units + kWaves - 1) / kWaves,
+                                                std::max<int64_t>(1, static_cast<int64_t>(kWalks * share))));
 }
 
 template <typename F>
@@ -629,18 +684,26 @@ void by_bool(bool b, F &&f) {
     f(std::false_type{});
 }
 
+// Whether rows are loaded and stored past the caches: where a pass moves several times what they hold.
+// Time past them over time through them: 70 MB 1.43, 220 MB 1.01, 500 MB 1.08, 1 GB 0.92.
+bool streams(const HeadArgs &a, const slowmo_head_config &c, int passes) {
+  const int64_t bytes = a.tokens * (a.side[0].heads + a.side[1].heads) * a.dim * (c.dtype == SLOWMO_BF16 ? 2 : 4);
+  return passes * bytes >= (int64_t(768) << 20);
+}
+
 template <typename F>
-void dispatch(const slowmo_head_config &c, const Shape &s, F &&f) {
+void dispatch(const slowmo_head_config &c, const Shape &s, bool streaming, F &&f) {
   by_bool(c.interleaved, [&](auto inter) {
     by_bool(c.norm, [&](auto norm) {
       auto typed = [&](auto zero) {
         using T = decltype(zero);
+        std::integral_constant<int, 1> one;
         if (s.v == 8)
-          f(zero, std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{}, inter, norm);
+          by_bool(streaming, [&](auto nt) { f(zero, std::integral_constant<int, 8>{}, one, inter, norm, nt); });
         else if (s.v == 4)
-          f(zero, std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{}, inter, norm);
+          by_bool(streaming, [&](auto nt) { f(zero, std::integral_constant<int, 4>{}, one, inter, norm, nt); });
         else
-          f(T{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{}, inter, norm);
+          f(T{}, one, std::integral_constant<int, 4>{}, inter, norm, std::false_type{});
       };
       if (c.dtype == SLOWMO_BF16)
         typed(uint16_t{});
@@ -691,15 +754,15 @@ slowmo_status slowmo_head_norm_rotary(const slowmo_head_config *cfg, int64_t tok
     const Shape s = shape_of(*cfg, every, 4);
     HeadArgs a{};
     fill(a, *cfg, tokens, *q, *k, s);
-    a.yq = rows_of(*q_out);
-    a.yk = rows_of(*k_out);
+    a.side[0].y = rows_of(*q_out);
+    a.side[1].y = rows_of(*k_out);
     a.slots = k_slots;
     a.slot_rows = k_rows;
-    const int64_t blocks = (tokens * a.parts + kWaves - 1) / kWaves;
+    const int64_t blocks = (a.side[0].units + a.side[1].units + kWaves - 1) / kWaves;
     if (blocks > INT32_MAX) return fail_thread(SLOWMO_ERR_ARG, "too many tokens for one call");
     hipError_t e = hipSuccess;
-    dispatch(*cfg, s, [&](auto zero, auto v, auto nch, auto inter, auto norm) {
-      k_head_forward<decltype(zero), v(), nch(), inter(), norm()>
+    dispatch(*cfg, s, streams(a, *cfg, 2), [&](auto zero, auto v, auto nch, auto inter, auto norm, auto nt) {
+      k_head_forward<decltype(zero), v(), nch(), inter(), norm(), nt()>
           <<<static_cast<uint32_t>(blocks), kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
       e = hipGetLastError();
     });
@@ -713,8 +776,8 @@ size_t slowmo_head_backward_bytes(const slowmo_head_config *cfg, int64_t tokens,
       q_heads < 0 || k_heads < 0 || q_heads > (1 << 20) || k_heads > (1 << 20))
     return 0;
   // the number of workgroups depends on the pieces, so on alignment: the most there can be
-  const int64_t units = tokens * std::max<int64_t>(1, std::min<int64_t>(q_heads + k_heads, kFill / tokens));
-  return static_cast<size_t>(backward_blocks(units)) * 2 * cfg->head_dim * sizeof(float);
+  return static_cast<size_t>(std::min<int64_t>(kWalks + 2, tokens * (static_cast<int64_t>(q_heads) + k_heads) + 2)) *
+         cfg->head_dim * sizeof(float);
 }
 
 slowmo_status slowmo_head_norm_rotary_backward(const slowmo_head_config *cfg, int64_t tokens,
@@ -759,32 +822,34 @@ slowmo_status slowmo_head_norm_rotary_backward(const slowmo_head_config *cfg, in
     const Shape s = shape_of(*cfg, every, used);
     HeadArgs a{};
     fill(a, *cfg, tokens, *q, *k, s);
-    a.gq = rows_of(*gq);
-    a.gk = rows_of(*gk);
-    a.yq = rows_of(*dq);
-    a.yk = rows_of(*dk);
+    a.side[0].g = rows_of(*gq);
+    a.side[1].g = rows_of(*gk);
+    a.side[0].y = rows_of(*dq);
+    a.side[1].y = rows_of(*dk);
     const bool weights = dq_weight || dk_weight;
-    const int32_t blocks = a.heads ? backward_blocks(tokens * a.parts) : 0;
+    const double heads = std::max(1, q->heads + k->heads);
+    a.q_blocks = backward_blocks(a.side[0].units, q->heads / heads);
+    const int32_t blocks = a.q_blocks + backward_blocks(a.side[1].units, k->heads / heads);
     if (weights && blocks) {
       if (!workspace) return fail_thread(SLOWMO_ERR_ARG, "workspace is NULL");
       if (!aligned(workspace, 16)) return fail_thread(SLOWMO_ERR_ALIGN, "workspace must be 16-byte aligned");
-      if (workspace_bytes < static_cast<size_t>(blocks) * 2 * a.dim * sizeof(float))
+      if (workspace_bytes < static_cast<size_t>(blocks) * a.dim * sizeof(float))
         return fail_thread(SLOWMO_ERR_NOMEM, "workspace is smaller than slowmo_head_backward_bytes()");
       a.partial = static_cast<float *>(workspace);
     }
     hipError_t e = hipSuccess;
     if (blocks) {
-      dispatch(*cfg, s, [&](auto zero, auto v, auto nch, auto inter, auto norm) {
-        const uint32_t lds = norm() ? 2 * kWaves * a.dim * sizeof(float) : 0;
-        k_head_backward<decltype(zero), v(), nch(), inter(), norm()>
+      dispatch(*cfg, s, streams(a, *cfg, cfg->norm ? 3 : 2), [&](auto zero, auto v, auto nch, auto inter, auto norm, auto nt) {
+        const uint32_t lds = norm() ? kWaves * a.dim * sizeof(float) : 0;
+        k_head_backward<decltype(zero), v(), nch(), inter(), norm(), nt()>
             <<<blocks, kThreads, lds, static_cast<hipStream_t>(stream)>>>(a);
         e = hipGetLastError();
       });
       if (e != hipSuccess) return fail_thread_hip(e, "slowmo_head_norm_rotary_backward");
     }
     if (weights) {
-      k_head_weights<<<(2 * a.dim + 15) / 16, 256, 0, static_cast<hipStream_t>(stream)>>>(
-          a.partial, blocks, a.dim, dq_weight, dk_weight);
+      k_head_weights<<<dim3((a.dim + 15) / 16, 2), 1024, 0, static_cast<hipStream_t>(stream)>>>(
+          a.partial, a.q_blocks, blocks, a.dim, dq_weight, dk_weight);
       e = hipGetLastError();
       if (e != hipSuccess)
         return fail_thread_hip(e, "slowmo_head_norm_rotary_backward (gradients of q and k are written, "

@@ -102,7 +102,7 @@ class HeadNormRotary:
 
     Queries and keys are [tokens, heads, head_dim] (or with more leading dimensions that
     flatten without a copy), each head's elements contiguous, other strides free.
-    `positions` is int64, [tokens] or [axes, tokens]: rows of the table, -1 for no turn."""
+    A handle is not thread-safe.  `positions` is int64, [tokens] or [axes, tokens]: rows of the table, -1 for no turn."""
 
     def __init__(self, head_dim: int, table: Optional[torch.Tensor] = None, *, dtype: str = "bf16",
                  norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
@@ -116,33 +116,35 @@ class HeadNormRotary:
         self.table, self.dtype, self.norm = table, _TORCH_GRAD[dtype], bool(norm)
         self.head_dim, self.pairs = int(head_dim), pairs
         self._axis = None if pair_axis is None else (C.c_uint8 * max(pairs, 1))(*pair_axis)
-        self._fixed = dict(dtype=_DTYPE[dtype], head_dim=head_dim, rotary_dim=2 * pairs,
-                           interleaved=int(interleaved), norm=int(norm), eps=eps,
-                           pair_axis=C.addressof(self._axis) if self._axis is not None else None,
-                           table=table.data_ptr() if table is not None else None,
-                           table_rows=table.shape[0] if table is not None else 0)
+        self._cfg = slowmo_head_config(
+            dtype=_DTYPE[dtype], head_dim=head_dim, rotary_dim=2 * pairs, interleaved=int(interleaved),
+            norm=int(norm), eps=eps, n_axes=1,
+            pair_axis=C.addressof(self._axis) if self._axis is not None else None,
+            table=table.data_ptr() if table is not None else None,
+            table_rows=table.shape[0] if table is not None else 0)
 
     def _heads(self, x: torch.Tensor, what: str) -> slowmo_heads:
-        assert x.dtype == self.dtype and x.is_cuda, what
-        assert x.dim() == 3 and x.shape[2] == self.head_dim, what
-        st = x.stride()
+        shape, st = x.shape, x.stride()
+        assert x.dtype == self.dtype and x.is_cuda and len(shape) == 3 and shape[2] == self.head_dim, what
         assert st[2] == 1 or self.head_dim == 1 or x.numel() == 0, f"{what}: a head's elements must be contiguous"
-        return slowmo_heads(x.data_ptr() or None, x.shape[1], st[0], st[1])
+        return slowmo_heads(x.data_ptr() or None, shape[1], st[0], st[1])
 
     def _config(self, positions, tokens, wq, wk) -> slowmo_head_config:
-        for w in (wq, wk):
-            assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.is_cuda
-                                 and w.numel() == self.head_dim), "weights: [head_dim] fp32"
-        cfg = slowmo_head_config(q_weight=wq.data_ptr() if wq is not None else None,
-                                 k_weight=wk.data_ptr() if wk is not None else None,
-                                 n_axes=1, **self._fixed)
+        cfg = self._cfg                # one per handle: only what a call brings is written
+        for name, w in (("q_weight", wq), ("k_weight", wk)):
+            if w is not None:
+                assert w.dtype == torch.float32 and w.is_contiguous() and w.is_cuda \
+                    and w.numel() == self.head_dim, "weights: [head_dim] fp32"
+                setattr(cfg, name, w.data_ptr())
+            else:
+                setattr(cfg, name, None)
         if self.pairs:
+            shape = positions.shape
             assert positions.dtype == torch.int64 and positions.is_cuda
-            if positions.dim() == 2:
-                cfg.n_axes, cfg.position_stride = positions.shape[0], positions.stride(0)
-                if positions.shape[0] == 1:
-                    cfg.position_stride = 0
-            assert positions.shape[-1] == tokens and (tokens < 2 or positions.stride(-1) == 1)
+            cfg.n_axes, cfg.position_stride = 1, 0
+            if len(shape) == 2 and shape[0] != 1:
+                cfg.n_axes, cfg.position_stride = shape[0], positions.stride(0)
+            assert shape[-1] == tokens and (tokens < 2 or positions.stride(-1) == 1)
             cfg.positions = positions.data_ptr() or None
         return cfg
 
@@ -159,8 +161,8 @@ class HeadNormRotary:
         q, k = self._flat(q), self._flat(k)
         tokens = q.shape[0]
         assert k.shape[0] == tokens
-        yq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else self._flat(q_out)
-        yk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else self._flat(k_out)
+        yq = q.new_empty(q.shape) if q_out is None else self._flat(q_out)
+        yk = k.new_empty(k.shape) if k_out is None else self._flat(k_out)
         assert yq.shape == q.shape and (k_slots is not None or yk.shape == k.shape)
         slots = None
         if k_slots is not None:
@@ -171,8 +173,8 @@ class HeadNormRotary:
         _check(lib().slowmo_head_norm_rotary(cfg, tokens, self._heads(q, "q"), self._heads(k, "k"),
                                              self._heads(yq, "q_out"), self._heads(yk, "k_out"), slots,
                                              yk.shape[0], _raw_stream(q.device) or None))
-        return (yq.view(shapes[0]) if q_out is None else q_out,
-                yk.view(shapes[1]) if k_out is None else k_out)
+        return ((yq if len(shapes[0]) == 3 else yq.view(shapes[0])) if q_out is None else q_out,
+                (yk if len(shapes[1]) == 3 else yk.view(shapes[1])) if k_out is None else k_out)
 
     def backward(self, gq, gk, q, k, positions=None, q_weight=None, k_weight=None):
         """(dq, dk, dq_weight, dk_weight) from the gradients of forward's results and its inputs;
