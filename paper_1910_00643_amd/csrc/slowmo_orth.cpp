@@ -67,7 +67,7 @@ struct Plan {
   Lists lists[kKinds];
   int64_t partial_sums = 0;   // floats
   int32_t tickets = 0;
-  size_t matrices_at = 0, addresses_at = 0, sums_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
+  size_t matrices_at = 0, addresses_at = 0, sums_at = 0, factor_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
          tiles_at[kKinds][3] = {}, tickets_at = 0, partial_at = 0, arena_at = 0, total = 0;
 };
 
@@ -240,7 +240,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.small = p.tiny.size() < p.matrices.size() && small == static_cast<int32_t>(p.matrices.size());
   if (p.small)
     for (auto &list : of) list.clear();
-  // Two steps at a time, on n x n matrices: see program().
+  // The first two steps as one, on n x n matrices: see program().
   p.pairs = !p.small && c.steps >= 3 && by_pairs < 0.93 * one_by_one;
 
   int64_t halves = 0;
@@ -319,6 +319,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.matrices_at = section(p.matrices.size() * sizeof(Matrix));
   p.addresses_at = section(p.matrices.size() * sizeof(Addresses));
   p.sums_at = section(p.sums.size() * sizeof(double));
+  p.factor_at = section(p.matrices.size() * sizeof(float));
   p.tiny_at = section(p.tiny.size() * sizeof(int32_t));
   p.sum_items_at = section(p.sums.size() * sizeof(Item));
   p.load_at = section(p.load.size() * sizeof(Item));
@@ -349,11 +350,13 @@ float power(double most) {
 }
 
 // The steps as launches.  One step is A = X X^T, P = b A + c A A, X <- a X + P X.  Where X is much
-// longer than wide, two steps are one: with P0 from A0, the second step's A is (a0 + P0)^2 A0, a product of
-// n x n matrices too, and X <- a0 a1 X + Q X with Q = (a0 + P0)(a1 + P1) - a0 a1.  X is read and
-// written half as often, and of the products with X two of three per pair are left: 3 n n k + 5 n n n
-// for 6 n n k + 2 n n n.  (All n x n factors are polynomials of the same A, so that each product of
-// two is symmetric again.)  The last step is never one of a pair: rounding would show.
+// longer than wide, the first two steps are one: with P0 from A0, the second step's A is
+// (a0 + P0)^2 A0, a product of n x n matrices too, and X <- a0 a1 X + Q X with
+// Q = (a0 + P0)(a1 + P1) - a0 a1: 3 n n k + 5 n n n for 6 n n k + 2 n n n, and X is read and written once
+// less.  (All n x n factors are polynomials of the same A, so that each product of two is symmetric
+// again.)  Only the first two: A's roundings reach the second step's A a0^2 = 12 times as large, which shows
+// once singular values are near 1.  512 x 2048 against 64 bits, products of halves / of pairs: one by
+// one 0.8e-3 / 2.2e-6, first two 0.8e-3 / 1.8e-6, the next two as well 3.3e-3 / 3.8e-6.
 // Leaves the powers of two with the steps.  Returns an empty program if the coefficients let X outgrow a half.
 std::vector<Op> program(Steps &steps, bool pairs, bool split) {
   std::vector<Op> ops;
@@ -366,7 +369,7 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
   double most = 1.;   // of the singular values
   int32_t from = 0;
   for (int32_t t = 0; t < steps.count;) {
-    const bool two = pairs && steps.count - t >= 3;
+    const bool two = pairs && t == 0;
     const double a0 = steps.abc[t][0], b0 = steps.abc[t][1], c0 = steps.abc[t][2];
     auto p0 = [=](double s) { return b0 * s * s + c0 * s * s * s * s; };
     // Of single halves the last two steps' a goes to P's diagonal; the others' X enters as hi + lo.
@@ -378,12 +381,12 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
     steps.a_power[t] = sa;
     steps.p_power[t] = sp;
     steps.carry[t] = carry;
-    symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f});
+    symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f, t == 0});
     symmetric({from, kA, kA, kA, -1, kP, static_cast<float>(c0 * sp / (double(sa) * sa)),
-               static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp)});
+               static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp), 0});
     Op op{};
     op.update = true;
-    op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0)};
+    op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0), t == 0};
     double after = largest(most, [&](double s) { return s * (a0 + p0(s)); });
     if (two) {
       const double a1 = steps.abc[t + 1][0], b1 = steps.abc[t + 1][1], c1 = steps.abc[t + 1][2];
@@ -394,12 +397,12 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
       const float sa1 = power(largest(most, [&](double s) { return x1(s) * x1(s); }));
       const float sp1 = power(largest(most, p1));
       const float sq = power(largest(most, [&](double s) { return (a0 + p0(s)) * (a1 + p1(s)) - a0 * a1 + keep; }));
-      symmetric({from, kP, kA, kA, -1, kW, sw / (sp * sa), static_cast<float>(a0 * sw / sa), 0.f, 0.f});
-      symmetric({from, kW, kP, kW, -1, kA, sa1 / (sw * sp), static_cast<float>(a0 * sa1 / sw), 0.f, 0.f});
+      symmetric({from, kP, kA, kA, -1, kW, sw / (sp * sa), static_cast<float>(a0 * sw / sa), 0.f, 0.f, 0});
+      symmetric({from, kW, kP, kW, -1, kA, sa1 / (sw * sp), static_cast<float>(a0 * sa1 / sw), 0.f, 0.f, 0});
       symmetric({from, kA, kA, kA, -1, kW, static_cast<float>(c1 * sp1 / (double(sa1) * sa1)),
-                 static_cast<float>(b1 * sp1 / sa1), 0.f, 0.f});
+                 static_cast<float>(b1 * sp1 / sa1), 0.f, 0.f, 0});
       symmetric({from, kW, kP, kP, kW, kQ, sq / (sp1 * sp), static_cast<float>(a1 * sq / sp),
-                 static_cast<float>(a0 * sq / sp1), static_cast<float>(keep * sq)});
+                 static_cast<float>(a0 * sq / sp1), static_cast<float>(keep * sq), 0});
       op.up.by = kQ;
       op.up.alpha = 1.f / sq;
       op.up.beta = static_cast<float>(a0 * a1);
@@ -441,6 +444,7 @@ slowmo_status run(slowmo_orth *h, const void *const *in, float *const *momentum,
   c.mu = mu;
   c.nesterov = nesterov;
   c.momentum = with_momentum;
+  c.exact = c.in_bf16 && !with_momentum && !h->split;
   hipError_t e = hipSuccess;
   auto ok = [&](hipError_t got) { return (e = got) == hipSuccess; };
   auto refused = [&] { return fail_thread_hip(e, "slowmo_orthogonalize (results may be partly written)"); };
@@ -543,6 +547,7 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     if (e != hipSuccess) return fail_thread_hip(e, "slowmo_orth_create");
     h->call.addresses = reinterpret_cast<Addresses *>(base + p.addresses_at);
     h->call.sums = reinterpret_cast<double *>(base + p.sums_at);
+    h->call.factor = reinterpret_cast<float *>(base + p.factor_at);
     h->call.tickets = reinterpret_cast<uint32_t *>(base + p.tickets_at);
     h->call.partial = reinterpret_cast<float *>(base + p.partial_at);
     h->call.arena = reinterpret_cast<_Float16 *>(base + p.arena_at);

@@ -91,21 +91,27 @@ struct Call {
   float *partial;        // partial sums of tiles
   uint32_t *tickets;     // zero between calls
   float eps, mu;
+  float *factor;         // per matrix, where `exact`: X_0 over what is held in its place
   int32_t in_bf16, out_bf16, momentum, nesterov;
+  int32_t exact;         // X_0 is held as U times a power of two: 8 bits of bf16 fit a half whole, and no lower
+                         // halves are needed
   int32_t buffers;       // n x n buffers of a matrix
 };
 
+// (`first_step`: of X_0, which Call::exact may have held without its factor.)
 // out = alpha * left * right (+ beta * first) (+ gamma * second) (+ delta on the diagonal), symmetric;
 // buffers are numbered, left = -1: X X^T.  The factors hold the buffers' powers of two.
 struct Symmetric {
   int32_t from, left, right, first, second, out;  // first, second: -1: none
   float alpha, beta, gamma, delta;
+  int32_t first_step;
 };
 
 // x[1 - from] = alpha * buffer[by] x[from] (+ beta * (hi + lo of x[from])); or the caller's result.
 struct Update {
   int32_t from, by, carry, carry_next, last;
   float alpha, beta;
+  int32_t first_step;
 };
 
 struct Steps {

@@ -4,11 +4,11 @@
 // P X (2 n n k).  They run on the matrix cores in halves with fp32 sums.  Of the two 16-bit types a
 // half has 11 bits and bf16 has 8; X, A and P lie in a range known beforehand, so bf16's exponents buy
 // nothing.  A step multiplies small singular values by a = 3.4, so a rounding of X early on comes out
-// up to 3.4^5 times as large; X therefore keeps the next 11 bits too (x = hi + lo), which enter where X
-// enters linearly, in a X, while the products take hi alone.  Against 64 bits, 512 x 2048 and 1024 x
-// 1024 with flat, decaying and deficient spectra: 0.3e-3 to 1.7e-3 (hi alone 1.2e-3 to 8.6e-3, bf16
-// 0.9e-2 to 7e-2).  For fp32 results all factors are such pairs and a product is three: hi hi + hi lo +
-// lo hi, 22 bits.
+// up to 3.4^5 times as large; X therefore keeps the next 11 bits too (x = hi + lo) until the last two steps,
+// which enter where X enters linearly, in a X, while the products take hi alone.  Against 64 bits,
+// matrices of 64 to 1024 a side with flat spectra, a few strong directions above noise, or decaying ones:
+// 0.8e-3 to 1.5e-3, of deficient rank up to 2.9e-3 (hi alone up to 8.6e-3, products of bf16 up to 7e-2).
+// For fp32 results all factors are such pairs and a product is three: hi hi + hi lo + lo hi, 22 bits.
 #include "slowmo_orth.h"
 
 #include <type_traits>
@@ -177,7 +177,10 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   __shared__ double shared[4];
   double squares = 0.;
   for (int i = threadIdx.x; i < m.sums; i += 256) squares += c.sums[m.first_sum + i];
-  const float inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
+  const double by = inverse_norm(block_sum(squares, shared), c.eps);
+  const float inverse = static_cast<float>(by);
+  const int power = c.exact && by > 0. ? ilogb(by) : 0;
+  if (c.exact && it.i == 0 && it.j == 0 && threadIdx.x == 0) c.factor[it.matrix] = static_cast<float>(ldexp(by, -power));
   auto walk = [&](auto *in) {
     const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
     for (int patch = it.j; patch < it.j + kPatches && patch * kPatch < across; ++patch) {
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = u[i] * inverse * kScaleX;
+        for (int i = 0; i < 8; ++i) u[i] = c.exact ? ldexpf(u[i], power + 13) : u[i] * inverse * kScaleX;
         if (m.tall) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) turn[r][c8 + i] = row < rows && col + i < cols ? u[i] : 0.f;
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
           split8(u, hi, lo);
           const int64_t to = (static_cast<int64_t>(col >> 5) * m.np + row) * kDeep + (col & 31);
           *reinterpret_cast<half8 *>(x + to) = hi;
-          *reinterpret_cast<half8 *>(x_lo + to) = lo;
+          if (!c.exact) *reinterpret_cast<half8 *>(x_lo + to) = lo;
         }
       }
       if (!m.tall) continue;
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
         const int n = patch * kPatch + r, k = it.i * kPatch + c8;
         const int64_t to = (static_cast<int64_t>(k >> 5) * m.np + n) * kDeep + (k & 31);
         *reinterpret_cast<half8 *>(x + to) = hi;
-        *reinterpret_cast<half8 *>(x_lo + to) = lo;
+        if (!c.exact) *reinterpret_cast<half8 *>(x_lo + to) = lo;
       }
       __syncthreads();
     }
@@ -517,6 +520,13 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
   }
   __syncthreads();
 
+  float alpha = st.alpha, beta = st.beta;
+  const bool bare = st.first_step && c.exact;  // X_0 without its factor and lower halves
+  if (bare) {
+    const float factor = c.factor[it.matrix];
+    alpha *= UPDATE ? factor : factor * factor;
+    if constexpr (UPDATE) beta *= factor;
+  }
   const int ai = it.j * A + wa * kWideA, bi = it.i * B + wb * kWideB;  // first place along each factor
   if constexpr (UPDATE) {
     if (st.last) {
@@ -525,7 +535,7 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
       float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
       const Matrix &m = c.matrices[it.matrix];
       const Addresses at = c.addresses[it.matrix];
-      const float scale = m.scale * st.alpha * (1.f / kScaleX);
+      const float scale = m.scale * alpha * (1.f / kScaleX);
       auto leave = [&](auto wide, int row0, int rows, int col0, int cols) {
         constexpr int kLanes = decltype(wide)::value / 8, kRows = 64 / kLanes;
         const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
@@ -606,7 +616,7 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
         if constexpr (UPDATE) {
           if (st.carry) {
             more[x][0][g] = four(arena + places.x(st.from) + pos, g);
-            more[x][1][g] = four(arena + places.x_lo(0) + pos, g);
+            if (!bare) more[x][1][g] = four(arena + places.x_lo(0) + pos, g);
           }
         } else {
           constexpr int kNext = SPLIT ? 2 : 1;
@@ -630,15 +640,16 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
       for (int g = 0; g < 4; ++g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = acc[x][y][4 * g + e] * st.alpha;
+          float v = acc[x][y][4 * g + e] * alpha;
           if constexpr (UPDATE) {
-            if (st.carry) v = fmaf(st.beta, static_cast<float>(more[x][0][g][e]) + static_cast<float>(more[x][1][g][e]), v);
+            if (st.carry)
+              v = fmaf(beta, static_cast<float>(more[x][0][g][e]) + (bare ? 0.f : static_cast<float>(more[x][1][g][e])), v);
           } else {
             auto value = [&](int which) {
               const float h = static_cast<float>(more[x][which][g][e]);
               return SPLIT ? h + static_cast<float>(more[x][which + 1][g][e]) : h;
             };
-            if (st.first >= 0) v = fmaf(st.beta, value(0), v);
+            if (st.first >= 0) v = fmaf(beta, value(0), v);
             if (st.second >= 0) v = fmaf(st.gamma, value(SPLIT ? 2 : 1), v);
             if (row0 + low == col0 + g * 8 + high * 4 + e) v += st.delta;
           }
