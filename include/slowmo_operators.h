@@ -127,7 +127,9 @@ typedef struct {
   int32_t steps;      /* Newton-Schulz steps, 1..SLOWMO_MAX_ORTH_STEPS */
   int32_t scale;      /* slowmo_orth_scale */
   float eps;          /* added to the Frobenius norm, >= 0 */
-  const float *coefficients; /* host, [steps][3]: a, b, c of every step, finite; NULL: (3.4445, -4.7750, 2.0315) */
+  const float *coefficients; /* host, [steps][3]: a, b, c of every step, finite; NULL: (3.4445, -4.7750, 2.0315).
+                                Refused if some singular value of 0..1 comes to 7.5 or more in a step (8 less a
+                                margin): X's elements have to stay in a half's range */
 } slowmo_orth_config;
 
 /*
@@ -157,7 +159,8 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
 
 /*
  * out[i] <- the orthogonalised in[i].  `in` and `out` are host arrays of n_matrices device
- * pointers, aligned to their element size; out[i] may be in[i] where the types are the same.
+ * pointers, aligned to their element size; out[i] may be in[i] where the types are the same, and
+ * results overlap nothing else.
  * Errors: ARG, ALIGN, HIP.
  */
 slowmo_status slowmo_orthogonalize(slowmo_orth *h, const void *const *in, void *const *out,

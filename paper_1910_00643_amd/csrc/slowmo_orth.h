@@ -25,7 +25,8 @@ constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
 
 // X is held as halves times this power of two: its elements are below 8 in size (checked on the
 // coefficients), and what of them is subnormal as a half is below 2^-27.
-constexpr float kScaleX = 8192.f;
+constexpr int kPowerX = 13;
+constexpr float kScaleX = 1 << kPowerX;
 
 // A list of small matrices alone goes by one workgroup each too: n up to 128 and k up to 256 for products
 // of halves, n up to 64 for those of pairs of halves (X, A and P fill shared memory).

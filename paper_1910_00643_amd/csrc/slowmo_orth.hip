@@ -178,9 +178,9 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   double squares = 0.;
   for (int i = threadIdx.x; i < m.sums; i += 256) squares += c.sums[m.first_sum + i];
   const double by = inverse_norm(block_sum(squares, shared), c.eps);
-  const float inverse = static_cast<float>(by);
-  const int power = c.exact && by > 0. ? ilogb(by) : 0;
-  if (c.exact && it.i == 0 && it.j == 0 && threadIdx.x == 0) c.factor[it.matrix] = static_cast<float>(ldexp(by, -power));
+  const int power = by > 0. ? ilogb(by) : 0;  // apart: of subnormal matrices the inverse is no fp32 number
+  const float inverse = static_cast<float>(ldexp(by, -power));
+  if (c.exact && it.i == 0 && it.j == 0 && threadIdx.x == 0) c.factor[it.matrix] = inverse;
   auto walk = [&](auto *in) {
     const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
     for (int patch = it.j; patch < it.j + kPatches && patch * kPatch < across; ++patch) {
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = c.exact ? ldexpf(u[i], power + 13) : u[i] * inverse * kScaleX;
+        for (int i = 0; i < 8; ++i) u[i] = ldexpf(u[i], power + kPowerX) * (c.exact ? 1.f : inverse);
         if (m.tall) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) turn[r][c8 + i] = row < rows && col + i < cols ? u[i] : 0.f;
@@ -788,7 +788,8 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   // loops here are kept short rather than unrolled.
   const int pieces = (cols + 7) / 8, units = rows * pieces;
   double squares = 0.;
-  float inverse = 0.f;
+  float inverse = 0.f;  // times 2^power: of subnormal matrices it is no fp32 number
+  int power = 0;
   // some units at a time, so that their loads are on their way together
   auto look = [&](auto *in, auto whole, int pass) {
     constexpr int kSome = decltype(whole)::value ? 4 : 1;
@@ -829,7 +830,7 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
         }
         half8 hi, lo;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[i][e] *= inverse * kScaleX;
+        for (int e = 0; e < 8; ++e) u[i][e] = ldexpf(u[i][e], power) * inverse;
         split8(u[i], hi, lo);
         if (!m.tall) {  // past the row's end: zeros, into the padding
           *reinterpret_cast<half8 *>(x[0] + place(row, col)) = hi;
@@ -851,7 +852,10 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
       *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
       *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
     }
-    inverse = static_cast<float>(inverse_norm(block_sum(squares, shared), c.eps));
+    const double by = inverse_norm(block_sum(squares, shared), c.eps);
+    power = by > 0. ? ilogb(by) : 0;
+    inverse = static_cast<float>(ldexp(by, -power));
+    power += kPowerX;
     look(in, whole, 1);
   };
   auto by_rows = [&](auto *in) {
@@ -946,7 +950,9 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
 
   for (int s = 0; s < steps.count; ++s) {
     const float sa = steps.a_power[s], sp = steps.p_power[s], a0 = steps.abc[s][0];
-    const bool carry = !SPLIT && steps.carry[s];
+    // of pairs of halves always: with a on P's diagonal, results of matrices of deficient rank were 1.3 times as
+    // far off (64 x 40, rank 5: 1.6e-5 to 2.1e-5)
+    const bool carry = SPLIT || steps.carry[s];
     clear();
 #pragma unroll
     for (int pass = kFirstPass; pass < 3; ++pass)
@@ -1001,9 +1007,9 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
         for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (1.f / sp);
         if (carry) {
           const half4 h = *reinterpret_cast<const half4 *>(x[0] + pos);
+          const half4 l = SPLIT ? *reinterpret_cast<const half4 *>(x[1] + pos) : lower[t][xb][yb][g];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            v[e] = fmaf(a0, static_cast<float>(h[e]) + static_cast<float>(lower[t][xb][yb][g][e]), v[e]);
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(a0, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e]);
         }
         lower[t][xb][yb][g] = keep(x, pos, v);
       });

@@ -291,7 +291,11 @@ class Orthogonalizer:
         return (C.c_void_p * max(len(flat), 1))(*flat)
 
     def _array(self, tensors, dtype):
-        return tensors if isinstance(tensors, C.Array) else self.pointer_array(tensors, dtype)
+        if not isinstance(tensors, C.Array):
+            return self.pointer_array(tensors, dtype)
+        if len(tensors) < self.n_matrices:
+            raise ValueError(f"{self.n_matrices} addresses wanted, {len(tensors)} given")
+        return tensors
 
     def orthogonalize(self, inputs, out) -> None:
         """out[i] <- the orthogonalised inputs[i]: lists of tensors, or arrays from

@@ -69,3 +69,18 @@ def test_null_handles():
     assert L.slowmo_orthogonalize(None, None, None, None) == B.SLOWMO_ERR_ARG
     assert L.slowmo_momentum_orthogonalize(None, None, None, None, 0.9, 1, None) == B.SLOWMO_ERR_ARG
     assert L.slowmo_orth_destroy(None) == B.SLOWMO_OK
+
+
+def test_coefficients_that_let_singular_values_grow_are_refused():
+    """X is held as halves times 2^13: its elements have to stay below 8."""
+    three = lambda *abc: (C.c_float * 15)(*(abc * 5))  # noqa: E731
+    assert _bytes(_config(coefficients=three(3.4445, -4.7750, 2.0315))) > 0
+    assert _bytes(_config(coefficients=three(1.5, -0.5, 0.0))) > 0
+    assert _bytes(_config(coefficients=three(2.0, 0.0, 0.0))) == 0        # 2^5 times as large
+    assert "grow" in P.slowmo_last_error(None)
+    assert _bytes(_config(coefficients=three(1.0, 1.0, 1.0))) == 0
+    assert _bytes(_config(coefficients=three(-3e38, 3e38, 3e38))) == 0
+    h = C.c_void_p()
+    assert O.lib().slowmo_orth_create(C.byref(h), _config(coefficients=three(2.0, 0.0, 0.0)), 1, _i64(64), _i64(32),
+                                      None, 0x10000, 1 << 30, None) == B.SLOWMO_ERR_ARG
+    assert not h.value
