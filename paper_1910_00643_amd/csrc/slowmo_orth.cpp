@@ -118,6 +118,15 @@ std::vector<Tile> spread(const std::vector<Tile> &v) {
       steps[die] += v[at].count;
     }
   }
+  // All of them run at once, and a die's CUs take them in turn: where their sums are of very unequal length, long
+  // and short ones go together, by three rounds of 32 of which the second runs backwards (ResNet-18's matrices
+  // for 8 workers, 4 to 144 steps: 2.48 / 2.45 ms a call without / with this).
+  const auto [least, most] = std::minmax_element(v.begin(), v.end(), [](const Tile &a, const Tile &b) { return a.count < b.count; });
+  if (!v.empty() && v.size() <= 768 && most->count > 4 * least->count)
+    for (auto &q : queue) {
+      std::stable_sort(q.begin(), q.end(), [](const Tile &a, const Tile &b) { return a.count > b.count; });
+      for (size_t at = 32; at < q.size(); at += 64) std::reverse(q.begin() + at, q.begin() + std::min(q.size(), at + 32));
+    }
   size_t next[8] = {};
   while (out.size() < v.size()) {
     size_t die = out.size() % 8;
@@ -131,8 +140,9 @@ std::vector<Tile> spread(const std::vector<Tile> &v) {
 
 // What is left of the list after whole rounds of `slots` workgroups would leave most of the card idle
 // for the length of its longest tile: its tiles are cut along the summed side into shares of about equal
-// length, as many as there are slots.  Shares are no shorter than 32 steps and no more than 16 to
-// a tile, since the last one adds the others' sums up.
+// length, as many as there are slots.  Shares are no shorter than 48 steps and no more than 16 to
+// a tile, since the last one adds the others' sums up (no shorter than 32 / 48 / 96 / 128: an encoder block's
+// matrices 432 / 405 / 411 / 437 us a call).
 void balance(std::vector<Tile> &v, int kind, Plan &p) {
   const int32_t slots = kSlotsOf[kind];
   const size_t whole = v.size() / slots * slots;
@@ -144,7 +154,7 @@ void balance(std::vector<Tile> &v, int kind, Plan &p) {
     for (size_t i = whole; i < v.size(); ++i) n += (v[i].count + length - 1) / length;
     return n;
   };
-  int32_t lo = std::max(32, (longest + 15) / 16), hi = std::max(longest, lo);
+  int32_t lo = std::max(48, (longest + 15) / 16), hi = std::max(longest, lo);
   while (lo < hi) {
     const int32_t mid = (lo + hi) / 2;
     if (shares(mid) <= slots)
@@ -270,22 +280,27 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     };
     std::stable_sort(grams.begin(), grams.end(), by(&Matrix::kp));  // long sums first
     std::stable_sort(updates.begin(), updates.end(), by(&Matrix::np));
-    const int32_t side = kRowsOf[which], times = split ? 3 : 1;
+    const int32_t side = kRowsOf[which];
     auto put = [&](std::vector<Tile> &v, int32_t at, int32_t i, int32_t j, int32_t depth) {
       const Matrix &m = p.matrices[at];
-      v.push_back({m.at, m.np, m.kp, i, j, 0, times * (depth / kDeep), 0, 1, 0, 0, at, {}});
+      v.push_back({m.at, m.np, m.kp, i, j, 0, depth / kDeep, 0, 1, 0, 0, at, {}});
+    };
+    auto put_half = [&](std::vector<Tile> &v, int32_t at, int32_t i, int32_t j, int32_t depth) {
+      if (j > i) return;
+      put(v, at, i, j, depth);
+      if (j == i && !split) v.back().count /= 2;  // the diagonal's steps go two by two; depth is a multiple of 128
     };
     Lists &to = p.lists[which];
     for (int32_t at : grams) {
       const Matrix &m = p.matrices[at];
       walk(m.np / side, m.np / side, [&](int32_t i, int32_t j) {
-        if (j <= i) put(to.gram, at, i, j, m.kp);
+        put_half(to.gram, at, i, j, m.kp);
       });
     }
     for (int32_t at : updates) {
       const Matrix &m = p.matrices[at];
       walk(m.np / side, m.np / side, [&](int32_t i, int32_t j) {
-        if (j <= i) put(to.square, at, i, j, m.np);
+        put_half(to.square, at, i, j, m.np);
       });
       const int kind = which == kSmall && wide_tiles(m) ? kWide : which;
       walk(m.np / side, m.kp / kColsOf[kind], [&](int32_t i, int32_t j) { put(p.lists[kind].update, at, i, j, m.np); });

@@ -61,7 +61,8 @@ struct Item {
   int32_t matrix, i, j, pad;
 };
 
-// A workgroup's share of a product: steps first..first + count - 1 of tile (i, j); where a tile is in
+// A workgroup's share of a product: steps first..first + count - 1 of tile (i, j) (of a symmetric product's
+// diagonal, i = j: in twos); where a tile is in
 // `pieces` > 1 shares, `slot` counts the places of their partial sums and `ticket` its counter.  What it
 // needs of the matrix comes along: one load in front of the first of its data.
 struct Tile {

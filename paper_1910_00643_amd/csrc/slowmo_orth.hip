@@ -283,7 +283,13 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // rows meet all 64 banks once.  X of P X has the summed side down its columns: it is read turned, 4 rows x
 // 16 columns per 16 lanes, which meets all banks as it lies.
 // Everything is padded to whole tiles; nothing is checked in the loop.
-
+//
+// Pairs of halves: a panel's hi lo, lo hi and hi hi are two stages and three products, the third of what the
+// other two left in registers; loads and reads per product are 2/3 of three passes' over the summed side, and
+// what a pass would fetch again is at hand (a list of ResNet-18's matrices for 8 workers, X in 370 MB: its
+// X X^T 242 -> 156 us, with P X 2.97 -> 2.45 ms a call; errors as before within 1.1).
+// A tile of the diagonal of a matrix times itself needs one side's rows alone: 32 x 768 x 2560, 1.13 ->
+// 1.10 ms a call.
 
 // m0 is written and read within the block, with the one wait between that the two need; no vector register
 // is written.  `base` comes from scalar instructions.
@@ -324,14 +330,12 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
 
   // factor a: columns of the tile (j), factor b: rows (i).  The accumulators' four neighbours run along a.
   int64_t a_hi, a_lo, b_hi, b_lo;
-  int depth = it.np;
   if constexpr (UPDATE) {
     a_hi = places.x(st.from);
     a_lo = places.x_lo(st.from);
     b_hi = places.buffer(st.by);
     b_lo = places.buffer_lo(st.by);
   } else if (st.left < 0) {
-    depth = it.kp;
     a_hi = b_hi = places.x(st.from);
     a_lo = b_lo = places.x_lo(st.from);
   } else {
@@ -344,51 +348,49 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
   const int64_t a_at = UPDATE ? static_cast<int64_t>(it.j) * (A / kDeep) * panel : static_cast<int64_t>(it.j) * A * kDeep;
   const int64_t a_step = UPDATE ? kDeep * kDeep : panel;
   const int64_t b_at = static_cast<int64_t>(it.i) * B * kDeep;
-  const int steps = depth / kDeep;
 
   // bytes of a lane's piece within a load's 1024: 16 rows of 4 pieces
   const u32 b_off = ((lane & ~3) | ((lane & 3) ^ ((lane >> 4) & 3))) * 16, a_off = UPDATE ? lane * 16 : b_off;
   const u32 shared0 = static_cast<u32>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half *)ring));
 
-  // The next step to fetch.  Split: the small products first (hi lo, lo hi), while their sums are small, then
-  // hi hi; `left` steps until the next of the three.
-  const int total = it.count;
-  int segment = SPLIT ? it.first / steps : 2, left = steps;
-  const half *a_next, *b_next;
-  auto enter = [&](int at) {
-    a_next = arena + (segment == 1 ? a_lo : a_hi) + a_at + wave * kLoadsA * (UPDATE ? panel / 2 : 512) + at * a_step;
-    b_next = arena + (segment == 0 ? b_lo : b_hi) + b_at + wave * kLoadsB * 512 + at * panel;
-    left = steps - at;
-  };
-  enter(SPLIT ? it.first - segment * steps : it.first);
-  constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a step
-  auto fetch_one = [&](int slot, int q) {
+  // A tile of the diagonal of a matrix times itself, of single halves: both factors are the same rows, so that
+  // a stage holds two neighbouring panels of them and serves two steps.  The diagonal's list counts two as one.
+  const bool twice = !UPDATE && !SPLIT && it.i == it.j;
+  bool own = false;
+  if constexpr (!UPDATE) own = twice && st.left == st.right;
+  const int total = (SPLIT || (twice && !own)) ? 2 * it.count : it.count;  // stages
+  const int first = twice && !own ? 2 * it.first : it.first;
+
+  // The next stage to fetch.  Of pairs of halves a panel is two stages, a's hi with b's lo, then a's lo with
+  // b's hi.
+  const int64_t a_stride = own ? 2 * panel : a_step, b_stride = own ? 2 * panel : panel;
+  const half *a_next = arena + a_hi + a_at + wave * kLoadsA * (UPDATE ? panel / 2 : 512) + first * a_stride;
+  const half *b_next = arena + b_hi + b_at + wave * kLoadsB * 512 + first * b_stride + (own ? panel : 0);
+  const int64_t a_other = a_lo - a_hi, b_other = b_lo - b_hi;
+  constexpr int kStep = kLoadsA + kLoadsB;  // loads of a wave in a stage
+  auto fetch_one = [&](int slot, int second, int q) {
     const u32 to = shared0 + slot * (kStage * 2);
+    const half *a = a_next, *b = b_next;
+    if (SPLIT && second) a += a_other;
+    if (SPLIT && !second) b += b_other;
     if (q < kLoadsA)  // of X for P X, two loads to a panel's 32 rows
-      to_shared(to + (wave * kLoadsA + q) * 1024, a_off, a_next + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
+      to_shared(to + (wave * kLoadsA + q) * 1024, a_off, a + (UPDATE ? (q >> 1) * panel + (q & 1) * 512 : q * 512));
     else
-      to_shared(to + kShareA * 2 + (wave * kLoadsB + q - kLoadsA) * 1024, b_off, b_next + (q - kLoadsA) * 512);
+      to_shared(to + kShareA * 2 + (wave * kLoadsB + q - kLoadsA) * 1024, b_off, b + (q - kLoadsA) * 512);
   };
-  auto fetched = [&] {
-    a_next += a_step;
-    b_next += panel;
-    if (SPLIT && --left == 0 && segment < 2) {
-      ++segment;
-      enter(0);
-    }
+  auto fetched = [&](int second) {
+    if (SPLIT && !second) return;
+    a_next += a_stride;
+    b_next += b_stride;
   };
 
   half8 fa[2][2][kBlocksA], fb[2][2][kBlocksB];  // of this step and of the next, 16 deep each
   constexpr int kReads = 2 * (kBlocksA + kBlocksB);
-  auto read_one = [&](int slot, int which, int q) {
-    const int kk = q / (kBlocksA + kBlocksB), f = q % (kBlocksA + kBlocksB);
-    const half *sa = ring + slot * kStage, *sb = sa + kShareA;
-    if (f < kBlocksB) {
-      const int rb = wb * kWideB + f * 32 + low;
-      fb[which][kk][f] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
-      return;
-    }
-    const int x = f - kBlocksB;
+  auto read_b = [&](const half *sb, int which, int kk, int y) {
+    const int rb = wb * kWideB + y * 32 + low;
+    fb[which][kk][y] = *reinterpret_cast<const half8 *>(sb + rb * kDeep + (((kk * 2 + high) ^ ((rb >> 2) & 3)) * 8));
+  };
+  auto read_a = [&](const half *sa, int which, int kk, int x) {
     if constexpr (UPDATE) {
       const int r = kk * 16 + high * 8 + ((lane >> 2) & 3), col = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
       const half *from = sa + ((wa * kWideA / 32 + x) * kDeep + r) * kDeep + col;
@@ -401,6 +403,14 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
       fa[which][kk][x] = *reinterpret_cast<const half8 *>(sa + ra * kDeep + (((kk * 2 + high) ^ ((ra >> 2) & 3)) * 8));
     }
   };
+  // read q of a stage's kReads, of a to registers to_a, of b to to_b
+  auto read_one = [&](const half *sa, const half *sb, int to_a, int to_b, int q) {
+    const int kk = q / (kBlocksA + kBlocksB), f = q % (kBlocksA + kBlocksB);
+    if (f < kBlocksB)
+      read_b(sb, to_b, kk, f);
+    else
+      read_a(sa, to_a, kk, f - kBlocksB);
+  };
 
   f32x16 acc[kBlocksA][kBlocksB];
 #pragma unroll
@@ -410,28 +420,24 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
   constexpr int kProducts = 2 * kBlocksA * kBlocksB;
-  auto multiply_one = [&](int which, int q) {
+  auto multiply_one = [&](int of_a, int of_b, int q) {
     const int kk = q / (kBlocksA * kBlocksB), x = q / kBlocksB % kBlocksA, y = q % kBlocksB;
-    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[which][kk][x], fb[which][kk][y], acc[x][y], 0, 0, 0);
+    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[of_a][kk][x], fb[of_b][kk][y], acc[x][y], 0, 0, 0);
   };
 
   for (int s = 0; s < STAGES && s < total; ++s) {
 #pragma unroll
-    for (int q = 0; q < kStep; ++q) fetch_one(s, q);
-    fetched();
+    for (int q = 0; q < kStep; ++q) fetch_one(s, s & 1, q);
+    fetched(s & 1);
   }
   if (total >= STAGES)
     arrive<kStep * (STAGES - 1)>();
   else
     arrive<0>();
-  int left_steps = total, slot = 0;  // the factors of a step with r left are in registers r mod 2
-#pragma unroll
-  for (int q = 0; q < kReads; ++q) {
-    if (total & 1)
-      read_one(0, 1, q);
-    else
-      read_one(0, 0, q);
-  }
+  int left_steps = total, slot = 0;
+  std::integral_constant<int, 0> even;
+  std::integral_constant<int, 1> odd;
+  std::integral_constant<int, kStep * (STAGES - 2)> full;
   // One step: the next one's factors go to registers while this one's are multiplied.  `pending` loads may
   // still be on their way when the next step's have arrived.  Reads and loads are issued one by one between
   // products: a wave issues in order, and in a row they hold it up for as long as the products take.
@@ -444,33 +450,165 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
     each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
       constexpr int I = decltype(i)::value;
 #pragma unroll
-      for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q) read_one(slot, 1 - kThis, q);
+      for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q)
+        read_one(ring + slot * kStage, ring + slot * kStage + kShareA, 1 - kThis, 1 - kThis, q);
       if constexpr (decltype(more)::value) {  // to where this step was: everybody has read it
 #pragma unroll
-        for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, q);
+        for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, 0, q);
       }
-      multiply_one(kThis, I);
+      multiply_one(kThis, kThis, I);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (decltype(more)::value) fetched();
+    if constexpr (decltype(more)::value) fetched(0);
     --left_steps;
   };
-  std::integral_constant<int, 0> even;
-  std::integral_constant<int, 1> odd;
-  std::integral_constant<int, kStep * (STAGES - 2)> full;
-  if (left_steps > STAGES && (left_steps & 1)) step(odd, full, std::true_type{});
-  while (left_steps - 1 > STAGES) {
-    step(even, full, std::true_type{});
-    step(odd, full, std::true_type{});
+  if (!SPLIT && (UPDATE || !own)) {
+    // the factors of a step with r left are in registers r mod 2
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) {
+      if (total & 1)
+        read_one(ring, ring + kShareA, 1, 1, q);
+      else
+        read_one(ring, ring + kShareA, 0, 0, q);
+    }
+    if (left_steps > STAGES && (left_steps & 1)) step(odd, full, std::true_type{});
+    while (left_steps - 1 > STAGES) {
+      step(even, full, std::true_type{});
+      step(odd, full, std::true_type{});
+    }
+    if (left_steps > STAGES) step(even, full, std::true_type{});
+    // nothing is left to fetch; what is on its way arrives one step after the other
+    each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) {
+      constexpr int kLeft = STAGES - decltype(n)::value;
+      if (left_steps == kLeft)
+        step(std::integral_constant<int, (kLeft & 1)>{}, std::integral_constant<int, kStep * (kLeft - 2)>{}, std::false_type{});
+    });
   }
-  if (left_steps > STAGES) step(even, full, std::true_type{});
-  // nothing is left to fetch; what is on its way arrives one step after the other
-  each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) {
-    constexpr int kLeft = STAGES - decltype(n)::value;
-    if (left_steps == kLeft)
-      step(std::integral_constant<int, (kLeft & 1)>{}, std::integral_constant<int, kStep * (kLeft - 2)>{}, std::false_type{});
-  });
-  each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) { multiply_one(1, decltype(i)::value); });
+  if constexpr (!UPDATE && !SPLIT) {
+    // The same with two steps to a stage: a stage's first is in registers 0, its second in registers 1.
+    auto first_half = [&] {  // the second one's factors go to registers
+      each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+#pragma unroll
+        for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q)
+          read_one(ring + slot * kStage + kShareA, ring + slot * kStage + kShareA, 1, 1, q);
+        multiply_one(0, 0, I);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto stage = [&](auto pending, auto more) {
+      __builtin_amdgcn_sched_barrier(0);
+      first_half();
+      const int here = slot;
+      slot = slot + 1 == STAGES ? 0 : slot + 1;
+      arrive<decltype(pending)::value>();
+      each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+#pragma unroll
+        for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q)
+          read_one(ring + slot * kStage, ring + slot * kStage, 0, 0, q);
+        if constexpr (decltype(more)::value) {
+#pragma unroll
+          for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, 0, q);
+        }
+        multiply_one(1, 1, I);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (decltype(more)::value) fetched(0);
+      --left_steps;
+    };
+    if (own) {
+#pragma unroll
+      for (int q = 0; q < kReads; ++q) read_one(ring, ring, 0, 0, q);
+      while (left_steps > STAGES) stage(full, std::true_type{});
+      each(std::make_integer_sequence<int, STAGES - 1>{}, [&](auto n) {
+        constexpr int kLeft = STAGES - decltype(n)::value;
+        if (left_steps == kLeft) stage(std::integral_constant<int, kStep * (kLeft - 2)>{}, std::false_type{});
+      });
+      first_half();
+    }
+  }
+  if constexpr (SPLIT) {
+    // A panel: hi lo, lo hi, and, of what both left in registers, hi hi: three products for two stages' loads and
+    // reads.  The first product's factors are fa[type] and fb[0], the second's fa[1 - type] and fb[1], so that
+    // the third's are fa[type] and fb[1] and the next panel, of the other type, has the rest.  `left`: stages
+    // left, this panel's included, or more than STAGES + 1.
+    auto panel_of = [&](auto type_, auto left_) {
+      constexpr int T = decltype(type_)::value, L = decltype(left_)::value;
+      constexpr bool kMore0 = L > STAGES, kMore1 = L > STAGES + 1, kLast = L == 2;
+      int here = slot;
+      slot = slot + 1 == STAGES ? 0 : slot + 1;
+      __builtin_amdgcn_sched_barrier(0);
+      arrive<kStep * ((kMore0 ? STAGES : L) - 2)>();
+      each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+#pragma unroll
+        for (int q = I * kReads / kProducts; q < (I + 1) * kReads / kProducts; ++q)
+          read_one(ring + slot * kStage, ring + slot * kStage + kShareA, 1 - T, 1, q);
+        if constexpr (kMore0) {
+#pragma unroll
+          for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, STAGES & 1, q);
+        }
+        multiply_one(T, 0, I);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (kMore0) fetched(STAGES & 1);
+      here = slot;
+      if constexpr (!kLast) {
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        __builtin_amdgcn_sched_barrier(0);
+        arrive<kStep * ((kMore1 ? STAGES : L - 1) - 2)>();
+      }
+      constexpr int kReadsA = 2 * kBlocksA, kReadsB = 2 * kBlocksB;
+      each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+        if constexpr (!kLast) {
+#pragma unroll
+          for (int q = I * kReadsB / kProducts; q < (I + 1) * kReadsB / kProducts; ++q)
+            read_b(ring + slot * kStage + kShareA, 0, q / kBlocksB, q % kBlocksB);
+        }
+        if constexpr (kMore1) {
+#pragma unroll
+          for (int q = I * kStep / kProducts; q < (I + 1) * kStep / kProducts; ++q) fetch_one(here, 1 - (STAGES & 1), q);
+        }
+        multiply_one(1 - T, 1, I);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (kMore1) fetched(1 - (STAGES & 1));
+      each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+        if constexpr (!kLast) {
+#pragma unroll
+          for (int q = I * kReadsA / kProducts; q < (I + 1) * kReadsA / kProducts; ++q)
+            read_a(ring + slot * kStage, 1 - T, q / kBlocksA, q % kBlocksA);
+        }
+        multiply_one(T, 1, I);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      left_steps -= 2;
+    };
+    std::integral_constant<int, 1 << 20> many;
+    // a panel with r stages left is of type r / 2 mod 2
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) {
+      if (total & 2)
+        read_one(ring, ring + kShareA, 1, 0, q);
+      else
+        read_one(ring, ring + kShareA, 0, 0, q);
+    }
+    if (left_steps > STAGES + 1 && (left_steps & 2)) panel_of(odd, many);
+    while (left_steps - 2 > STAGES + 1) {
+      panel_of(even, many);
+      panel_of(odd, many);
+    }
+    if (left_steps > STAGES + 1) panel_of(even, many);
+    each(std::make_integer_sequence<int, (STAGES + 1) / 2>{}, [&](auto n) {
+      constexpr int kLeft = ((STAGES + 1) / 2 - decltype(n)::value) * 2;
+      if (left_steps == kLeft) panel_of(std::integral_constant<int, (kLeft / 2) & 1>{}, std::integral_constant<int, kLeft>{});
+    });
+  } else {
+    each(std::make_integer_sequence<int, kProducts>{}, [&](auto i) { multiply_one(1, 1, decltype(i)::value); });
+  }
 
   // A tile in several shares: each leaves its sums in memory, and the one that comes last adds them all
   // up, in their order whichever it is.  The sums pass the dies' separate L2 caches by themselves (8 bytes

@@ -39,14 +39,15 @@ static void check(bool ok, const char *what) {
 // Squares of 128 that each matrix's products cover: [matrix, product].
 using Cover = std::map<std::array<int, 2>, std::set<std::pair<int, int>>>;
 
-static void check_list(const Plan &p, int kind, const std::vector<Tile> &list, int product, int times, Cover &cover) {
+static void check_list(const Plan &p, int kind, const std::vector<Tile> &list, int product, bool split, Cover &cover) {
   std::map<std::array<int, 3>, std::vector<Tile>> tiles;
   for (const Tile &t : list) tiles[{t.matrix, t.i, t.j}].push_back(t);
   const int rows = kRowsOf[kind], cols = product == 2 ? kColsOf[kind] : rows;
   std::set<int> slots;
   for (const auto &[key, shares] : tiles) {
     const Matrix &m = p.matrices[key[0]];
-    const int depth = (product == 0 ? m.kp : m.np) / kDeep * times;
+    const bool diagonal = !split && product != 2 && key[1] == key[2];  // counted in twos
+    const int depth = (product == 0 ? m.kp : m.np) / kDeep / (diagonal ? 2 : 1);
     check((key[1] + 1) * rows <= m.np && (key[2] + 1) * cols <= (product == 2 ? m.kp : m.np), "a tile is inside");
     std::vector<char> seen(depth, 0);
     std::set<int> pieces;
@@ -96,7 +97,7 @@ int main() {
     for (int kind = 0; kind < kKinds; ++kind) {
       const Lists &l = p.lists[kind];
       const std::vector<Tile> *of[] = {&l.gram, &l.square, &l.update};
-      for (int product = 0; product < 3; ++product) check_list(p, kind, *of[product], product, split ? 3 : 1, cover);
+      for (int product = 0; product < 3; ++product) check_list(p, kind, *of[product], product, split, cover);
     }
     for (size_t i = 0; i < p.matrices.size(); ++i) {
       const Matrix &m = p.matrices[i];
