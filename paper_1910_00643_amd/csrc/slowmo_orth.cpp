@@ -199,6 +199,13 @@ bool large_tiles(const Matrix &m) {
 // Rows of 256 for P X: three quarters of the traffic per product, two workgroups per CU.
 bool wide_tiles(const Matrix &m) { return m.n >= 256 && m.kp % 256 == 0; }
 
+// One workgroup in 64 bits: what fits its shared memory, and longer ones that k_small does not take, while
+// the products' launches take longer (one workgroup / products: 604 x 17 72 / 123 us, 32 x 512 148 / 115 us).
+bool tiny(const Matrix &m) {
+  const int64_t n = m.n, k = m.k;
+  return n <= kTinySide && (n * k <= kTinyElements || (k > kSmallLength && n * n * k <= kTinyWork));
+}
+
 float factor(const slowmo_orth_config &c, int64_t rows, int64_t cols) {
   const double r = static_cast<double>(rows), k = static_cast<double>(cols);
   return static_cast<float>(c.scale == SLOWMO_SCALE_NONE    ? 1.
@@ -229,7 +236,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
     m.ld = ld ? ld[i] : cols[i];
     m.scale = factor(c, rows[i], cols[i]);
     const int32_t at = static_cast<int32_t>(p.matrices.size());
-    if (m.n <= kTinySide && static_cast<int64_t>(m.n) * m.k <= kTinyElements) {
+    if (tiny(m)) {
       p.tiny.push_back(at);
       m.tiny = 1;
     } else {

@@ -22,6 +22,7 @@ constexpr int32_t kSlotsOf[kKinds] = {768, 256, 512};  // workgroups that run at
 
 // Matrices that one workgroup takes from load to store.
 constexpr int kTinySide = 32, kTinyElements = 4096, kTinyThreads = 512;
+constexpr int64_t kTinyWork = int64_t(1) << 18;  // most of n n k, where the matrix is longer than kTinyElements
 
 // X is held as halves times this power of two: its elements are below 8 in size (checked on the
 // coefficients), and what of them is subnormal as a half is below 2^-27.

@@ -98,7 +98,10 @@ __device__ __forceinline__ double block_sum(double v, double *shared) {
 }
 
 // A workgroup's share of the sum of squares of U, in 64 bits: squares of fp32 values neither overflow nor
-// vanish there.  Updates the momentum on the way.
+// vanish there.  Updates the momentum on the way.  Memory bounds it: with momentum 5.3 TB/s (93 million fp32
+// elements in 211 us), alone 3.9 TB/s (67 million in 68 us).  That U is read again by k_load is the price of not
+// knowing its norm; by groups of matrices that the last-level cache would keep between the two, a call took
+// 1.00 to 1.15 of the time, since every launch has its ends.
 __global__ __launch_bounds__(256) void k_sums(Call c, const Item *items) {
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
@@ -165,7 +168,8 @@ __device__ __forceinline__ void split8(const float *v, half8 &hi, half8 &lo) {
 }
 
 // X_0 (n x k, turned if the caller's matrix is tall) as halves hi and lo, with zeros in the padding (which
-// an earlier call's NaN may have reached).
+// an earlier call's NaN may have reached).  Memory bounds it: 4.7 TB/s (93 million fp32 elements with momentum
+// in 239 us).  A patch of 64 x 64 turns in shared memory; rows of 65 keep its columns on different banks.
 __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   const Item it = items[blockIdx.x];
   const Matrix &m = c.matrices[it.matrix];
@@ -270,10 +274,16 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 
 // ---- products -----------------------------------------------------------------
 //
-// Tiles of B x A by 4 waves of B/2 x A/2, where A runs along the result's rows.  Steps of 32 of the summed side go from memory straight to a
-// ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead of their use.  A wave reads the next step's factors into
-// registers before it issues the products of this one, so that the matrix cores go on with one wave per SIMD
-// too (B = 256: 256 accumulators a lane).
+// Tiles of B x A by 4 waves of B/2 x A/2, where A runs along the result's rows.  Steps of 32 of the summed side
+// go from memory straight to a ring of STAGES stages in shared memory (16 bytes a lane), STAGES - 1 steps ahead
+// of their use.  A wave reads the next step's factors into registers between the products of this one, so that
+// the matrix cores go on with one wave per SIMD too (B = 256: 256 accumulators a lane).
+//
+// What bounds them: 8192 x 8192 (256 x 256) the matrix cores at the clock that their power leaves, 1.09e15
+// flop/s over the whole call, where a library's product of that size reaches 1.11e15.  The smaller tiles are
+// bound by the way from L2 to shared memory, 12.7 TB/s for 16 KB a step of 128 x 128 (0.33 us with every CU at
+// work, 0.13 us of it products): 0.75e15 in lists of many matrices; and a launch of one round by its ends, 8 us
+// of 16 (1024 x 1024 x 1024, 216 tiles).
 //
 // X and the n x n matrices lie in panels of 32 columns, [column / 32][row][column mod 32]: a step's share of a
 // factor is one piece of memory (P X's X: one per panel) and every cache line of it is used whole.  (Rows
@@ -819,80 +829,141 @@ __global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGE
   }
 }
 
-// A tiny matrix from its load to its store: one workgroup, all steps, X, A and P in shared memory.
-// There is so little work that it is done in 64 bits: with few directions (a rank of one or two) the
-// largest singular values of X_0 are near 1, the early steps' roundings enter in full, and fp32 sums
-// alone would cost a fp32 result five of its bits.
+// A matrix of few rows from its load to its store: one workgroup.  There is so little work that it is done in
+// 64 bits: with few directions (a rank of one or two) the largest singular values of X_0 are near 1, the early
+// steps' roundings enter in full, and fp32 sums alone would cost a fp32 result five of its bits.  In 64 bits
+// A = U U^T has all that the steps need: with B_0 = I and A_0 = A / |U|^2 a step is
+//   G = a I + b A + c A A;   B <- G B;   A <- G (G A)
+// (polynomials of the same A, so that they commute), n^3 each, and the result is s B U / |U|.  U is read
+// twice, in chunks that fit shared memory; the n x n products take blocks of 2 x 2 a thread, of which
+// shared memory's reads are what bounds them.  32 x 128: 53 us (with the steps on X itself, n n k each, 293); 256
+// of them 62 us; 4 x 4 12 us.
 __global__ __launch_bounds__(kTinyThreads) void k_tiny(Call c, Steps steps, const int32_t *list) {
-  __shared__ double x[kTinyElements], gram[kTinySide * kTinySide], poly[kTinySide * kTinySide];
-  __shared__ double sums[kTinyThreads / 64];
-  const int32_t at_matrix = list[blockIdx.x];
+  constexpr int kPitch = kTinySide;
+  __shared__ float x[kTinyElements + kTinySide];
+  __shared__ __align__(16) double matrices[5][kTinySide * kPitch];
+  double *const gram = matrices[0], *const g = matrices[1], *const turn = matrices[2];
+  double *b = matrices[3], *b_next = matrices[4];
+  const int at_matrix = list[blockIdx.x];
   const Matrix &m = c.matrices[at_matrix];
   const Addresses at = c.addresses[at_matrix];
-  const int n = m.n, k = m.k, count = n * k, tid = threadIdx.x, lane = tid & 63;
-  double sum = 0.;
-  for (int e = tid; e < count; e += kTinyThreads) {  // in the caller's order; x is n x k
-    const int cols = m.tall ? n : k, row = e / cols, col = e - row * cols;
-    const int64_t from = row * m.ld + col;
-    float u = load_input(c, at, from);
-    if (c.momentum) {
-      const float h = fmaf(c.mu, at.momentum[from], u);
-      at.momentum[from] = h;
-      u = c.nesterov ? fmaf(c.mu, h, u) : h;
+  const int n = m.n, k = m.k, tid = threadIdx.x, lane = tid & 63;
+  const int chunk = min(k, kTinyElements / n), pitch = chunk | 1;  // odd: a column's elements on different banks
+
+  // U from column k0 on, in the caller's order of memory
+  auto fill = [&](int k0, int width, bool once) {
+    for (int e = tid; e < n * width; e += kTinyThreads) {
+      const int i = m.tall ? e % n : e / width, q = m.tall ? e / n : e % width;
+      const int64_t from = m.tall ? (k0 + q) * m.ld + i : i * m.ld + k0 + q;
+      float u = load_input(c, at, from);
+      if (c.momentum) {
+        float h = at.momentum[from];
+        if (once) {
+          h = fmaf(c.mu, h, u);
+          at.momentum[from] = h;
+        }
+        u = c.nesterov ? fmaf(c.mu, h, u) : h;
+      }
+      x[i * pitch + q] = u;
     }
-    const double v = u;
-    x[m.tall ? col * k + row : e] = v;
-    sum = fma(v, v, sum);
-  }
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) sums[tid >> 6] = sum;
-  __syncthreads();
-  sum = 0.;
-  for (int w = 0; w < kTinyThreads / 64; ++w) sum += sums[w];
-  const double inverse = inverse_norm(sum, c.eps);
-  for (int e = tid; e < count; e += kTinyThreads) x[e] *= inverse;
-  __syncthreads();
+  };
+  for (int e = tid; e < n * kPitch; e += kTinyThreads) gram[e] = 0.;
   // a group of lanes per element of A: few elements have long rows, many have short ones
   const int log2 = n <= 4 ? 6 : n <= 12 ? 4 : 3, lanes = 1 << log2;
-  for (int t = 0; t < steps.count; ++t) {
-    for (int e0 = (tid >> log2); e0 < n * n; e0 += kTinyThreads >> log2) {
-      const int i = e0 / n, j = e0 - i * n;
-      double dot = 0.;
-      for (int q = lane & (lanes - 1); q < k; q += lanes) dot = fma(x[i * k + q], x[j * k + q], dot);
-      for (int o = lanes >> 1; o; o >>= 1) dot += __shfl_xor(dot, o);
-      if ((lane & (lanes - 1)) == 0) gram[e0] = dot;
-    }
+  for (int k0 = 0; k0 < k; k0 += chunk) {
+    const int width = min(chunk, k - k0);
+    fill(k0, width, true);
     __syncthreads();
-    const float *abc = steps.abc[t];
-    for (int e = tid; e < n * n; e += kTinyThreads) {
+    for (int e = tid >> log2; e < n * n; e += kTinyThreads >> log2) {
       const int i = e / n, j = e - i * n;
+      if (j > i) continue;
       double dot = 0.;
-      for (int q = 0; q < n; ++q) dot = fma(gram[i * n + q], gram[q * n + j], dot);
-      poly[e] = abc[1] * gram[e] + abc[2] * dot + (i == j ? static_cast<double>(abc[0]) : 0.);
-    }
-    __syncthreads();
-    for (int col = tid; col < k; col += kTinyThreads) {
-      double v[kTinySide];
-#pragma unroll
-      for (int q = 0; q < kTinySide; ++q) v[q] = q < n ? x[q * k + col] : 0.;
-      for (int i = 0; i < n; ++i) {
-        double dot = 0.;
-#pragma unroll
-        for (int q = 0; q < kTinySide; ++q)
-          if (q < n) dot = fma(poly[i * n + q], v[q], dot);
-        x[i * k + col] = dot;
+      for (int q = lane & (lanes - 1); q < width; q += lanes)
+        dot = fma(static_cast<double>(x[i * pitch + q]), static_cast<double>(x[j * pitch + q]), dot);
+      for (int o = lanes >> 1; o; o >>= 1) dot += __shfl_xor(dot, o);
+      if ((lane & (lanes - 1)) == 0) {
+        dot += gram[i * kPitch + j];
+        gram[i * kPitch + j] = dot;
+        gram[j * kPitch + i] = dot;
       }
     }
     __syncthreads();
   }
-  for (int e = tid; e < count; e += kTinyThreads) {
-    const int cols = m.tall ? n : k, row = e / cols, col = e - row * cols;
-    const float o = static_cast<float>(x[m.tall ? col * k + row : e] * static_cast<double>(m.scale));
-    const int64_t to = row * m.ld + col;
-    if (c.out_bf16)
-      static_cast<uint16_t *>(at.out)[to] = narrow_bf16(o);
-    else
-      static_cast<float *>(at.out)[to] = o;
+  double squares = 0.;
+  for (int i = 0; i < n; ++i) squares += gram[i * kPitch + i];
+  const double inverse = inverse_norm(squares, c.eps);
+  __syncthreads();
+  for (int e = tid; e < n * kPitch; e += kTinyThreads) gram[e] *= inverse * inverse;
+  __syncthreads();
+
+  const int half_n = (n + 1) / 2;  // past n: the padding, which reaches nothing else
+  auto product = [&](const double *left, const double *right, auto &&to) {
+    for (int block = tid; block < half_n * half_n; block += kTinyThreads) {
+      const int i = block / half_n * 2, j = (block - block / half_n * half_n) * 2;
+      double v[2][2] = {};
+#pragma unroll 4
+      for (int q = 0; q < n; ++q) {
+        const double r0 = right[q * kPitch + j], r1 = right[q * kPitch + j + 1];
+        const double l0 = left[i * kPitch + q], l1 = left[(i + 1) * kPitch + q];
+        v[0][0] = fma(l0, r0, v[0][0]);
+        v[0][1] = fma(l0, r1, v[0][1]);
+        v[1][0] = fma(l1, r0, v[1][0]);
+        v[1][1] = fma(l1, r1, v[1][1]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to(i + (e >> 1), j + (e & 1), v[e >> 1][e & 1]);
+    }
+  };
+  for (int t = 0; t < steps.count; ++t) {
+    const double a0 = steps.abc[t][0], b0 = steps.abc[t][1], c0 = steps.abc[t][2];
+    product(gram, gram, [&](int i, int j, double v) {
+      v = b0 * gram[i * kPitch + j] + c0 * v + (i == j ? a0 : 0.);
+      g[i * kPitch + j] = v;
+      if (t == 0) b[i * kPitch + j] = v;
+    });
+    __syncthreads();
+    if (t > 0) product(g, b, [&](int i, int j, double v) { b_next[i * kPitch + j] = v; });
+    if (t + 1 < steps.count) {
+      product(g, gram, [&](int i, int j, double v) { turn[i * kPitch + j] = v; });
+      __syncthreads();
+      product(g, turn, [&](int i, int j, double v) { gram[i * kPitch + j] = v; });
+    }
+    if (t > 0) {
+      double *const old = b;
+      b = b_next;
+      b_next = old;
+    }
+    __syncthreads();
+  }
+
+  const double factor = inverse * static_cast<double>(m.scale);
+  constexpr int kRows = 8;  // of a column, a thread
+  for (int k0 = 0; k0 < k; k0 += chunk) {
+    const int width = min(chunk, k - k0);
+    if (chunk < k) {
+      __syncthreads();
+      fill(k0, width, false);
+      __syncthreads();
+    }
+    for (int e = tid; e < (n + kRows - 1) / kRows * width; e += kTinyThreads) {
+      const int r0 = e / width * kRows, q = e - e / width * width;
+      double v[kRows] = {};
+      for (int j = 0; j < n; ++j) {
+        const double u = x[j * pitch + q];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) v[r] = fma(b[(r0 + r) * kPitch + j], u, v[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        if (r0 + r >= n) break;
+        const float o = static_cast<float>(v[r] * factor);
+        const int64_t to = m.tall ? (k0 + q) * m.ld + r0 + r : (r0 + r) * m.ld + k0 + q;
+        if (c.out_bf16)
+          static_cast<uint16_t *>(at.out)[to] = narrow_bf16(o);
+        else
+          static_cast<float *>(at.out)[to] = o;
+      }
+    }
   }
 }
 
@@ -900,7 +971,8 @@ __global__ __launch_bounds__(kTinyThreads) void k_tiny(Call c, Steps steps, cons
 // memory, in panels of 32 columns as the products' factors lie there.  A call is one launch instead of 17:
 // launches, each with its way to memory and back, are all that such a call takes.  N: 128, or 64 for pairs of
 // halves, and the side of the tiles of X that are replaced one after the other; 4 waves have a quarter of
-// a tile each.
+// a tile each.  128 x 96: 41 us where the launches of the products take 98; 64 x 64: 14 us.  A step takes 5.6 us at
+// 128, most of it the turns from accumulators to halves and back; the rest is the way of code that runs once.
 template <int N, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, int32_t first) {
   extern __shared__ half memory[];
