@@ -225,7 +225,8 @@ __device__ __forceinline__ int axis_of(const HeadArgs &a, int pair) {
   return (a.pair_axis[pair >> 4] >> (2 * (pair & 15))) & 3;
 }
 
-// cos and sin of a lane's pairs for token t.  `axis`: of the lane's pairs where they share one, else -1.
+// cos and sin of a lane's pairs for token t.  `axis`: of the lane's pairs where they share one, else -1 less all
+// of them, two bits each.
 template <int V>
 __device__ __forceinline__ void angles(const HeadArgs &a, const Place &p, int axis, int64_t t, float *c,
                                        float *s) {
@@ -245,16 +246,29 @@ __device__ __forceinline__ void angles(const HeadArgs &a, const Place &p, int ax
     }
     return;
   }
+  // every axis' position, then every pair's angle, each all on their way together
+  const uint32_t axes = -1 - axis;
+  int64_t at[SLOWMO_MAX_AXES], of[V];
+#pragma unroll
+  for (int i = 0; i < SLOWMO_MAX_AXES; ++i) at[i] = a.positions[min(i, a.axes - 1) * a.position_stride + t];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int64_t at = a.positions[axis_of(a, p.pair + i) * a.position_stride + t];
-    if (at >= 0 && at < a.table_rows) {
-      const float *row = a.table + at * a.rot + p.pair + i;
+    const uint32_t which = (axes >> (2 * i)) & 3;
+    of[i] = which < 2 ? (which ? at[1] : at[0]) : which == 2 ? at[2] : at[3];
+  }
+  if (a.table_rows > 0) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float *row = a.table + (of[i] >= 0 && of[i] < a.table_rows ? of[i] : 0) * a.rot + p.pair + i;
       c[i] = row[0];
       s[i] = row[half];
-    } else if (at != -1) {
-      c[i] = s[i] = __builtin_nanf("");
     }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (of[i] >= 0 && of[i] < a.table_rows) continue;
+    c[i] = of[i] == -1 ? 1.f : __builtin_nanf("");
+    s[i] = of[i] == -1 ? 0.f : __builtin_nanf("");
   }
 }
 
@@ -262,9 +276,14 @@ template <int V>
 __device__ __forceinline__ int shared_axis(const HeadArgs &a, const Place &p) {
   if (a.axes == 1 || !p.here || !p.turned) return 0;
   const int first = axis_of(a, p.pair);
-  for (int i = 1; i < V; ++i)
-    if (axis_of(a, p.pair + i) != first) return -1;
-  return first;
+  int all = first;
+  bool one = true;
+  for (int i = 1; i < V; ++i) {
+    const int axis = axis_of(a, p.pair + i);
+    one &= axis == first;
+    all |= axis << (2 * i);
+  }
+  return one ? first : -1 - all;
 }
 
 // Turns a lane's pairs by the angle (DIR 1) or back (DIR -1).  Past the rotated part c = 1, s = 0,
