@@ -573,8 +573,17 @@ Shape shape_of(const slowmo_head_config &c, const slowmo_heads *const *every, in
     }
     return true;
   };
+  // Whether a lane of v pairs would have several axes: its angles are then fetched pair by pair, so that lanes of 4
+  // pairs, of which fewer do, are taken (8 / 4, three axes: 30 000 tokens of 24 heads of 64, forward, 83 / 64 us;
+  // 43 869 of 16 of 80, backward, 158 / 159, without the norm 130 / 108).
+  auto mixes = [&](int v) {
+    if (!c.pair_axis || c.n_axes < 2) return false;
+    for (int i = 0; i < c.rotary_dim / 2; ++i)
+      if (c.pair_axis[i] != c.pair_axis[i / v * v]) return true;
+    return false;
+  };
   Shape s{};
-  s.v = fits(8) ? 8 : fits(4) ? 4 : 1;
+  s.v = fits(8) && !mixes(8) ? 8 : fits(4) ? 4 : 1;
   s.chunks = s.v > 1 ? c.head_dim / (2 * s.v) : (c.head_dim + 1) / 2;
   s.nch = s.v > 1 ? 1 : 4;
   while ((s.nch << s.lanes_log2) < s.chunks) ++s.lanes_log2;
