@@ -324,7 +324,7 @@ typedef short short8v __attribute__((ext_vector_type(8)));
 
 // UPDATE: P X by Update, else a symmetric product by Symmetric.
 template <int A, int B, int STAGES, bool UPDATE, bool SPLIT>
-__global__ __launch_bounds__(256, B == 256 || STAGES > 5 ? 1 : A == 256 || STAGES > 3 ? 2 : 3) void k_products(
+__global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_products(
     Call c, std::conditional_t<UPDATE, Update, Symmetric> st, const Tile *tiles) {
   extern __shared__ half ring[];
   constexpr int kBlocksA = A / 64, kBlocksB = B / 64;  // blocks of 32 x 32 along the sides of a wave's share
@@ -1308,11 +1308,11 @@ hipError_t launch_load(const Call &c, const Item *items, int32_t count, hipStrea
 
 namespace {
 
-// The kernel for a kind of tiles.  Of small ones, `count` decides how many workgroups share a CU: few leave
-// shared memory for a deeper ring, which hides more of memory's latency.  Block of the Transformer-big shapes,
-// 216 tiles a launch: 19.4 us with 9 stages, 22.2 with 3.
+// The kernel for a kind of tiles: rings as deep as the workgroups that share a CU leave room for.  (Of small
+// tiles in lists too short for that, rings of 9 stages took 1.01 to 1.06 of the time of 3: their longer code,
+// which comes from memory once a launch, costs what they hide.)
 template <bool UPDATE, typename F>
-hipError_t with_products(int kind, int32_t count, bool split, F &&f) {
+hipError_t with_products(int kind, bool split, F &&f) {
   auto sized = [&](auto a, auto b, auto stages) {
     constexpr int A = a(), B = b(), S = stages();
     constexpr size_t bytes = sizeof(half) * S * (A + B) * kDeep;
@@ -1320,12 +1320,11 @@ hipError_t with_products(int kind, int32_t count, bool split, F &&f) {
   };
   std::integral_constant<int, 128> small;
   std::integral_constant<int, 256> large;
+  std::integral_constant<int, 3> three;
   if (kind == kLarge) return sized(large, large, std::integral_constant<int, 4>{});
   if constexpr (UPDATE)
-    if (kind == kWide) return sized(large, small, std::integral_constant<int, 3>{});
-  if (count <= 256) return sized(small, small, std::integral_constant<int, 9>{});
-  if (count <= 512) return sized(small, small, std::integral_constant<int, 5>{});
-  return sized(small, small, std::integral_constant<int, 3>{});
+    if (kind == kWide) return sized(large, small, three);
+  return sized(small, small, three);
 }
 
 }  // namespace
@@ -1337,18 +1336,16 @@ hipError_t prepare_products(bool split) {
                                static_cast<int>(bytes));
   };
   for (int kind : {kSmall, kLarge, kWide}) {
-    for (int32_t count : {256, 512, 768}) {
-      hipError_t e = with_products<false>(kind, count, split, allow);
-      if (e == hipSuccess) e = with_products<true>(kind, count, split, allow);
-      if (e != hipSuccess) return e;
-    }
+    hipError_t e = with_products<false>(kind, split, allow);
+    if (e == hipSuccess) e = with_products<true>(kind, split, allow);
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
 hipError_t launch_symmetric(const Call &c, int kind, const Symmetric &p, const Tile *tiles, int32_t count,
                             bool split, hipStream_t s) {
-  return with_products<false>(kind, count, split, [&](auto *k, size_t bytes) {
+  return with_products<false>(kind, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
@@ -1356,7 +1353,7 @@ hipError_t launch_symmetric(const Call &c, int kind, const Symmetric &p, const T
 
 hipError_t launch_update(const Call &c, int kind, const Update &p, const Tile *tiles, int32_t count, bool split,
                          hipStream_t s) {
-  return with_products<true>(kind, count, split, [&](auto *k, size_t bytes) {
+  return with_products<true>(kind, split, [&](auto *k, size_t bytes) {
     k<<<count, 256, bytes, s>>>(c, p, tiles);
     return hipGetLastError();
   });
