@@ -138,6 +138,8 @@ typedef struct {
  *   X_0 = U / (|U|_F + eps)     (as n x k: transposed if it has more rows than columns)
  *   A = X X^T;   X <- a X + (b A + c A A) X,   `steps` times
  *   O = s X                     (in U's own orientation)
+ * U's bits count in full however small |U| is beside eps (unless a step's a is 0: X then shrinks with
+ * its cube and may come to zeros).
  * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN
  * everywhere.  A handle is made for a list of shapes and keeps a workspace:
  *   rows, cols : host, n_matrices entries each, >= 0 (an empty matrix is skipped),

@@ -67,7 +67,7 @@ struct Plan {
   Lists lists[kKinds];
   int64_t partial_sums = 0;   // floats
   int32_t tickets = 0;
-  size_t matrices_at = 0, addresses_at = 0, sums_at = 0, factor_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
+  size_t matrices_at = 0, addresses_at = 0, sums_at = 0, scales_at = 0, abc_at = 0, tiny_at = 0, sum_items_at = 0, load_at = 0,
          tiles_at[kKinds][3] = {}, tickets_at = 0, partial_at = 0, arena_at = 0, total = 0;
 };
 
@@ -342,7 +342,8 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.matrices_at = section(p.matrices.size() * sizeof(Matrix));
   p.addresses_at = section(p.matrices.size() * sizeof(Addresses));
   p.sums_at = section(p.sums.size() * sizeof(double));
-  p.factor_at = section(p.matrices.size() * sizeof(float));
+  p.scales_at = section(p.matrices.size() * kScales * sizeof(float));
+  p.abc_at = section(sizeof(Steps::abc));
   p.tiny_at = section(p.tiny.size() * sizeof(int32_t));
   p.sum_items_at = section(p.sums.size() * sizeof(Item));
   p.load_at = section(p.load.size() * sizeof(Item));
@@ -404,12 +405,12 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
     steps.a_power[t] = sa;
     steps.p_power[t] = sp;
     steps.carry[t] = carry;
-    symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f, t == 0});
+    symmetric({from, -1, -1, -1, -1, kA, sa / (kScaleX * kScaleX), 0.f, 0.f, 0.f, t == 0, t});
     symmetric({from, kA, kA, kA, -1, kP, static_cast<float>(c0 * sp / (double(sa) * sa)),
-               static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp), 0});
+               static_cast<float>(b0 * sp / sa), 0.f, static_cast<float>(two ? 0. : keep0 * sp), 0, -1});
     Op op{};
     op.update = true;
-    op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0), t == 0};
+    op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0), t == 0, kScales / 2 + t};
     double after = largest(most, [&](double s) { return s * (a0 + p0(s)); });
     if (two) {
       const double a1 = steps.abc[t + 1][0], b1 = steps.abc[t + 1][1], c1 = steps.abc[t + 1][2];
@@ -420,12 +421,12 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
       const float sa1 = power(largest(most, [&](double s) { return x1(s) * x1(s); }));
       const float sp1 = power(largest(most, p1));
       const float sq = power(largest(most, [&](double s) { return (a0 + p0(s)) * (a1 + p1(s)) - a0 * a1 + keep; }));
-      symmetric({from, kP, kA, kA, -1, kW, sw / (sp * sa), static_cast<float>(a0 * sw / sa), 0.f, 0.f, 0});
-      symmetric({from, kW, kP, kW, -1, kA, sa1 / (sw * sp), static_cast<float>(a0 * sa1 / sw), 0.f, 0.f, 0});
+      symmetric({from, kP, kA, kA, -1, kW, sw / (sp * sa), static_cast<float>(a0 * sw / sa), 0.f, 0.f, 0, -1});
+      symmetric({from, kW, kP, kW, -1, kA, sa1 / (sw * sp), static_cast<float>(a0 * sa1 / sw), 0.f, 0.f, 0, -1});
       symmetric({from, kA, kA, kA, -1, kW, static_cast<float>(c1 * sp1 / (double(sa1) * sa1)),
-                 static_cast<float>(b1 * sp1 / sa1), 0.f, 0.f, 0});
+                 static_cast<float>(b1 * sp1 / sa1), 0.f, 0.f, 0, -1});
       symmetric({from, kW, kP, kP, kW, kQ, sq / (sp1 * sp), static_cast<float>(a1 * sq / sp),
-                 static_cast<float>(a0 * sq / sp1), static_cast<float>(keep * sq), 0});
+                 static_cast<float>(a0 * sq / sp1), static_cast<float>(keep * sq), 0, -1});
       op.up.by = kQ;
       op.up.alpha = 1.f / sq;
       op.up.beta = static_cast<float>(a0 * a1);
@@ -563,6 +564,8 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
       put(p.tiles_at[which][1], p.lists[which].square, d.square, d.n_square);
       put(p.tiles_at[which][2], p.lists[which].update, d.update, d.n_update);
     }
+    if (e == hipSuccess)
+      e = hipMemcpyAsync(base + p.abc_at, h->steps.abc, sizeof(Steps::abc), hipMemcpyHostToDevice, s);
     if (e == hipSuccess) e = h->small ? prepare_small() : prepare_products(h->split);
     if (p.tickets && e == hipSuccess) e = hipMemsetAsync(base + p.tickets_at, 0, p.tickets * sizeof(uint32_t), s);
     const hipError_t waited = hipStreamSynchronize(s);  // the tables are in ordinary memory that ends here
@@ -570,7 +573,9 @@ slowmo_status slowmo_orth_create(slowmo_orth **out, const slowmo_orth_config *cf
     if (e != hipSuccess) return fail_thread_hip(e, "slowmo_orth_create");
     h->call.addresses = reinterpret_cast<Addresses *>(base + p.addresses_at);
     h->call.sums = reinterpret_cast<double *>(base + p.sums_at);
-    h->call.factor = reinterpret_cast<float *>(base + p.factor_at);
+    h->call.scales = reinterpret_cast<float *>(base + p.scales_at);
+    h->call.abc = reinterpret_cast<const float *>(base + p.abc_at);
+    h->call.steps = h->steps.count;
     h->call.tickets = reinterpret_cast<uint32_t *>(base + p.tickets_at);
     h->call.partial = reinterpret_cast<float *>(base + p.partial_at);
     h->call.arena = reinterpret_cast<_Float16 *>(base + p.arena_at);

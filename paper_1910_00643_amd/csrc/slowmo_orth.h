@@ -86,6 +86,9 @@ struct Few {
   Addresses at[kInline];
 };
 
+// Floats of a matrix in Call::scales: one for X X^T of each step, one for each update of X.
+constexpr int kScales = 2 * 16;
+
 struct Call {
   const Matrix *matrices;
   Addresses *addresses;
@@ -94,27 +97,31 @@ struct Call {
   float *partial;        // partial sums of tiles
   uint32_t *tickets;     // zero between calls
   float eps, mu;
-  float *factor;         // per matrix, where `exact`: X_0 over what is held in its place
+  float *scales;         // [matrix][kScales]: what a product of X is times for the powers of two that X is held
+                         // times while it is small and, where `exact`, for the rest of 1 / (|U| + eps) at the first step
+  const float *abc;      // the steps' coefficients
+  int32_t steps;
   int32_t in_bf16, out_bf16, momentum, nesterov;
   int32_t exact;         // X_0 is held as U times a power of two: 8 bits of bf16 fit a half whole, and no lower
                          // halves are needed
   int32_t buffers;       // n x n buffers of a matrix
 };
 
-// (`first_step`: of X_0, which Call::exact may have held without its factor.)
+// (`first_step`: of X_0, which Call::exact may have held without its factor; `scale`: the place in Call::scales,
+// -1: none.)
 // out = alpha * left * right (+ beta * first) (+ gamma * second) (+ delta on the diagonal), symmetric;
 // buffers are numbered, left = -1: X X^T.  The factors hold the buffers' powers of two.
 struct Symmetric {
   int32_t from, left, right, first, second, out;  // first, second: -1: none
   float alpha, beta, gamma, delta;
-  int32_t first_step;
+  int32_t first_step, scale;
 };
 
 // x[1 - from] = alpha * buffer[by] x[from] (+ beta * (hi + lo of x[from])); or the caller's result.
 struct Update {
   int32_t from, by, carry, carry_next, last;
   float alpha, beta;
-  int32_t first_step;
+  int32_t first_step, scale;
 };
 
 struct Steps {

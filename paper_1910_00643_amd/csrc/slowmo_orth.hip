@@ -155,6 +155,18 @@ __device__ __forceinline__ double inverse_norm(double squares, float eps) {
   return norm == 0. ? 0. : norm < 1.7e308 ? 1. / norm : __builtin_nan("");
 }
 
+// Where eps is large against |U|, X is small for the first steps: its elements times 2^kPowerX would lose their
+// bits to a half's smallest numbers.  X is then held times one more power of two, which brings the bound on its norm to
+// 0.5..1, where X_0's is with eps small.  The n x n matrices need none: beside a, which P is added to, their
+// smallest numbers do not count.
+__device__ __forceinline__ int lift(double bound) { return bound > 0. && bound < 0.5 ? -1 - ilogb(bound) : 0; }
+// The bound after a step; infinity or NaN: no lift.
+__device__ __forceinline__ double grown(double bound, const float *abc) {
+  const double b2 = bound * bound;
+  return bound * (fabs(static_cast<double>(abc[0])) +
+                  b2 * (fabs(static_cast<double>(abc[1])) + b2 * fabs(static_cast<double>(abc[2]))));
+}
+
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ void split8(const float *v, half8 &hi, half8 &lo) {
@@ -181,10 +193,24 @@ __global__ __launch_bounds__(256) void k_load(Call c, const Item *items) {
   __shared__ double shared[4];
   double squares = 0.;
   for (int i = threadIdx.x; i < m.sums; i += 256) squares += c.sums[m.first_sum + i];
-  const double by = inverse_norm(block_sum(squares, shared), c.eps);
-  const int power = by > 0. ? ilogb(by) : 0;  // apart: of subnormal matrices the inverse is no fp32 number
-  const float inverse = static_cast<float>(ldexp(by, -power));
-  if (c.exact && it.i == 0 && it.j == 0 && threadIdx.x == 0) c.factor[it.matrix] = inverse;
+  squares = block_sum(squares, shared);
+  const double by = inverse_norm(squares, c.eps), size = sqrt(squares) * by;
+  const int by_power = by > 0. ? ilogb(by) : 0;  // apart: of subnormal matrices the inverse is no fp32 number
+  const float inverse = static_cast<float>(ldexp(by, -by_power));
+  const int power = by_power + lift(size);
+  if (it.i == 0 && it.j == 0 && threadIdx.x == 0) {
+    float *gram = c.scales + static_cast<int64_t>(it.matrix) * kScales, *update = gram + kScales / 2;
+    const bool pairs = c.buffers == kSquares;
+    double bound = size;
+    for (int t = 0; t < c.steps;) {
+      const int here = lift(bound), first = t;
+      bound = grown(bound, c.abc + 3 * t++);
+      if (pairs && first == 0) bound = grown(bound, c.abc + 3 * t++);
+      const float rest = c.exact && first == 0 ? inverse : 1.f;
+      gram[first] = ldexpf(rest * rest, -2 * here);
+      update[first] = ldexpf(rest, (t < c.steps ? lift(bound) : 0) - here);
+    }
+  }
   auto walk = [&](auto *in) {
     const bool wide = whole_rows(in, m.ld), wide_m = whole_rows(at.momentum, m.ld);
     for (int patch = it.j; patch < it.j + kPatches && patch * kPatch < across; ++patch) {
@@ -334,6 +360,8 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_produc
   const Tile it = tiles[blockIdx.x];
   const Places places(it.np, it.kp, c.buffers);
   half *const arena = c.arena + it.at;
+  // asked for ahead of the products
+  const float held = st.scale >= 0 ? c.scales[static_cast<int64_t>(it.matrix) * kScales + st.scale] : 1.f;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave & 1, wb = wave >> 1;
   const int low = lane & 31, high = lane >> 5;
@@ -668,13 +696,7 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_produc
   }
   __syncthreads();
 
-  float alpha = st.alpha, beta = st.beta;
   const bool bare = st.first_step && c.exact;  // X_0 without its factor and lower halves
-  if (bare) {
-    const float factor = c.factor[it.matrix];
-    alpha *= UPDATE ? factor : factor * factor;
-    if constexpr (UPDATE) beta *= factor;
-  }
   const int ai = it.j * A + wa * kWideA, bi = it.i * B + wb * kWideB;  // first place along each factor
   if constexpr (UPDATE) {
     if (st.last) {
@@ -683,7 +705,9 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_produc
       float *stage = reinterpret_cast<float *>(ring) + wave * 32 * kPitch;
       const Matrix &m = c.matrices[it.matrix];
       const Addresses at = c.addresses[it.matrix];
-      const float scale = m.scale * alpha * (1.f / kScaleX);
+      // X's power of two by itself: together with the others it may be below fp32's numbers
+      const bool lifted = held > 0.f && held < 1.f;
+      const float lower = lifted ? held : 1.f, scale = m.scale * (st.alpha * (lifted ? 1.f : held)) * (1.f / kScaleX);
       auto leave = [&](auto wide, int row0, int rows, int col0, int cols) {
         constexpr int kLanes = decltype(wide)::value / 8, kRows = 64 / kLanes;
         const int sub = lane / kLanes, c8 = (lane % kLanes) * 8;
@@ -691,7 +715,8 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_produc
         for (int r = 0; r < 32; r += kRows) {
           const f32x4 p = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8),
                       q = *reinterpret_cast<const f32x4 *>(stage + (r + sub) * kPitch + c8 + 4);
-          const float v[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+          const float v[8] = {p[0] * lower, p[1] * lower, p[2] * lower, p[3] * lower,
+                              q[0] * lower, q[1] * lower, q[2] * lower, q[3] * lower};
           write_out(c, at, m.ld, row0 + r + sub, rows, col0 + c8, cols, v, scale);
         }
       };
@@ -721,6 +746,7 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : A == 256 ? 2 : 3) void k_produc
     }
   }
 
+  const float alpha = st.alpha * held, beta = UPDATE ? st.beta * held : st.beta;
   // A block of 32 x 32 is 2 KB in one piece, row `low` of it 64 bytes of which a lane holds four times 8.
   // It passes through shared memory to leave in stores of 1 KB; read turned there, it is its
   // mirror image's block.  Pieces of 16 bytes are placed as the factors' are.
@@ -1000,6 +1026,7 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
   double squares = 0.;
   float inverse = 0.f;  // times 2^power: of subnormal matrices it is no fp32 number
   int power = 0;
+  double size = 0.;     // of X_0
   // some units at a time, so that their loads are on their way together
   auto look = [&](auto *in, auto whole, int pass) {
     constexpr int kSome = decltype(whole)::value ? 4 : 1;
@@ -1062,10 +1089,12 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
       *reinterpret_cast<half8 *>(x[0] + q * 8) = none;
       *reinterpret_cast<half8 *>(x[1] + q * 8) = none;
     }
-    const double by = inverse_norm(block_sum(squares, shared), c.eps);
+    squares = block_sum(squares, shared);
+    const double by = inverse_norm(squares, c.eps);
+    size = sqrt(squares) * by;
     power = by > 0. ? ilogb(by) : 0;
     inverse = static_cast<float>(ldexp(by, -power));
-    power += kPowerX;
+    power += kPowerX + lift(size);
     look(in, whole, 1);
   };
   auto by_rows = [&](auto *in) {
@@ -1163,6 +1192,10 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
     // of pairs of halves always: with a on P's diagonal, results of matrices of deficient rank were 1.3 times as
     // far off (64 x 40, rank 5: 1.6e-5 to 2.1e-5)
     const bool carry = SPLIT || steps.carry[s];
+    // the powers of two that X is held times, here and after the step
+    const int here = lift(size);
+    size = grown(size, steps.abc[s]);
+    const float lowered = ldexpf(1.f, -2 * here), on = ldexpf(1.f, lift(size) - here);
     clear();
 #pragma unroll
     for (int pass = kFirstPass; pass < 3; ++pass)
@@ -1173,7 +1206,7 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
     each_four([&](int xb, int yb, int g) {
       float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (sa / (kScaleX * kScaleX));
+      for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (sa / (kScaleX * kScaleX) * lowered);
       keep(gram, mine(0, xb, yb, g), v);
     });
     __syncthreads();
@@ -1214,12 +1247,12 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
         const int pos = mine(t, xb, yb, g);
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (1.f / sp);
+        for (int e = 0; e < 4; ++e) v[e] = acc[xb][yb][4 * g + e] * (on / sp);
         if (carry) {
           const half4 h = *reinterpret_cast<const half4 *>(x[0] + pos);
           const half4 l = SPLIT ? *reinterpret_cast<const half4 *>(x[1] + pos) : lower[t][xb][yb][g];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = fmaf(a0, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e]);
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(a0 * on, static_cast<float>(h[e]) + static_cast<float>(l[e]), v[e]);
         }
         lower[t][xb][yb][g] = keep(x, pos, v);
       });
@@ -1227,6 +1260,7 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
     __syncthreads();
   }
   // The result, hi + lo, in the caller's rows.
+  const float lower_all = ldexpf(1.f, -lift(size));
   if constexpr (!SPLIT) {
 #pragma unroll
     for (int t = 0; t < kMostTiles; ++t)
@@ -1249,6 +1283,8 @@ __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, 
         v[e] = static_cast<float>(x[0][from]) + static_cast<float>(x[1][from]);
       }
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= lower_all;
     write_out(c, at, m.ld, row, rows, col, cols, v, m.scale * (1.f / kScaleX));
   }
 }
