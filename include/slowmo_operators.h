@@ -128,8 +128,10 @@ typedef struct {
   int32_t scale;      /* slowmo_orth_scale */
   float eps;          /* added to the Frobenius norm, >= 0 */
   const float *coefficients; /* host, [steps][3]: a, b, c of every step, finite; NULL: (3.4445, -4.7750, 2.0315).
-                                Refused if some singular value of 0..1 comes to 7.5 or more in a step (8 less a
-                                margin): X's elements have to stay in a half's range */
+                                Refused if some singular value of 0..1 comes to 7.5 or more after a step, where each
+                                step from s adds up to (|a| s + |b| s^3 + |c| s^5) / 1024 for rounding: X's elements
+                                have to stay in a half's range.  (Steps that are steep at the largest values that
+                                reach them need a safety factor, as the roundings grow there) */
 } slowmo_orth_config;
 
 /*

@@ -373,6 +373,54 @@ float power(double most) {
   return static_cast<float>(std::min(8192., std::exp2(std::floor(std::log2(32768. / std::max(most, 1e-30))))));
 }
 
+// The largest singular value of X in front of each step and after the last, and whether all stay under 7.5 (halves
+// times 2^kPowerX reach 8).  Followed in 4096 pieces of 0..1, each as the interval that a step's polynomial takes it
+// to, widened for rounding by kRounding of |a| s + |b| s^3 + |c| s^5.  One interval, or 2 % of each value for
+// rounding, refuses schedules of steps that are steep past the values that arrive there, as fast ones are:
+// quintics that are each the best approximation of 1 on what the one before leaves of 1e-3..1 reach 1.99 and, divided by
+// a safety factor of 1.01, stay at 2.00 here.  Without the factor they are refused, rightly: roundings at the steep end
+// grow 12-fold a step, and matrices of equal elements came to infinity (halves) and 249 (pairs) on the CPU.
+constexpr double kMostValue = 7.5, kRounding = 1. / 1024;
+
+bool follow(const Steps &steps, double (&most)[SLOWMO_MAX_ORTH_STEPS + 1]) {
+  constexpr int kPieces = 4096;
+  struct Interval {
+    double lo, hi;
+  };
+  std::vector<Interval> v(kPieces);
+  for (int i = 0; i < kPieces; ++i) v[i] = {i / double(kPieces), (i + 1) / double(kPieces)};
+  most[0] = 1.;
+  for (int32_t t = 0; t < steps.count; ++t) {
+    const double a = steps.abc[t][0], b = steps.abc[t][1], c = steps.abc[t][2];
+    auto f = [=](double s) { return s * (a + s * s * (b + c * s * s)); };
+    // where the slope a + 3 b s^2 + 5 c s^4 is zero
+    double turns[4], square[2] = {-1., -1.};
+    const double root = 9. * b * b - 20. * a * c;
+    if (root >= 0.) {
+      const double q = -0.5 * (3. * b + std::copysign(std::sqrt(root), b));
+      if (c != 0.) square[0] = q / (5. * c);
+      if (q != 0.) square[1] = a / q;
+    }
+    for (int i = 0; i < 2; ++i) {
+      turns[2 * i] = square[i] > 0. ? std::sqrt(square[i]) : 0.;
+      turns[2 * i + 1] = -turns[2 * i];
+    }
+    double largest = 0.;
+    for (Interval &p : v) {
+      const double at = std::max(std::fabs(p.lo), std::fabs(p.hi)), square = at * at;
+      const double wide = kRounding * at * (std::fabs(a) + square * (std::fabs(b) + square * std::fabs(c)));
+      double lo = std::min(f(p.lo), f(p.hi)), hi = std::max(f(p.lo), f(p.hi));
+      for (double s : turns)
+        if (s > p.lo && s < p.hi) lo = std::min(lo, f(s)), hi = std::max(hi, f(s));
+      p = {lo - wide, hi + wide};
+      largest = std::max({largest, -p.lo, p.hi});
+    }
+    if (!(largest < kMostValue)) return false;
+    most[t + 1] = std::max(largest, 1e-3);
+  }
+  return true;
+}
+
 // The steps as launches.  One step is A = X X^T, P = b A + c A A, X <- a X + P X.  Where X is much
 // longer than wide, the first two steps are one: with P0 from A0, the second step's A is
 // (a0 + P0)^2 A0, a product of n x n matrices too, and X <- a0 a1 X + Q X with
@@ -381,7 +429,7 @@ float power(double most) {
 // again.)  Only the first two: A's roundings reach the second step's A a0^2 = 12 times as large, which shows
 // once singular values are near 1.  512 x 2048 against 64 bits, products of halves / of pairs: one by
 // one 0.8e-3 / 2.2e-6, first two 0.8e-3 / 1.8e-6, the next two as well 3.3e-3 / 3.8e-6.
-// Leaves the powers of two with the steps.  Returns an empty program if the coefficients let X outgrow a half.
+// Leaves the powers of two with the steps.  Returns an empty program if the coefficients let X outgrow a half (follow()).
 std::vector<Op> program(Steps &steps, bool pairs, bool split) {
   std::vector<Op> ops;
   enum { kA, kP, kW, kQ };
@@ -390,10 +438,12 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
     op.symmetric = s;
     ops.push_back(op);
   };
-  double most = 1.;   // of the singular values
+  double bounds[SLOWMO_MAX_ORTH_STEPS + 1];
+  if (!follow(steps, bounds)) return {};
   int32_t from = 0;
   for (int32_t t = 0; t < steps.count;) {
     const bool two = pairs && t == 0;
+    const double most = bounds[t];
     const double a0 = steps.abc[t][0], b0 = steps.abc[t][1], c0 = steps.abc[t][2];
     auto p0 = [=](double s) { return b0 * s * s + c0 * s * s * s * s; };
     // Of single halves the last two steps' a goes to P's diagonal; the others' X enters as hi + lo.
@@ -411,7 +461,6 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
     Op op{};
     op.update = true;
     op.up = {from, kP, carry, 0, 0, 1.f / sp, static_cast<float>(a0), t == 0, kScales / 2 + t};
-    double after = largest(most, [&](double s) { return s * (a0 + p0(s)); });
     if (two) {
       const double a1 = steps.abc[t + 1][0], b1 = steps.abc[t + 1][1], c1 = steps.abc[t + 1][2];
       auto x1 = [=](double s) { return s * (a0 + p0(s)); };
@@ -430,11 +479,7 @@ std::vector<Op> program(Steps &steps, bool pairs, bool split) {
       op.up.by = kQ;
       op.up.alpha = 1.f / sq;
       op.up.beta = static_cast<float>(a0 * a1);
-      if (after >= 7.9) return {};
-      after = largest(most, [&](double s) { return x1(s) * (a1 + p1(s)); });
     }
-    if (after >= 7.9) return {};
-    most = std::max(after, 1e-3);
     ops.push_back(op);
     from = 1 - from;
     t += two ? 2 : 1;
@@ -508,7 +553,7 @@ static const char *refusal(const slowmo_orth_config *cfg, int32_t n_matrices, co
                            const int64_t *cols, const int64_t *ld) {
   if (const char *bad = check(cfg, n_matrices, rows, cols, ld)) return bad;
   Steps steps = steps_of(*cfg);
-  if (program(steps, false, false).empty()) return "the coefficients let singular values grow past 7";
+  if (program(steps, false, false).empty()) return "the coefficients let singular values grow to 7.5";
   return nullptr;
 }
 
