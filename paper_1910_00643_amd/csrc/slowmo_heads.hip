@@ -27,6 +27,7 @@ namespace {
 constexpr int kWaves = 4;                      // waves per workgroup
 constexpr int kThreads = 64 * kWaves;
 constexpr int kPairs = SLOWMO_MAX_HEAD_DIM / 2;
+constexpr int kMostBlocks = 1 << 23;           // workgroups of a launch: a grid has less than 2^32 threads
 constexpr int kFill = 8192;                    // waves that fill the card: 256 CUs, 8 waves per SIMD
 constexpr int kWalks = 768;                    // workgroups of a backward pass: all run at once, 3 per CU
 
@@ -47,6 +48,7 @@ struct Side {
 
 struct HeadArgs {
   int64_t tokens;
+  int64_t first;         // forward: the unit that this launch begins with
   const float *table;
   const int64_t *positions;
   int64_t table_rows, position_stride;
@@ -362,7 +364,7 @@ __device__ __forceinline__ Row row_of(const HeadArgs &a, const Side &s, int64_t 
 template <typename T, int V, int NCH, bool INTER, bool NORM, bool NT>
 __global__ __launch_bounds__(kThreads) void k_head_forward(HeadArgs a) {
   const int lane = threadIdx.x & 63;
-  int64_t unit = static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t unit = a.first + static_cast<int64_t>(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool key = unit >= a.side[0].units;
   const Side &s = a.side[key];
   if (key) unit -= a.side[0].units;
@@ -792,13 +794,15 @@ slowmo_status slowmo_head_norm_rotary(const slowmo_head_config *cfg, int64_t tok
     a.side[1].y = rows_of(*k_out);
     a.slots = k_slots;
     a.slot_rows = k_rows;
-    const int64_t blocks = (a.side[0].units + a.side[1].units + kWaves - 1) / kWaves;
-    if (blocks > INT32_MAX) return fail_thread(SLOWMO_ERR_ARG, "too many tokens for one call");
+    const int64_t units = a.side[0].units + a.side[1].units;
     hipError_t e = hipSuccess;
     dispatch(*cfg, s, streams(a, *cfg, 2), [&](auto zero, auto v, auto nch, auto inter, auto norm, auto nt) {
-      k_head_forward<decltype(zero), v(), nch(), inter(), norm(), nt()>
-          <<<static_cast<uint32_t>(blocks), kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
-      e = hipGetLastError();
+      for (; a.first < units && e == hipSuccess; a.first += static_cast<int64_t>(kMostBlocks) * kWaves) {
+        const int64_t blocks = std::min<int64_t>(kMostBlocks, (units - a.first + kWaves - 1) / kWaves);
+        k_head_forward<decltype(zero), v(), nch(), inter(), norm(), nt()>
+            <<<static_cast<uint32_t>(blocks), kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+        e = hipGetLastError();
+      }
     });
     return e == hipSuccess ? SLOWMO_OK : fail_thread_hip(e, "slowmo_head_norm_rotary");
   });
