@@ -54,7 +54,7 @@ typedef struct {
   const int64_t *positions; /* device, [n_axes][tokens]: row of the table for each axis and token; -1: the
                                axis's pairs are not turned.  Any other place outside the table gives
                                NaN in the axis's pairs and nothing else */
-  int64_t position_stride;  /* elements from one axis to the next */
+  int64_t position_stride;  /* elements from one axis to the next, >= tokens; 0: all axes have the same positions */
 } slowmo_head_config;
 
 /* A [tokens][heads][D] array; the D elements of a head are contiguous.  Strides in

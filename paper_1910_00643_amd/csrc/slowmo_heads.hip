@@ -613,8 +613,9 @@ const char *check(const slowmo_head_config *c, int64_t tokens) {
     if (c->table_rows < 0 || c->table_rows > (int64_t(1) << 40)) return "table_rows must be in 0..2^40";
     if (tokens && c->table_rows && !c->table) return "table is NULL";
     if (tokens && !c->positions) return "positions is NULL";
-    if (c->position_stride < 0 || (c->n_axes > 1 && c->position_stride < tokens))
-      return "position_stride must be >= tokens";
+    if (c->position_stride < 0 || c->position_stride > (int64_t(1) << 40) ||
+        (c->n_axes > 1 && c->position_stride && c->position_stride < tokens))
+      return "position_stride must be 0 or in tokens..2^40";
   }
   return nullptr;
 }

@@ -107,7 +107,8 @@ class HeadNormRotary:
 
     Queries and keys are [tokens, heads, head_dim] (or with more leading dimensions that
     flatten without a copy), each head's elements contiguous, other strides free.
-    A handle is not thread-safe.  `positions` is int64, [tokens] or [axes, tokens]: rows of the table, -1 for no turn."""
+    A handle is not thread-safe.  `positions` is int64, [tokens] or [axes, tokens]
+    (expanded, where all axes have the same): rows of the table, -1 for no turn."""
 
     def __init__(self, head_dim: int, table: Optional[torch.Tensor] = None, *, dtype: str = "bf16",
                  norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
