@@ -162,7 +162,8 @@ class HeadNormRotary:
         if self.pairs:
             shape, st = positions.shape, positions.stride()
             assert positions.dtype is torch.int64 and positions.is_cuda
-            assert shape[-1] == tokens and (tokens < 2 or st[-1] == 1)
+            assert 0 < len(shape) < 3 and shape[-1] == tokens and (tokens < 2 or st[-1] == 1), \
+                "positions: [tokens] or [axes, tokens], an axis's tokens contiguous"
             if len(shape) == 2 and shape[0] != 1:
                 cfg.n_axes, cfg.position_stride = shape[0], st[0]
             else:
