@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -94,6 +95,15 @@ def rotary_table(rows: int, pairs, base: float = 10000.0, device="cuda") -> torc
     return torch.stack([angle.cos(), angle.sin()], 1).float().contiguous()
 
 
+class _Arguments(threading.local):
+    """The structures of a handle's calls, for each thread its own: ctypes lets go of the interpreter in a call."""
+
+    def __init__(self, config):
+        self.cfg = slowmo_head_config(**config)
+        self.rows = (slowmo_heads * 6)()
+        self.refs = [C.byref(r) for r in self.rows]
+
+
 class HeadNormRotary:
     """The norm of queries and keys for each head and the position rotation.
 
@@ -107,8 +117,8 @@ class HeadNormRotary:
 
     Queries and keys are [tokens, heads, head_dim] (or with more leading dimensions that
     flatten without a copy), each head's elements contiguous, other strides free.
-    A handle is not thread-safe.  `positions` is int64, [tokens] or [axes, tokens]
-    (expanded, where all axes have the same): rows of the table, -1 for no turn."""
+    `positions` is int64, [tokens] or [axes, tokens] (expanded, where all axes have the same): rows of the
+    table, -1 for no turn.  A handle may serve several threads."""
 
     def __init__(self, head_dim: int, table: Optional[torch.Tensor] = None, *, dtype: str = "bf16",
                  norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
@@ -122,14 +132,12 @@ class HeadNormRotary:
         self.table, self.dtype, self.norm = table, _TORCH_GRAD[dtype], bool(norm)
         self.head_dim, self.pairs = int(head_dim), pairs
         self._axis = None if pair_axis is None else (C.c_uint8 * max(pairs, 1))(*pair_axis)
-        self._cfg = slowmo_head_config(
+        self._args = _Arguments(dict(
             dtype=_DTYPE[dtype], head_dim=head_dim, rotary_dim=2 * pairs, interleaved=int(interleaved),
             norm=int(norm), eps=eps, n_axes=1,
             pair_axis=C.addressof(self._axis) if self._axis is not None else None,
             table=table.data_ptr() if table is not None else None,
-            table_rows=table.shape[0] if table is not None else 0)
-        self._rows = (slowmo_heads * 6)()
-        self._refs = [C.byref(r) for r in self._rows]
+            table_rows=table.shape[0] if table is not None else 0))
 
     # A call on few tokens ends before the next one is issued, so that the time between two launches is what
     # it takes: checks and addresses go straight into structures that the handle keeps, 10.8 -> 9.9 us a
@@ -157,7 +165,7 @@ class HeadNormRotary:
         return w.data_ptr()
 
     def _config(self, positions, tokens, wq, wk) -> slowmo_head_config:
-        cfg = self._cfg                # one per handle: only what a call brings is written
+        cfg = self._args.cfg           # only what a call brings is written
         cfg.q_weight, cfg.k_weight = self._weight(wq), self._weight(wk)
         if self.pairs:
             shape, st = positions.shape, positions.stride()
@@ -205,8 +213,8 @@ class HeadNormRotary:
                 slots, rows = k_slots.data_ptr() or None, yk.shape[0]
             at_yk = self._row(yk, "k_out")
         cfg = self._config(positions, tokens, q_weight, k_weight)
-        _HEADS4.pack_into(self._rows, 0, *at_q, *at_k, *at_yq, *at_yk)
-        r = self._refs
+        _HEADS4.pack_into(self._args.rows, 0, *at_q, *at_k, *at_yq, *at_yk)
+        r = self._args.refs
         status = lib().slowmo_head_norm_rotary(cfg, tokens, r[0], r[1], r[2], r[3], slots, rows,
                                                _raw_stream(q.device) or None)
         if status:
@@ -231,8 +239,8 @@ class HeadNormRotary:
             dwk = torch.empty_like(dwq)
             nbytes = lib().slowmo_head_backward_bytes(cfg, tokens, at_q[1], at_k[1])
             space = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        _HEADS6.pack_into(self._rows, 0, *self._row(gq, "gq"), *self._row(gk, "gk"), *at_q, *at_k, *at_dq, *at_dk)
-        r = self._refs
+        _HEADS6.pack_into(self._args.rows, 0, *self._row(gq, "gq"), *self._row(gk, "gk"), *at_q, *at_k, *at_dq, *at_dk)
+        r = self._args.refs
         status = lib().slowmo_head_norm_rotary_backward(
             cfg, tokens, r[0], r[1], r[2], r[3], r[4], r[5],
             dwq.data_ptr() if self.norm else None, dwk.data_ptr() if self.norm else None,

@@ -51,3 +51,35 @@ def test_positions_of_other_shapes_are_refused(shape):
 def test_positions_of_one_axis_and_of_several(shape, axes, stride):
     cfg = _op()._config(Stand(64, *shape, dtype=torch.int64), 12, None, None)
     assert (cfg.n_axes, cfg.position_stride, cfg.positions) == (axes, stride, 64)
+
+
+def test_two_threads_on_one_handle(monkeypatch):
+    """The library lets another thread run while it is called: each call keeps its own addresses."""
+    seen, inside, done = {}, threading.Event(), threading.Event()
+
+    class Library:
+        def slowmo_head_norm_rotary(self, cfg, tokens, q, k, q_out, k_out, slots, rows, stream):
+            if threading.current_thread().name == "first":
+                inside.set()
+                assert done.wait(20)
+            seen[threading.current_thread().name] = (cfg.positions, tokens, *[r._obj.data for r in (q, k, q_out, k_out)])
+            return 0
+
+    monkeypatch.setattr(O, "lib", Library)
+    monkeypatch.setattr(O, "_raw_stream", lambda device: 0)
+    op = _op()
+
+    def call(base, tokens):
+        q, k, yq, yk = (Stand(base + 4096 * i, tokens, 2, 16) for i in range(4))
+        op.forward(q, k, Stand(base + 64, tokens, dtype=torch.int64), q_out=yq, k_out=yk)
+
+    first = threading.Thread(target=call, args=(1 << 20, 5), name="first")
+    first.start()
+    assert inside.wait(20)
+    second = threading.Thread(target=call, args=(2 << 20, 7), name="second")
+    second.start()
+    second.join(20)
+    done.set()
+    first.join(20)
+    for name, base, tokens in (("first", 1 << 20, 5), ("second", 2 << 20, 7)):
+        assert seen[name] == (base + 64, tokens, *[base + 4096 * i for i in range(4)])
