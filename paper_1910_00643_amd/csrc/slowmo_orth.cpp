@@ -254,7 +254,7 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   }
   // Small matrices alone (beside tiny ones): one workgroup each.
   int32_t side = split ? kSmallSideSplit : kSmallSide, small = 0;
-  for (const Matrix &m : p.matrices) small += m.n <= side && m.k <= kSmallLength;
+  for (const Matrix &m : p.matrices) small += m.tiny || (m.n <= side && m.k <= kSmallLength);
   p.small = p.tiny.size() < p.matrices.size() && small == static_cast<int32_t>(p.matrices.size());
   if (p.small)
     for (auto &list : of) list.clear();
