@@ -46,7 +46,7 @@ typedef struct {
   float eps;           /* >= 0 */
   int32_t n_axes;      /* 1..SLOWMO_MAX_AXES */
   const uint8_t *pair_axis; /* host: the axis (0..n_axes-1) of each of the R/2 pairs; NULL: axis 0 */
-  const float *q_weight;    /* device, D floats; NULL: ones */
+  const float *q_weight;    /* device, D floats; NULL: ones (must be NULL without norm) */
   const float *k_weight;
   const float *table;       /* device, [table_rows][2][R/2]: cos, then sin, of the angle of a pair at a
                                position; 4-byte aligned */

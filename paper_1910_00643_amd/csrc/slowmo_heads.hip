@@ -603,6 +603,7 @@ const char *check(const slowmo_head_config *c, int64_t tokens) {
     return "rotary_dim must be even and in 0..head_dim";
   if (c->interleaved != 0 && c->interleaved != 1) return "interleaved must be 0 or 1";
   if (c->norm != 0 && c->norm != 1) return "norm must be 0 or 1";
+  if (!c->norm && (c->q_weight || c->k_weight)) return "without the norm there are no weights";
   if (!(std::isfinite(c->eps) && c->eps >= 0.f)) return "eps must be finite and >= 0";
   if (c->n_axes < 1 || c->n_axes > SLOWMO_MAX_AXES) return "n_axes must be in 1..SLOWMO_MAX_AXES";
   if (tokens < 0 || tokens > (int64_t(1) << 31)) return "tokens must be in 0..2^31";

@@ -111,7 +111,8 @@ class HeadNormRotary:
     table       -- rotary_table(...), [rows, 2, pairs] fp32 on the GPU: the first 2 * pairs elements
                    of a head are turned; None: no rotation
     dtype       -- "bf16" or "f32": of queries, keys, results and their gradients
-    norm, eps   -- whether to divide by sqrt(mean(x^2) + eps) and multiply by the weights
+    norm, eps   -- whether to divide by sqrt(mean(x^2) + eps) and multiply by the weights (without it
+                   a call has none)
     interleaved -- pair i is elements (2i, 2i + 1); else (i, i + pairs)
     pair_axis   -- the axis of positions that each pair belongs to; None: one axis
 

@@ -1,0 +1,16 @@
+"""More arguments that the heads' C entry points refuse, without a GPU."""
+import pytest
+
+import paper_1910_00643_amd as P
+from paper_1910_00643_amd import binding as B
+
+from test_heads_host import _backward, _config, _forward
+
+
+@pytest.mark.parametrize("weight", ["q_weight", "k_weight"])
+def test_weights_without_the_norm(weight):
+    """They were ignored without a word."""
+    assert _forward(_config(norm=0, **{weight: 0x700000})) == B.SLOWMO_ERR_ARG
+    assert "weights" in P.slowmo_last_error(None)
+    assert _backward(_config(norm=0, **{weight: 0x700000}), dwq=None) == B.SLOWMO_ERR_ARG
+    assert "weights" in P.slowmo_last_error(None)
