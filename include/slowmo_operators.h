@@ -58,7 +58,7 @@ typedef struct {
 } slowmo_head_config;
 
 /* A [tokens][heads][D] array; the D elements of a head are contiguous.  Strides in
- * elements, >= 0; data aligned to its element size. */
+ * elements, >= 0, and no array longer than 2^50 elements; data aligned to its element size. */
 typedef struct {
   void *data;      /* device; may be NULL if heads == 0 */
   int32_t heads;   /* >= 0 */

@@ -627,6 +627,10 @@ const char *check_heads(const slowmo_heads *h, int64_t tokens) {
   if (h->token_stride < 0 || h->head_stride < 0 || h->token_stride > (int64_t(1) << 40) ||
       h->head_stride > (int64_t(1) << 40))
     return "strides must be in 0..2^40";
+  // so that no offset or extent passes 64 bits
+  if (static_cast<double>(h->token_stride) * static_cast<double>(std::max<int64_t>(tokens - 1, 0)) +
+          static_cast<double>(h->head_stride) * std::max(h->heads - 1, 0) > std::exp2(50.))
+    return "an array reaches past 2^50 elements";
   if (h->heads && tokens && !h->data) return "data is NULL";
   return nullptr;
 }
