@@ -130,6 +130,7 @@ class HeadNormRotary:
             assert table.dim() == 3 and table.shape[1] == 2
             pairs = table.shape[2]
         assert pair_axis is None or len(pair_axis) == pairs
+        assert pair_axis is None or all(0 <= a < SLOWMO_MAX_AXES for a in pair_axis), "pair_axis: 0..3 for each pair"
         self.table, self.dtype, self.norm = table, _TORCH_GRAD[dtype], bool(norm)
         self.head_dim, self.pairs = int(head_dim), pairs
         self._axis = None if pair_axis is None else (C.c_uint8 * max(pairs, 1))(*pair_axis)

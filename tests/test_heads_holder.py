@@ -83,3 +83,12 @@ def test_two_threads_on_one_handle(monkeypatch):
     first.join(20)
     for name, base, tokens in (("first", 1 << 20, 5), ("second", 2 << 20, 7)):
         assert seen[name] == (base + 64, tokens, *[base + 4096 * i for i in range(4)])
+
+
+@pytest.mark.parametrize("axis", [256, 4, -1, -256])
+def test_axes_that_are_none_are_refused(axis):
+    """256 went into 8 bits as axis 0."""
+    table = Stand(1 << 12, 5, 2, 2)
+    O.HeadNormRotary(16, table, pair_axis=[0, 3])
+    with pytest.raises(AssertionError):
+        O.HeadNormRotary(16, table, pair_axis=[0, axis])
