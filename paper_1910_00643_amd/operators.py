@@ -319,6 +319,7 @@ class Orthogonalizer:
             raise B.SlowMoError(B.SLOWMO_ERR_ARG, B.slowmo_last_error(None))
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.device = self.workspace.device       # with its number, whichever was the current one
             self.handle = C.c_void_p()
             _check(lib().slowmo_orth_create(C.byref(self.handle), cfg, self.n_matrices, *arrays,
                                             self.workspace.data_ptr(), nbytes,
@@ -330,8 +331,8 @@ class Orthogonalizer:
             raise ValueError(f"{len(self.shapes)} tensors wanted, {len(tensors)} given")
         flat = []
         for t, s, ld in zip(tensors, self.shapes, self.ld):
-            if tuple(t.shape) != s or t.dtype != dtype or t.device.type != "cuda":
-                raise ValueError(f"a {dtype} tensor of shape {s} on the GPU is wanted: got {tuple(t.shape)}, "
+            if tuple(t.shape) != s or t.dtype != dtype or t.device != self.device:
+                raise ValueError(f"a {dtype} tensor of shape {s} on {self.device} is wanted: got {tuple(t.shape)}, "
                                  f"{t.dtype}, {t.device}")
             st = t.stride()
             if t.numel() and (s[-1] > 1 and st[-1] != 1 or s[-2] > 1 and st[-2] != ld):
