@@ -8,6 +8,13 @@ torch = pytest.importorskip("torch")
 DEV = "cuda:0"
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _memory_goes_back():
+    """Later tests look at allocations of their own."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def test_more_tokens_than_a_grid_has_waves():
     import paper_1910_00643_amd as P
     tokens, dim, rows = (1 << 26) + 1001, 512, 97

@@ -14,6 +14,13 @@ from test_gpu_heads import DEV, _P, _inputs, _norm64, _turn64  # noqa: E402
 T = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _memory_goes_back():
+    """Later tests look at allocations of their own."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def _check(tokens, hq, hk, dim, rot, dtype, axes=1, pair_axis=None, norm=True, interleaved=False, pad=0):
     q, k, table, positions, mixed, wq, wk = _inputs(11, tokens, hq, hk, dim, rot, T[dtype], axes, pad=pad)
     pair_axis = mixed if pair_axis is None else pair_axis

@@ -22,6 +22,13 @@ from test_gpu_orth import ABC, DEV, _P, _exact, _matrix  # noqa: E402
 T = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _memory_goes_back():
+    """Later tests look at allocations of their own."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def _in_halves(u):
     a, b, c = ABC
     one = 2.0 ** 13

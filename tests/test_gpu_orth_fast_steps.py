@@ -12,6 +12,13 @@ from test_gpu_orth import DEV, _P, _matrix  # noqa: E402
 from test_orth_coefficients import SAFE  # noqa: E402
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _memory_goes_back():
+    """Later tests look at allocations of their own."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def _steps(u, change, seed=5):
     g = torch.Generator(device=DEV).manual_seed(seed)
     x = u.double()

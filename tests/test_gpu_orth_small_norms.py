@@ -15,6 +15,13 @@ LISTS = {"tiny": [(20, 30), (5, 700)], "small": [(60, 100), (100, 64)], "tiles":
          "pairs": [(300, 1000), (2000, 140)]}
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _memory_goes_back():
+    """Later tests look at allocations of their own."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def _of_norm(size, seed, norm, dtype):
     x = _matrix(*size, seed, "flat").double()
     return (x * (norm / x.norm())).to(dtype)
