@@ -8,7 +8,9 @@ every local step of a worker
     momentum, then Newton-Schulz products.  They go to SlowMo.local_step as the gradient
     (momentum 0 there; its coupled decay is then the decoupled one);
   - embeddings, norm weights and the head take Adam, in a SlowMo of their own.
-Every tau steps the workers' replicas are averaged and the slow momentum is applied.
+Every tau steps the workers' replicas are averaged and the slow momentum is applied.  The directions'
+momentum is this program's: it is kept over the outer step, each worker's own, whatever the buffer policy
+of SlowMo does to Adam's buffers.
 
     python examples/orthogonal_attention.py [outer iterations]
 """

@@ -52,8 +52,9 @@ typedef struct {
                                position; 4-byte aligned */
   int64_t table_rows;
   const int64_t *positions; /* device, [n_axes][tokens]: row of the table for each axis and token; -1: the
-                               axis's pairs are not turned.  Any other place outside the table gives
-                               NaN in the axis's pairs and nothing else */
+                               axis's pairs are not turned.  Any other place outside the table is not
+                               read and gives NaN in the axis's pairs and nothing else (backward, with
+                               norm: in the token's heads, and in the pairs' weight gradients) */
   int64_t position_stride;  /* elements from one axis to the next, >= tokens; 0: all axes have the same positions */
 } slowmo_head_config;
 
@@ -95,7 +96,7 @@ slowmo_status slowmo_head_norm_rotary(const slowmo_head_config *cfg, int64_t tok
  *   dq_weight, dk_weight : device, D floats each; NULL: not wanted (must be NULL
  *            without norm).  Zeros if there are no tokens or heads.
  *   workspace : device, 16-byte aligned, slowmo_head_backward_bytes() long; NULL if
- *            that is 0.  Sums run in an order fixed by the sizes.
+ *            that is 0.  Sums run in an order fixed by the sizes, strides, alignment and pair_axis.
  * Errors: ARG, ALIGN, NOMEM (workspace too small), HIP.
  */
 size_t slowmo_head_backward_bytes(const slowmo_head_config *cfg, int64_t tokens, int32_t q_heads,
@@ -123,7 +124,10 @@ typedef enum {
 typedef struct {
   int32_t in_dtype;   /* slowmo_dtype of the matrices read */
   int32_t out_dtype;  /* slowmo_dtype of the results.  It decides how the products are formed: of
-                         11-bit halves for bf16 results, of pairs of halves (22 bits) for fp32 */
+                         11-bit halves for bf16 results, of pairs of halves (22 bits) for fp32,
+                         whatever in_dtype is.  Off from 64 bits, Frobenius norms: bf16 results 0.8e-3 to
+                         2.5e-3 (few rows) beside their own rounding of 1.65e-3, up to 2.9e-3 where the
+                         rank is deficient; fp32 results 2e-6, 1.6e-5 */
   int32_t steps;      /* Newton-Schulz steps, 1..SLOWMO_MAX_ORTH_STEPS */
   int32_t scale;      /* slowmo_orth_scale */
   float eps;          /* added to the Frobenius norm, >= 0 */
@@ -174,7 +178,9 @@ slowmo_status slowmo_orthogonalize(slowmo_orth *h, const void *const *in, void *
  * The same behind the momentum of the SGD row of Table C.1:
  *   M <- mu M + G,   U = G + mu M (nesterov) or M,   out <- the orthogonalised U.
  *   momentum : host array of n_matrices device pointers to fp32 matrices (row distance ld), updated
- *              in place; zeros at the start.
+ *              in place; zeros at the start.  It is the caller's: slowmo_outer_step's buffer policies
+ *              (reset, maintain, average) and slowmo_export_state do not reach it.  Left alone it is
+ *              maintained; to reset it, zero it after the outer step.
  *   mu       : 0 <= mu < 1
  * Errors: ARG, ALIGN, HIP.
  */

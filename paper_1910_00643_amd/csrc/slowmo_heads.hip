@@ -7,8 +7,9 @@
 // the mean of squares is the only exchange.  A wave has queries or keys only -- one weight and one
 // sum for its gradient in registers -- and, where a token has enough heads, one token at a time, whose
 // angles are fetched once.
-// Measured: forward 4.2 TB/s (8192 tokens of 32 heads of 64, bf16, 67 MB in 16 us), 4.1 TB/s on two axes in
-// fp32 (12 017 tokens of 32 heads of 72, 221 MB in 54 us); backward 4.8 TB/s (32 768 tokens of 40 heads of 128,
+// Measured: forward 4.2 TB/s (8192 tokens of 32 heads of 64, bf16, 67 MB in 16 us), 4.3 TB/s on two axes in
+// fp32 (12 017 tokens of 32 heads of 72, 221 MB in 52 us), both within the last-level cache, as repeated calls on the
+// same buffers are; backward 4.8 TB/s (32 768 tokens of 40 heads of 128,
 // 1.0 GB in 213 us); a large copy reaches 4.8 TB/s.  48 single tokens: 4.6 us of a call's 10, the rest its
 // launch.
 #include <hip/hip_runtime.h>

@@ -142,7 +142,8 @@ std::vector<Tile> spread(const std::vector<Tile> &v) {
 // for the length of its longest tile: its tiles are cut along the summed side into shares of about equal
 // length, as many as there are slots.  Shares are no shorter than 48 steps and no more than 16 to
 // a tile, since the last one adds the others' sums up (no shorter than 32 / 48 / 96 / 128: an encoder block's
-// matrices 432 / 405 / 411 / 437 us a call).
+// matrices 432 / 405 / 411 / 437 us a call).  The 48 was measured on bf16 results; of pairs of halves a step
+// has three products, and other lengths were not measured.
 void balance(std::vector<Tile> &v, int kind, Plan &p) {
   const int32_t slots = kSlotsOf[kind];
   const size_t whole = v.size() / slots * slots;
@@ -258,7 +259,10 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
   p.small = p.tiny.size() < p.matrices.size() && small == static_cast<int32_t>(p.matrices.size());
   if (p.small)
     for (auto &list : of) list.clear();
-  // The first two steps as one, on n x n matrices: see program().
+  // The first two steps as one, on n x n matrices: see program().  8 matrices of n x k, as one / one by one, us:
+  // n = 1024, k / n = 1.25 375 / 372, 1.5 395 / 396, 2 491 / 518, 4 759 / 842; n = 512 165 / 157, 169 / 163, 177 / 174,
+  // 231 / 242; fp32 results, n = 1024 807 / 778, 871 / 856, 1021 / 1043, 1583 / 1743.  The bound below takes one from
+  // k / n = 1.25 on, up to 8 % too early.
   p.pairs = !p.small && c.steps >= 3 && by_pairs < 0.93 * one_by_one;
 
   int64_t halves = 0;
@@ -314,7 +318,10 @@ Plan plan(const slowmo_orth_config &c, int32_t n_matrices, const int64_t *rows, 
       walk(m.np / side, m.kp / kColsOf[kind], [&](int32_t i, int32_t j) { put(p.lists[kind].update, at, i, j, m.np); });
     }
   }
-  // Too few to fill the card, or beside small ones, whose launch would come on top: as small ones.
+  // Too few to fill the card, or beside small ones, whose launch would come on top: as small ones.  Matrices of 1024 x
+  // 4096, wide / small, us: 256 wide tiles 318 / 315, 384 419 / 414, 512 459 / 465, 1024 760 / 777, 4096 2712 / 2827;
+  // with two of 128 x 512 beside them 384 444 / 413, 512 486 / 475, 768 647 / 652, 2048 1309 / 1313, 4096 2866 / 2829
+  // (fp32 results 384 786 / 752, 512 890 / 904, 2048 2925 / 2969).
   if (p.lists[kWide].update.size() < (p.lists[kSmall].update.empty() ? 512u : 2048u)) {
     for (const Tile &t : p.lists[kWide].update)
       for (int32_t half : {0, 1}) {

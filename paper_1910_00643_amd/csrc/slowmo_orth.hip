@@ -7,7 +7,9 @@
 // up to 3.4^5 times as large; X therefore keeps the next 11 bits too (x = hi + lo) until the last two steps,
 // which enter where X enters linearly, in a X, while the products take hi alone.  Against 64 bits,
 // matrices of 64 to 1024 a side with flat spectra, a few strong directions above noise, or decaying ones:
-// 0.8e-3 to 1.5e-3, of deficient rank up to 2.9e-3 (hi alone up to 8.6e-3, products of bf16 up to 7e-2).
+// 0.8e-3 to 1.5e-3, of deficient rank up to 2.9e-3 (hi alone up to 8.6e-3, products of bf16 up to 7e-2); of 33 to 63 rows
+// up to 2.5e-3.  (X's lower bits in the last two steps too: 1.1 to 1.6 times as far off, since P has a on its diagonal
+// there, which makes its elements smaller.)
 // For fp32 results all factors are such pairs and a product is three: hi hi + hi lo + lo hi, 22 bits.
 #include "slowmo_orth.h"
 
@@ -306,7 +308,8 @@ __device__ __forceinline__ void write_out(const Call &c, const Addresses &at, in
 // the matrix cores go on with one wave per SIMD too (B = 256: 256 accumulators a lane).
 //
 // What bounds them: 8192 x 8192 (256 x 256) the matrix cores at the clock that their power leaves, 1.09e15
-// flop/s over the whole call, where a library's product of that size reaches 1.11e15.  The smaller tiles are
+// flop/s over the whole call, where a library's product of that size reaches 1.11e15.  (All 512 registers of a lane
+// are taken; 4 to 52 more, 20 to 212 bytes, go to scratch memory in front of the loops and behind them.)  The smaller tiles are
 // bound by the way from L2 to shared memory, 12.7 TB/s for 16 KB a step of 128 x 128 (0.33 us with every CU at
 // work, 0.13 us of it products): 0.75e15 in lists of many matrices; and a launch of one round by its ends, 8 us
 // of 16 (1024 x 1024 x 1024, 216 tiles).
@@ -997,7 +1000,7 @@ __global__ __launch_bounds__(kTinyThreads) void k_tiny(Call c, Steps steps, cons
 // memory, in panels of 32 columns as the products' factors lie there.  A call is one launch instead of 17:
 // launches, each with its way to memory and back, are all that such a call takes.  N: 128, or 64 for pairs of
 // halves, and the side of the tiles of X that are replaced one after the other; 4 waves have a quarter of
-// a tile each.  128 x 96: 41 us where the launches of the products take 98; 64 x 64: 14 us.  A step takes 5.6 us at
+// a tile each.  128 x 96: 42 us where the launches of the products take 98; 64 x 64: 14 us.  A step takes 5.6 us at
 // 128, most of it the turns from accumulators to halves and back; the rest is the way of code that runs once.
 template <int N, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void k_small(Call c, Steps steps, Few few, int32_t first) {

@@ -119,7 +119,8 @@ class HeadNormRotary:
     Queries and keys are [tokens, heads, head_dim] (or with more leading dimensions that
     flatten without a copy), each head's elements contiguous, other strides free.
     `positions` is int64, [tokens] or [axes, tokens] (expanded, where all axes have the same): rows of the
-    table, -1 for no turn.  A handle may serve several threads."""
+    table, -1 for no turn.  A handle may serve several threads.  Calling it is an autograd function with a first
+    derivative: no vmap, no forward mode, and torch.compile breaks its graph there."""
 
     def __init__(self, head_dim: int, table: Optional[torch.Tensor] = None, *, dtype: str = "bf16",
                  norm: bool = True, eps: float = 1e-6, interleaved: bool = False,
@@ -361,7 +362,8 @@ class Orthogonalizer:
     def momentum_orthogonalize(self, grads, momentum, out, mu: float, nesterov: bool = True) -> None:
         """momentum <- mu momentum + grads (fp32, in place); out <- the orthogonalised
         grads + mu momentum (nesterov) or momentum.  What `out` holds goes to SlowMo.local_step
-        as the gradient, with momentum 0 there."""
+        as the gradient, with momentum 0 there.  The momentum stays the caller's: SlowMo's buffer
+        policies, averages and export_state() do not reach it (zero it after an outer step to reset it)."""
         _check(lib().slowmo_momentum_orthogonalize(
             self.handle, self._array(grads, self.dtype), self._array(momentum, torch.float32),
             self._array(out, self.out_dtype), mu, int(nesterov), _raw_stream(self.device) or None))
