@@ -22,4 +22,7 @@ def __getattr__(name):          # torch is imported only when the holder is used
     if name in ("Orthogonalizer", "HeadNormRotary", "rotary_table"):
         from . import operators
         return getattr(operators, name)
+    if name in ("Attention", "PagedAttention"):
+        from . import attention
+        return getattr(attention, name)
     raise AttributeError(name)

@@ -10,10 +10,12 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslowmo.so")
-SOURCES = ["slowmo_kernels.hip", "slowmo_heads.hip", "slowmo_orth.hip", "slowmo_orth.cpp", "slowmo_api.cpp", "slowmo_plan.cpp"]
-HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", "slowmo_status.h", "slowmo_orth.h",
+SOURCES = ["slowmo_kernels.hip", "slowmo_heads.hip", "slowmo_orth.hip", "slowmo_orth.cpp", "slowmo_api.cpp", "slowmo_plan.cpp",
+           "slowmo_attention.hip", "slowmo_attention_backward.hip", "slowmo_append.hip"]
+HEADERS = ["slowmo_kernels.h", "slowmo_plan.h", "slowmo_status.h", "slowmo_orth.h", "slowmo_attention.h",
            os.path.join("..", "..", "include", "slowmo.h"),
-           os.path.join("..", "..", "include", "slowmo_operators.h")]
+           os.path.join("..", "..", "include", "slowmo_operators.h"),
+           os.path.join("..", "..", "include", "slowmo_attention.h")]
 
 # -ffp-contract=off: every product and sum rounds on its own, in source order
 # (the order of the paper's formulas); the packed-fp32 feature is disabled.

@@ -1,0 +1,502 @@
+// The gradient of attention over packed sequences (include/slowmo_attention.h has the formulas).
+//
+// Two passes over the visible pairs, each the owner of what it sums, so that nothing is added by atomics: k_queries
+// has 32 queries to a wave and goes over the keys (dQ; it also leaves each row's g . out and its statistics for the other
+// pass), k_keys has 32 keys to a wave and goes over the rows of the query heads that share them (dK, dV).
+// That is seven products of a pair for five: the scores and g V^T are computed twice.
+#include "slowmo_attention.h"
+
+namespace slowmo {
+namespace attention {
+namespace {
+
+struct Args {
+  Rows q, k, v, g, out, dq, dk, dv;
+  const float *lse;
+  const int64_t *q_offsets, *k_offsets;
+  int32_t batch, heads, group, dim;
+  u32 by_group;  // 2^32 / group, rounded up
+  int64_t tokens, keys, first, slots;
+  float scale, scale2;  // of scores; of scores to powers of two
+  Mask mask;
+  bool wide, clear;
+  int32_t parts;        // pieces of the rows that a tile of keys goes over
+  float *lse2, *delta;  // [tokens][query heads]: lse in powers of two; g . out
+  float *sums;          // [parts][keys][key heads][2][padded head]: dK and dV of a piece
+};
+
+template <typename T, int DP>
+constexpr bool kTwoWaves = sizeof(T) == 2 && DP <= 128;  // 256 registers a lane are enough for two waves of a SIMD
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Args a) {
+  using L = Tile<T, DP>;
+  using frag = typename Kind<T>::frag;
+  constexpr int NB = DP / 32, KB = L::rows / 32;
+  extern __shared__ __align__(1024) char smem[];
+  const int lane = threadIdx.x & 63, low = lane & 31, high = lane >> 5;
+  const int wave = uniform(static_cast<int>(threadIdx.x >> 6)), waves = blockDim.x >> 6, height = waves * 32;
+  int head;
+  int64_t slot;
+  if (!head_slot(a.first + blockIdx.x, a.heads, a.slots, head, slot)) return;
+  slot = a.slots - 1 - slot;
+  const Place at = place_of(a.q_offsets, a.batch, a.tokens, a.group, height, slot);
+  const int64_t rows = static_cast<int64_t>(at.n) * a.group, row0 = static_cast<int64_t>(at.tile) * height;
+  if (at.b < 0 || row0 >= rows) return;
+  const int64_t row = row0 + wave * 32 + low;
+  const bool mine = row < rows;
+  const int64_t there = mine ? row : rows - 1;
+  const int token = static_cast<int>(there / a.group), of = static_cast<int>(there - static_cast<int64_t>(token) * a.group);
+  const int64_t qt = at.begin + token;
+  const int qh = head * a.group + of;
+  T *dq = static_cast<T *>(a.dq.data) + qt * a.dq.token + qh * a.dq.head;
+  f32x16 acc[NB];
+  if (at.b == a.batch) {
+    if (!a.clear) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+    store_columns<T, NB>(dq, acc, 0.f, a.dim, high, a.wide, mine);
+    return;
+  }
+  const int64_t k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
+  const int keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
+  const int far = keys - at.n;
+  const int64_t row_last = min(row0 + height, rows) - 1;
+  const Walk walk = walk_of(a.mask, static_cast<int>(row0 / a.group) + far, static_cast<int>(row_last / a.group) + far, keys, L::rows);
+  const Sight sight = sight_of(a.mask, token + far, keys);
+  const int64_t w0 = min(row0 + wave * 32, rows - 1), w1 = min(row0 + wave * 32 + 31, rows - 1);
+  const Sight first = sight_of(a.mask, uniform(static_cast<int>(w0 / a.group)) + far, keys),
+              last = sight_of(a.mask, uniform(static_cast<int>(w1 / a.group)) + far, keys);
+  frag qf[DP / 16], gf[DP / 16];
+  float delta = 0.f;
+  {
+    const T *q = static_cast<const T *>(a.q.data) + qt * a.q.token + qh * a.q.head;
+    const T *g = static_cast<const T *>(a.g.data) + qt * a.g.token + qh * a.g.head;
+    const T *o = static_cast<const T *>(a.out.data) + qt * a.out.token + qh * a.out.head;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      qf[s] = load_frag<T>(q, 16 * s + 8 * high, a.dim, a.wide);
+      gf[s] = load_frag<T>(g, 16 * s + 8 * high, a.dim, a.wide);
+      const frag of_out = load_frag<T>(o, 16 * s + 8 * high, a.dim, a.wide);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) delta += static_cast<float>(gf[s][i]) * static_cast<float>(of_out[i]);
+    }
+  }
+  delta = both_sum(delta);
+  const int64_t at_row = qt * (static_cast<int64_t>(a.heads) * a.group) + qh;
+  const float lse2 = a.lse[at_row] * kLog2E;
+  if (mine && !high) a.lse2[at_row] = lse2, a.delta[at_row] = delta;
+  if (a.dim != DP) {
+    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  const T *k = static_cast<const T *>(a.k.data) + k_begin * a.k.token + head * a.k.head;
+  const T *v = static_cast<const T *>(a.v.data) + k_begin * a.v.token + head * a.v.head;
+  for (bool careful = false;; careful = true) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+    auto bring = [&](int u) {
+      char *to = smem + (u & 1) * 2 * L::bytes;
+      const int j0 = walk.at(u) * L::rows, end = keys - 1 - j0;
+      bring_rows<T, DP>(to, k + j0 * a.k.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.k.token; });
+      bring_rows<T, DP>(to + L::bytes, v + j0 * a.v.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.v.token; });
+    };
+    if (walk.count) bring(0);
+    for (int u = 0; u < walk.count; ++u) {
+      arrive();
+      if (u + 1 < walk.count) bring(u + 1);
+      char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
+      const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
+      if (careful) tame<T, DP, NB, true>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
+      if ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks) continue;
+      const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        f32x16 s{}, dp{};
+#pragma unroll
+        for (int st = 0; st < DP / 16; ++st) {
+          s = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s);
+          dp = mma(row_frag<T, DP>(v_tile, 32 * kb + low, st, high), gf[st], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale2, -lse2)) * (dp[i] - delta);
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!sees(sight, j0 + 32 * kb + 8 * (i / 4) + 4 * high + i % 4)) s[i] = 0.f;
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const frag ds = as_frag<T>(s, half);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(k_tile, b, 2 * kb + half, lane), ds, acc[b]);
+        }
+      }
+    }
+    if (careful) break;
+    int any = 0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) any |= wild(acc[b][i]);
+    if (!__syncthreads_or(any)) break;
+  }
+  store_columns<T, NB>(dq, acc, a.scale, a.dim, high, a.wide, mine);
+}
+
+// A row of a tile as the keys see it.
+template <int ROWS>
+struct Stats {
+  float lse2[ROWS], delta[ROWS];
+  int position[ROWS];
+};
+constexpr int kNowhere = INT32_MIN + 1;  // of rows past the last one
+
+template <typename T, int DP>
+constexpr int keys_bytes() {
+  return 4 * Tile<T, DP>::bytes + 2 * static_cast<int>(sizeof(Stats<Tile<T, DP>::rows>));
+}
+
+__device__ __forceinline__ void word_to_shared(u32 shared, const float *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(shared), "v"(from) : "memory");
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void k_keys(Args a) {
+  using L = Tile<T, DP>;
+  using frag = typename Kind<T>::frag;
+  constexpr int NB = DP / 32, RB = L::rows / 32;
+  extern __shared__ __align__(1024) char smem[];
+  const int lane = threadIdx.x & 63, low = lane & 31, high = lane >> 5;
+  const int wave = uniform(static_cast<int>(threadIdx.x >> 6)), waves = blockDim.x >> 6, width = waves * 32;
+  int head;
+  int64_t slot;
+  if (!head_slot(a.first + blockIdx.x, a.heads, a.slots * a.parts, head, slot)) return;
+  const int part = static_cast<int>(slot % a.parts);
+  slot /= a.parts;  // the first tiles, which the most queries see, first
+  const Place at = place_of(a.k_offsets, a.batch, a.keys, 1, width, slot);
+  const int keys = at.n;
+  const int j0 = at.tile * width;
+  if (at.b < 0 || static_cast<int64_t>(at.tile) * width >= keys) return;
+  const int j = j0 + wave * 32 + low;
+  const bool mine = j < keys;
+  const int jc = mine ? j : keys - 1;
+  const int64_t kt = at.begin + jc;
+  T *dk = static_cast<T *>(a.dk.data) + kt * a.dk.token + head * a.dk.head;
+  T *dv = static_cast<T *>(a.dv.data) + kt * a.dv.token + head * a.dv.head;
+  f32x16 acck[NB], accv[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
+  if (at.b == a.batch) {
+    if (!a.clear || part) return;
+    store_columns<T, NB>(dk, acck, 0.f, a.dim, high, a.wide, mine);
+    store_columns<T, NB>(dv, accv, 0.f, a.dim, high, a.wide, mine);
+    return;
+  }
+  const int64_t q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
+  const int n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  const int far = keys - n;
+  // positions of the queries that see some key of the tile, of the wave, and this lane's key
+  const int j_end = min(j0 + width, keys) - 1;
+  auto from_of = [&](int key) { return a.mask.causal ? key : a.mask.window && key >= a.mask.sinks ? key - a.mask.window + 1 : kNowhere + 1; };
+  auto to_of = [&](int key) { return a.mask.window && key >= a.mask.sinks ? key + a.mask.window - 1 : INT32_MAX; };
+  int p_lo = from_of(j0), p_hi = to_of(j_end);
+  if (j0 < a.mask.sinks) p_hi = INT32_MAX, p_lo = a.mask.causal ? j0 : kNowhere + 1;
+  const int i_lo = static_cast<int>(clamped(static_cast<int64_t>(p_lo) - far, 0, n)),
+            i_hi = static_cast<int>(clamped(static_cast<int64_t>(p_hi) - far + 1, 0, n));  // exclusive
+  const int64_t r_lo = static_cast<int64_t>(i_lo) * a.group, r_hi = static_cast<int64_t>(max(i_hi, i_lo)) * a.group;
+  const int64_t tiles = (r_hi - r_lo + L::rows - 1) / L::rows, per = (tiles + a.parts - 1) / a.parts;
+  const int64_t u0 = min(part * per, tiles), u1 = min(u0 + per, tiles);
+  const int my_lo = mine ? from_of(j) : 1, my_hi = mine ? to_of(j) : 0;
+  const int wj0 = j0 + wave * 32, wj1 = min(wj0 + 31, keys - 1);
+  const bool whole = wj0 + 31 < keys;
+
+  frag kf[DP / 16], vf[DP / 16];
+  {
+    const T *k = static_cast<const T *>(a.k.data) + kt * a.k.token + head * a.k.head;
+    const T *v = static_cast<const T *>(a.v.data) + kt * a.v.token + head * a.v.head;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      kf[s] = load_frag<T>(k, 16 * s + 8 * high, a.dim, a.wide);
+      vf[s] = load_frag<T>(v, 16 * s + 8 * high, a.dim, a.wide);
+    }
+  }
+  if (a.dim != DP) {
+    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  const T *q = static_cast<const T *>(a.q.data) + static_cast<int64_t>(head) * a.group * a.q.head;
+  const T *g = static_cast<const T *>(a.g.data) + static_cast<int64_t>(head) * a.group * a.g.head;
+  const int64_t stat0 = static_cast<int64_t>(head) * a.group, per_token = static_cast<int64_t>(a.heads) * a.group;
+  using S = Stats<L::rows>;
+  S *stats = reinterpret_cast<S *>(smem + 4 * L::bytes);
+  for (bool careful = false;; careful = true) {
+    auto bring = [&](int64_t u) {
+      char *to = smem + (u & 1) * 2 * L::bytes;
+      S *st = stats + (u & 1);
+      // rows r0 .. of the sequence's (token, head) rows; those past the end take the last one's place
+      const int64_t r0 = r_lo + u * L::rows, t0 = r0 / a.group;
+      const int o0 = static_cast<int>(r0 - t0 * a.group), end = static_cast<int>(min(r_hi - r0, static_cast<int64_t>(L::rows))) - 1;
+      auto split = [&](int r, int &t, int &o) {
+        const u32 x = o0 + min(r, end);
+        t = a.group == 1 ? x : __umulhi(x, a.by_group);
+        o = x - t * a.group;
+      };
+      const int64_t qt = q_begin + t0;
+      bring_rows<T, DP>(to, q + qt * a.q.token, a.dim, a.wide, [&](int r) {
+        int t, o;
+        split(r, t, o);
+        return t * a.q.token + o * a.q.head;
+      });
+      bring_rows<T, DP>(to + L::bytes, g + qt * a.g.token, a.dim, a.wide, [&](int r) {
+        int t, o;
+        split(r, t, o);
+        return t * a.g.token + o * a.g.head;
+      });
+      int t, o;
+      split(lane & (L::rows - 1), t, o);
+      const int64_t s = (qt + t) * per_token + stat0 + o;
+      if (lane < L::rows) {
+        if (wave == 0) word_to_shared(uniform(offset_of(st->lse2)), a.lse2 + s);
+        if (wave == waves - 1) {
+          word_to_shared(uniform(offset_of(st->delta)), a.delta + s);
+          st->position[lane] = lane <= end ? static_cast<int>(t0) + t + far : kNowhere;
+        }
+      }
+    };
+    if (u0 < u1) bring(u0);
+    for (int64_t u = u0; u < u1; ++u) {
+      arrive();
+      if (u + 1 < u1) bring(u + 1);
+      char *q_tile = smem + (u & 1) * 2 * L::bytes, *g_tile = q_tile + L::bytes;
+      const S *st = stats + (u & 1);
+      auto sees_row = [&](int r) {
+        const int p = st->position[r];
+        return p >= my_lo && p <= my_hi && p != kNowhere;
+      };
+      if (careful) {
+        tame<T, DP, NB, true>(q_tile, acck, sees_row);
+        tame<T, DP, NB, true>(g_tile, accv, sees_row);
+      }
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int pa = uniform(st->position[32 * rb]), pb = uniform(st->position[32 * rb + 31]);
+        // every row sees every key of the wave, or (rows in order, none missing) none does
+        bool all = whole && pb != kNowhere && (!a.mask.causal || wj1 <= pa);
+        bool none = pa == kNowhere || wj0 >= keys || (pb != kNowhere && a.mask.causal && wj0 > pb);
+        if (a.mask.window) {
+          all = all && (wj1 < a.mask.sinks || (pb - wj0 < a.mask.window && wj1 - pa < a.mask.window));
+          none = none || (wj0 >= a.mask.sinks && ((pa - wj1 >= a.mask.window) || (pb != kNowhere && wj0 - pb >= a.mask.window)));
+        }
+        if (none) continue;
+        f32x16 s{}, dp{};
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e) {
+          s = mma(row_frag<T, DP>(q_tile, 32 * rb + low, e, high), kf[e], s);
+          dp = mma(row_frag<T, DP>(g_tile, 32 * rb + low, e, high), vf[e], dp);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int r = 32 * rb + 8 * c + 4 * high;
+          const f32x4 l = *reinterpret_cast<const f32x4 *>(st->lse2 + r), d = *reinterpret_cast<const f32x4 *>(st->delta + r);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[4 * c + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * c + i], a.scale2, -l[i]));
+            dp[4 * c + i] = s[4 * c + i] * (dp[4 * c + i] - d[i]);
+          }
+          if (!all) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!sees_row(r + i)) s[4 * c + i] = dp[4 * c + i] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const frag pf = as_frag<T>(s, half), df = as_frag<T>(dp, half);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            accv[b] = mma(column_frag<T, DP>(g_tile, b, 2 * rb + half, lane), pf, accv[b]);
+            acck[b] = mma(column_frag<T, DP>(q_tile, b, 2 * rb + half, lane), df, acck[b]);
+          }
+        }
+      }
+    }
+    if (careful) break;
+    int any = 0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) any |= wild(acck[b][i]) || wild(accv[b][i]);
+    if (!__syncthreads_or(any)) break;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
+  }
+  if (a.parts == 1) {
+    store_columns<T, NB>(dk, acck, a.scale, a.dim, high, a.wide, mine);
+    store_columns<T, NB>(dv, accv, 1.f, a.dim, high, a.wide, mine);
+  } else {
+    float *to = a.sums + ((part * a.keys + kt) * a.heads + head) * (2 * DP);
+    store_columns<float, NB>(to, acck, a.scale, DP, high, true, mine);
+    store_columns<float, NB>(to + DP, accv, 1.f, DP, high, true, mine);
+  }
+}
+
+// The pieces of a key's sums added in their order; 4 elements to a lane.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_add(Args a) {
+  constexpr int N = 2 * DP / 4;
+  const int64_t at = a.first * 256 + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t row = at / N;
+  const int e = static_cast<int>(at - row * N) * 4, d = e % DP;
+  if (row >= a.keys * a.heads || d >= a.dim) return;
+  const int64_t kt = row / a.heads;
+  const int head = static_cast<int>(row - kt * a.heads);
+  if (kt >= a.k_offsets[a.batch]) return;  // behind the last sequence
+  f32x4 sum = *reinterpret_cast<const f32x4 *>(a.sums + row * (2 * DP) + e);
+  for (int p = 1; p < a.parts; ++p) {
+    const f32x4 more = *reinterpret_cast<const f32x4 *>(a.sums + (p * a.keys * a.heads + row) * (2 * DP) + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += more[i];
+  }
+  const Rows &r = e < DP ? a.dk : a.dv;
+  T *to = static_cast<T *>(r.data) + kt * r.token + head * r.head + d;
+  for (int i = 0; i < 4; ++i)
+    if (d + i < a.dim) to[i] = static_cast<T>(sum[i]);
+}
+
+struct Plan {
+  int q_waves, k_waves, parts;
+};
+Plan plan_for(int64_t tokens, int64_t keys, int64_t group, int64_t heads, int64_t batch, int rows_of_tile) {
+  Plan p;
+  p.q_waves = waves_of(tokens, group, batch, 4);
+  p.k_waves = waves_of(keys, 1, batch, 4);
+  const int64_t blocks = std::max<int64_t>(1, (keys / (p.k_waves * 32) + std::min<int64_t>(batch, keys)) * heads);
+  const int64_t tiles = tokens * group / std::max<int64_t>(batch, 1) / rows_of_tile;
+  p.parts = static_cast<int>(std::clamp<int64_t>((512 + blocks - 1) / blocks, 1, std::clamp<int64_t>(tiles / 4, 1, 16)));
+  return p;
+}
+int tile_rows(int dim, int32_t dtype) { return padded(dim) * static_cast<int>(size_of(dtype)) > 512 ? 32 : 64; }
+
+hipError_t run(Args a, int32_t dtype, const Plan &p, hipStream_t stream) {
+  hipError_t e = hipSuccess;
+  auto room = [&](auto kernel, int bytes) {
+    if (bytes > 64 * 1024)
+      e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  };
+  dispatch(dtype, a.dim, [&](auto kind, auto dp) {
+    using T = decltype(kind);
+    constexpr int DP = dp();
+    using L = Tile<T, DP>;
+    if (a.tokens) {
+      room(k_queries<T, DP>, 4 * L::bytes);
+      a.slots = slots_of(a.tokens, a.group, p.q_waves * 32, a.batch);
+      const int64_t items = items_of(a.heads, a.slots);
+      for (a.first = 0; a.first < items && e == hipSuccess; a.first += kMostBlocks) {
+        k_queries<T, DP><<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.q_waves, 4 * L::bytes, stream>>>(a);
+        e = hipGetLastError();
+      }
+    }
+    if (a.keys && e == hipSuccess) {
+      room(k_keys<T, DP>, keys_bytes<T, DP>());
+      a.slots = slots_of(a.keys, 1, p.k_waves * 32, a.batch);
+      const int64_t items = items_of(a.heads, a.slots * a.parts);
+      for (a.first = 0; a.first < items && e == hipSuccess; a.first += kMostBlocks) {
+        k_keys<T, DP><<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.k_waves, keys_bytes<T, DP>(), stream>>>(a);
+        e = hipGetLastError();
+      }
+      if (a.parts > 1) {
+        const int64_t blocks = (a.keys * a.heads * (2 * DP / 4) + 255) / 256;
+        for (a.first = 0; a.first < blocks && e == hipSuccess; a.first += kMostBlocks) {
+          k_add<T, DP><<<static_cast<u32>(std::min(kMostBlocks, blocks - a.first)), 256, 0, stream>>>(a);
+          e = hipGetLastError();
+        }
+      }
+    }
+  });
+  return e;
+}
+
+size_t stat_bytes(int64_t tokens, int64_t q_heads) { return (static_cast<size_t>(tokens) * q_heads * 4 + 15) / 16 * 16; }
+
+}  // namespace
+}  // namespace attention
+}  // namespace slowmo
+
+using namespace slowmo;
+using namespace slowmo::attention;
+
+extern "C" {
+
+size_t slowmo_attention_backward_bytes(const slowmo_attention_config *cfg, int32_t batch, int64_t tokens, int64_t keys,
+                                       int32_t q_heads, int32_t k_heads) {
+  if (check_config(cfg) || batch < 0 || tokens < 0 || keys < 0 || tokens > kLongest || keys > kLongest || q_heads < 1 ||
+      k_heads < 1 || q_heads > (1 << 20) || q_heads % k_heads)
+    return 0;
+  const Plan p = plan_for(tokens, keys, q_heads / k_heads, k_heads, batch, tile_rows(cfg->head_dim, cfg->dtype));
+  return 2 * stat_bytes(tokens, q_heads) +
+         (p.parts > 1 ? static_cast<size_t>(p.parts) * keys * k_heads * 2 * padded(cfg->head_dim) * sizeof(float) : 0);
+}
+
+slowmo_status slowmo_attention_backward(const slowmo_attention_config *cfg, int32_t batch, const int64_t *q_offsets,
+                                        const int64_t *k_offsets, int64_t tokens, int64_t keys, const slowmo_heads *g,
+                                        const slowmo_heads *q, const slowmo_heads *k, const slowmo_heads *v,
+                                        const slowmo_heads *out, const float *lse, const slowmo_heads *dq,
+                                        const slowmo_heads *dk, const slowmo_heads *dv, void *workspace,
+                                        size_t workspace_bytes, void *stream) {
+  return walled([&]() -> slowmo_status {
+    auto bad = [](const char *msg) { return fail_thread(SLOWMO_ERR_ARG, msg); };
+    if (const slowmo_status s = check_call(cfg, batch, q_offsets, k_offsets, tokens, keys)) return s;
+    const slowmo_heads *in[] = {g, q, out, k, v}, *written[] = {dq, dk, dv};
+    const int32_t d = cfg->head_dim, dt = cfg->dtype;
+    for (int i = 0; i < 5; ++i)
+      if (const slowmo_status s = check_rows(in[i], i < 3 ? tokens : keys, d, dt, false)) return s;
+    for (int i = 0; i < 3; ++i)
+      if (const slowmo_status s = check_rows(written[i], i < 1 ? tokens : keys, d, dt, true)) return s;
+    if (q->heads != g->heads || q->heads != out->heads || q->heads != dq->heads || k->heads != v->heads ||
+        k->heads != dk->heads || k->heads != dv->heads)
+      return bad("g, out and dq have q's heads, v, dk and dv have k's");
+    if (const slowmo_status s = check_group(q->heads, k->heads)) return s;
+    if (tokens && !lse) return bad("lse is NULL");
+    if (!aligned(lse, 4)) return fail_thread(SLOWMO_ERR_ALIGN, "lse must be 4-byte aligned");
+    const size_t need = slowmo_attention_backward_bytes(cfg, batch, tokens, keys, q->heads, k->heads);
+    if (need && !workspace) return bad("workspace is NULL");
+    if (need && !aligned(workspace, 16)) return fail_thread(SLOWMO_ERR_ALIGN, "workspace must be 16-byte aligned");
+    if (workspace_bytes < need) return fail_thread(SLOWMO_ERR_NOMEM, "workspace is smaller than slowmo_attention_backward_bytes()");
+    Extent from[6], to[4];
+    for (int i = 0; i < 5; ++i) from[i] = extent(*in[i], i < 3 ? tokens : keys, d, dt);
+    from[5] = extent(lse, tokens * q->heads * sizeof(float));
+    for (int i = 0; i < 3; ++i) to[i] = extent(*written[i], i < 1 ? tokens : keys, d, dt);
+    to[3] = extent(workspace, need);
+    for (int i = 0; i < 4; ++i) {
+      for (const Extent &x : from)
+        if (overlap(to[i], x)) return bad("an output or the workspace overlaps an input");
+      for (int j = 0; j < i; ++j)
+        if (overlap(to[i], to[j])) return bad("outputs, or one and the workspace, overlap");
+    }
+    if (!tokens && !keys) return SLOWMO_OK;
+    Args a{};
+    a.q = rows_of(*q), a.k = rows_of(*k), a.v = rows_of(*v), a.g = rows_of(*g), a.out = rows_of(*out);
+    a.dq = rows_of(*dq), a.dk = rows_of(*dk), a.dv = rows_of(*dv);
+    a.lse = lse, a.q_offsets = q_offsets, a.k_offsets = k_offsets ? k_offsets : q_offsets;
+    a.batch = batch, a.heads = k->heads, a.group = q->heads / k->heads, a.dim = d;
+    a.by_group = static_cast<u32>(((uint64_t(1) << 32) + a.group - 1) / a.group);
+    a.tokens = tokens, a.keys = keys;
+    a.scale = cfg->scale, a.scale2 = cfg->scale * kLog2E;
+    a.mask = mask_of(*cfg);
+    a.clear = cfg->clear_rest != 0;
+    a.wide = true;
+    for (const slowmo_heads *h : in) a.wide = a.wide && wide_rows(*h, d, dt);
+    for (const slowmo_heads *h : written) a.wide = a.wide && wide_rows(*h, d, dt);
+    const Plan p = plan_for(tokens, keys, a.group, a.heads, batch, tile_rows(d, dt));
+    a.parts = p.parts;
+    a.lse2 = static_cast<float *>(workspace);
+    a.delta = a.lse2 + stat_bytes(tokens, q->heads) / 4;
+    a.sums = a.delta + stat_bytes(tokens, q->heads) / 4;
+    const hipError_t e = run(a, dt, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SLOWMO_OK : fail_thread_hip(e, "slowmo_attention_backward");
+  });
+}
+
+}  // extern "C"
