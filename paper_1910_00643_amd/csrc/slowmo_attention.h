@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <utility>
 
 #include "../../include/slowmo_attention.h"
 #include "slowmo_status.h"
@@ -153,19 +154,19 @@ __device__ __forceinline__ typename Kind<T>::frag column_frag(const char *tile, 
 // Rows to a tile: row r comes from base + row_at(r) elements (base and row_at of rows past the end: some row that
 // may be read).  wide: 16 bytes a lane straight to shared memory, 32-bit offsets; else element by element.
 template <typename T, int DP, typename F>
-__device__ __forceinline__ void bring_rows(char *tile, const T *base, int dim, bool wide, F &&row_at) {
+__device__ __forceinline__ void bring_rows(char *tile, int rows, const T *base, int dim, bool wide, F &&row_at) {
   using L = Tile<T, DP>;
   if (wide) {
     const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6)), waves = blockDim.x >> 6;
     const u32 shared = uniform(offset_of(tile));
     const T *from = uniform(base);
-    for (int n = wave; n < L::bytes / 1024; n += waves) {
+    for (int n = wave; n < rows * L::row_bytes / 1024; n += waves) {
       const int at = n * 64 + lane, row = at / L::C, c = (at & (L::C - 1)) ^ L::turn(row);
       const u32 offset = (static_cast<u32>(row_at(row)) + c * L::E) * sizeof(T);
       if (c * L::E < dim) to_shared(uniform(shared + n * 1024), offset, from);
     }
   } else {
-    for (int i = threadIdx.x; i < L::rows * L::used; i += blockDim.x) {
+    for (int i = threadIdx.x; i < rows * L::used; i += blockDim.x) {
       const int row = i / L::used, c = i % L::used;
       const T *x = base + row_at(row);
       T *to = reinterpret_cast<T *>(tile + row * L::row_bytes + ((c ^ L::turn(row)) << 4));
@@ -211,6 +212,32 @@ __device__ __forceinline__ typename Kind<T>::frag load_frag(const T *row, int d,
     for (int i = 0; i < 8; ++i) f[i] = d + i < dim ? row[d + i] : static_cast<T>(0.f);
   }
   return f;
+}
+
+// The value is waited for here: its first use inside a loop would wait in every turn, and with it for the loads to
+// shared memory that are under way (a tile 18 instead of 3 us).
+template <typename V>
+__device__ __forceinline__ void settle(V &v) {
+  asm volatile("" : "+v"(v));
+}
+
+// Keeps what follows a uniform condition behind it: the mask's comparisons, which few tiles need, would otherwise be
+// made for every one.
+__device__ __forceinline__ void branch() { asm volatile(""); }
+
+// The order of a stretch of N steps of PRODUCTS products that take READS reads of shared memory: AHEAD steps' reads first, then
+// a step's products and the reads of the one AHEAD of it in turn.  Left to itself the compiler reads for one product at a
+// time and waits for it.
+template <int PRODUCTS, int READS, int AHEAD, int... I>
+__device__ __forceinline__ void read_ahead(std::integer_sequence<int, I...>) {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+  ((__builtin_amdgcn_sched_group_barrier(0x8, PRODUCTS, 0), __builtin_amdgcn_sched_group_barrier(0x100, READS, 0), (void)I), ...);
+  __builtin_amdgcn_sched_group_barrier(0x8, AHEAD * PRODUCTS, 0);
+}
+template <typename T, int N, int PRODUCTS, int READS, int AHEAD>
+__device__ __forceinline__ void read_ahead() {
+  if constexpr (sizeof(T) == 2 && N > AHEAD) read_ahead<PRODUCTS, READS, AHEAD>(std::make_integer_sequence<int, N - AHEAD>{});
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // The two halves of the wave exchanged: x's upper with y's lower.
@@ -375,28 +402,25 @@ __device__ __forceinline__ T *element(char *tile, int row, int d) {
 // others' zeros (0 times infinity).  Only a pass whose result came out wild is done again with this, tile by
 // tile: what is wild is added to the columns that see it and then taken out of the tile.  `seen(row)`: whether the
 // lane's column sees the tile's row.  All waves of the workgroup come here.
-template <typename T, int DP, int NB, bool ADD, typename F>
+template <typename T, int DP, int ROWS, int NB, typename F>
 __device__ void tame(char *tile, f32x16 (&acc)[NB], F &&seen) {
-  using L = Tile<T, DP>;
-  const int lane = threadIdx.x & 63, high = lane >> 5;
+  const int high = (threadIdx.x & 63) >> 5;
   int any = 0;
-  for (int i = threadIdx.x; i < L::rows * DP; i += blockDim.x)
+  for (int i = threadIdx.x; i < ROWS * DP; i += blockDim.x)
     any |= wild(static_cast<float>(*element<T, DP>(tile, i / DP, i % DP)));
   if (!__syncthreads_or(any)) return;
-  if constexpr (ADD) {
-    for (int row = 0; row < L::rows; ++row) {
-      const bool mine = seen(row);
+  for (int row = 0; row < ROWS; ++row) {
+    const bool mine = seen(row);
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float v = static_cast<float>(*element<T, DP>(tile, row, 32 * b + 8 * (i / 4) + 4 * high + i % 4));
-          if (mine && wild(v)) acc[b][i] += v;
-        }
-    }
-    __syncthreads();
+      for (int i = 0; i < 16; ++i) {
+        const float v = static_cast<float>(*element<T, DP>(tile, row, 32 * b + 8 * (i / 4) + 4 * high + i % 4));
+        if (mine && wild(v)) acc[b][i] += v;
+      }
   }
-  for (int i = threadIdx.x; i < L::rows * DP; i += blockDim.x) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < ROWS * DP; i += blockDim.x) {
     T *e = element<T, DP>(tile, i / DP, i % DP);
     if (wild(static_cast<float>(*e))) *e = static_cast<T>(0.f);
   }
@@ -421,6 +445,12 @@ __device__ __forceinline__ Walk walk_of(const Mask &m, int p_lo, int p_hi, int k
   w.count = w.head + hi / tile - w.first + 1;
   return w;
 }
+// A walk over `count` tiles in pieces of `per`: at least `least` tiles each, at most `splits` pieces.
+__device__ __forceinline__ int pieces_of(int count, int splits, int least, int &per) {
+  per = max(least, (count + splits - 1) / splits);
+  return count ? (count + per - 1) / per : 1;
+}
+
 // ---- the C entries ----
 
 template <int DP, typename F>

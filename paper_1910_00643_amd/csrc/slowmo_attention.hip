@@ -10,6 +10,8 @@ namespace slowmo {
 namespace attention {
 namespace {
 
+constexpr int kMostPieces = 256;  // of a row's keys: a thread each where they are joined
+
 struct Args {
   Rows q, k, v, out;
   float *lse;
@@ -30,11 +32,6 @@ __device__ const u32x4 kNothing[1] = {{0, 0, 0, 0}};
 // NaN in bf16 and in fp32
 __device__ const u32x4 kNoNumber[1] = {{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u}};
 
-__device__ __forceinline__ int pieces_of(int count, int splits, int least, int &per) {
-  per = max(least, (count + splits - 1) / splits);
-  return count ? (count + per - 1) / per : 1;
-}
-
 // A tile's way from memory to shared memory.  j0: its first position; rows past `keys` take the last one's place
 // and are masked.
 template <typename T, int DP, bool PAGED>
@@ -52,7 +49,7 @@ struct Stage {
                                        int page) const {
     const T *base = static_cast<const T *>(x.data) + head * x.head;
     if constexpr (!PAGED) {
-      bring_rows<T, DP>(tile, base + (begin + j0) * x.token, a.dim, a.wide,
+      bring_rows<T, DP>(tile, L::rows, base + (begin + j0) * x.token, a.dim, a.wide,
                         [&](int r) { return min(r, keys - 1 - j0) * x.token; });
       return;
     }
@@ -72,6 +69,26 @@ struct Stage {
       return;
     }
     const u32 shared = uniform(offset_of(tile));
+    constexpr int R = L::C < 64 ? 64 / L::C : 1;  // rows of a piece
+    // Whole tiles whose pieces each lie in one page: the page's address is worked out once for a piece, by scalar
+    // instructions (48 single tokens over 16 000: 667 -> 452 us).
+    if ((1 << a.page_log2) >= R && j0 + L::rows <= keys &&
+        __all(static_cast<u32>(page) < static_cast<u32>(a.n_pages))) {
+      const u32 step = static_cast<u32>(x.token) * sizeof(T);
+      auto piece = [&](int n) {
+        const int row0 = n * R, row = row0 + lane / L::C, c = (lane & (L::C - 1)) ^ L::turn(row);
+        const int id = __builtin_amdgcn_readlane(page, row0);
+        const T *from = base + static_cast<int64_t>(id) * page_stride + ((j0 + row0) & ((1 << a.page_log2) - 1)) * x.token;
+        if (c * L::E < a.dim) to_shared(uniform(shared + n * 1024), (lane / L::C) * step + c * 16, uniform(from));
+      };
+      if (waves == 1) {
+#pragma unroll
+        for (int n = 0; n < L::bytes / 1024; ++n) piece(n);
+      } else {
+        for (int n = wave; n < L::bytes / 1024; n += waves) piece(n);
+      }
+      return;
+    }
     for (int n = wave; n < L::bytes / 1024; n += waves) {
       const int at = n * 64 + lane, row = at / L::C, c = (at & (L::C - 1)) ^ L::turn(row);
       const int r = min(row, keys - 1 - j0);
@@ -148,11 +165,14 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
   const Sight first = sight_of(a.mask, uniform(static_cast<int>(w0 / a.group)) + far, keys),
               last = sight_of(a.mask, uniform(static_cast<int>(w1 / a.group)) + far, keys);
 
+  const bool idle = row0 + wave * 32 >= rows;
   frag qf[DP / 16];
   {
     const T *q = static_cast<const T *>(a.q.data) + qt * a.q.token + qh * a.q.head;
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) qf[s] = load_frag<T>(q, 16 * s + 8 * high, a.dim, a.wide);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) settle(qf[s]);
   }
   if (a.dim != DP) {  // the rows' ends that no load writes
     for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
@@ -168,6 +188,7 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
     auto bring = [&](int u) {
       char *to = smem + (u & 1) * 2 * L::bytes;
       const int j0 = walk.at(u) * L::rows;
+      if constexpr (PAGED) settle(page);
       stage.template load<false>(to, a.k, a.k_page, k_begin, head, j0, page);
       stage.template load<true>(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
     };
@@ -187,17 +208,20 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
       if (careful)
-        tame<T, DP, NB, true>(v_tile, acc, [&](int r) { return sees(sight, j0 + r); });
-      // no row of the wave sees a key of the tile
-      if ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks) continue;
+        tame<T, DP, L::rows, NB>(v_tile, acc, [&](int r) { return sees(sight, j0 + r); });
+      // the wave has no row, or none that sees a key of the tile
+      if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       f32x16 s[KB];
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        s[kb] = f32x16{};
+      for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
 #pragma unroll
-        for (int st = 0; st < DP / 16; ++st) s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s[kb]);
-      }
+      for (int st = 0; st < DP / 16; ++st)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s[kb]);
+      read_ahead<T, KB * DP / 16, 1, 1, 6>();
       if (!((j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks)) {
+        branch();
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -235,6 +259,7 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, lane), p, acc[b]);
       }
+      read_ahead<T, NB * L::rows / 16, 1, 2, 3>();
     }
     if (careful) break;
     int any = 0;
@@ -258,12 +283,15 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
   }
 }
 
-// The pieces of a row joined in their order: a wave each, 4 elements to a lane.
-template <typename T, int DP>
+// The pieces of a row joined in their order.  WAVES = 1: a wave a row, for up to 32 pieces; 4: a workgroup a row, every
+// fourth piece to a wave.  4 elements to a lane.
+template <typename T, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
+  __shared__ float weights[4][64], of_wave[4];
+  __shared__ f32x4 sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t every = a.tokens * a.heads * a.group;
-  const int64_t at_row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) + a.first;
-  const int lane = threadIdx.x & 63;
+  const int64_t at_row = (blockIdx.x + a.first) * (4 / WAVES) + (WAVES == 1 ? uniform(wave) : 0);
   if (at_row >= every) return;
   const int64_t qt = at_row / (a.heads * a.group);
   const int qh = static_cast<int>(at_row - qt * (a.heads * a.group));
@@ -271,7 +299,7 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
   int count = 0;
   for (int first = 0; first <= a.batch; first += 64) {
     const int b = first + lane;
-    const int got = __popcll(__ballot(b <= a.batch && clamped(a.q_offsets[b], 0, a.tokens) <= qt));
+    const int got = __popcll(__ballot(b <= a.batch && clamped(a.q_offsets[min(b, a.batch)], 0, a.tokens) <= qt));
     count += got;
     if (got < 64) break;
   }
@@ -281,34 +309,55 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
   const int n = static_cast<int>(end - begin), keys = static_cast<int>(clamped(uniform(a.k_offsets[b]), 0, kLongest));
   const int64_t rows = static_cast<int64_t>(n) * a.group, row = (qt - begin) * a.group + qh % a.group;
   const int64_t row0 = row / height * height, row_last = min(row0 + height, rows) - 1;
+  if (row >= rows) return;
   const Walk walk = walk_of(a.mask, static_cast<int>(row0 / a.group) + keys - n, static_cast<int>(row_last / a.group) + keys - n,
                             keys, tile);
   int per;
   const int pieces = pieces_of(walk.count, a.splits, a.least, per);
   if (pieces == 1) return;
-  float m = -INFINITY;
-  bool none = false;
-  for (int z = 0; z < pieces; ++z) {
-    const float v = a.part_lse[z * every + at_row];
-    none |= v != v;
-    m = fmaxf(m, v);
-  }
-  const float under = m == -INFINITY ? 0.f : m;
-  float total = 0.f;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int z = 0; z < pieces; ++z) {
-    const float w = __builtin_amdgcn_exp2f(a.part_lse[z * every + at_row] - under);
-    total += w;
-    if (4 * lane < DP && w != 0.f) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part + (z * every + at_row) * DP + 4 * lane);
+  // one piece a lane: the largest, then the weights
+  const int z = WAVES == 1 ? lane : threadIdx.x;
+  const float mine = z < pieces ? a.part_lse[z * every + at_row] : -INFINITY;
+  float m = mine;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += w * v[i];
-    }
+  for (int by = 1; by < 64; by *= 2) m = fmaxf(m, __shfl_xor(m, by));
+  bool none = __any(mine != mine);
+  if constexpr (WAVES > 1) {
+    none = __syncthreads_or(none);
+    if (lane == 0) of_wave[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
   }
+  const float weight = __builtin_amdgcn_exp2f(mine - (m == -INFINITY ? 0.f : m));
+  if constexpr (WAVES > 1) {
+    weights[wave][lane] = weight;
+    __syncthreads();
+  }
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int y = WAVES == 1 ? 0 : wave; y < pieces; y += WAVES) {
+    const float w = WAVES == 1 ? __shfl(weight, y) : weights[y / 64][y % 64];
+    if (4 * lane >= DP) continue;
+    const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part + (y * every + at_row) * DP + 4 * lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += w == 0.f ? 0.f : w * v[i];
+  }
+  float total = weight;
+  if constexpr (WAVES > 1) {
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave) return;
+    total = weights[0][lane] + weights[1][lane] + weights[2][lane] + weights[3][lane];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = sums[0][lane][i] + sums[1][lane][i] + sums[2][lane][i] + sums[3][lane][i];
+  }
+#pragma unroll
+  for (int by = 1; by < 64; by *= 2) total += __shfl_xor(total, by);
   const float by = total == 0.f ? 0.f : 1.f / total;
   T *out = static_cast<T *>(a.out.data) + qt * a.out.token + qh * a.out.head;
   for (int i = 0; i < 4; ++i)
-    if (4 * lane + i < a.dim) out[4 * lane + i] = static_cast<T>(none ? __builtin_nanf("") : sum[i] * by);
+    if (4 * lane + i < a.dim)
+      out[4 * lane + i] = static_cast<T>(
+          none ? __builtin_nanf("") : sum[i] * by);
   if (a.lse && lane == 0) a.lse[at_row] = none ? __builtin_nanf("") : total == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
@@ -321,8 +370,8 @@ Pieces pieces_for(int64_t tokens, int64_t group, int64_t heads, int64_t batch, i
   p.waves = waves_of(tokens, group, batch, 4);
   const int64_t tiles = (std::min<int64_t>(positions, kLongest) + rows_of_tile - 1) / rows_of_tile;
   const int64_t groups = std::max<int64_t>(1, std::min(batch, tokens) * heads + tokens * group / (p.waves * 32) * heads);
-  p.least = 8;
-  p.splits = static_cast<int>(std::clamp<int64_t>((2048 + groups - 1) / groups, 1, std::max<int64_t>(1, tiles / p.least)));
+  p.least = p.waves == 1 ? 8 : 16;
+  p.splits = static_cast<int>(std::clamp<int64_t>(((p.waves == 1 ? 2048 : 1024) + groups - 1) / groups, 1, std::clamp<int64_t>(tiles / p.least, 1, kMostPieces)));
   // no more than a gigabyte of sums
   const int64_t row_bytes = tokens * heads * group * (SLOWMO_MAX_ATTENTION_DIM + 1) * 4;
   p.splits = static_cast<int>(std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(row_bytes, 1), 1, p.splits));
@@ -348,9 +397,11 @@ hipError_t launch(Args a, int32_t dtype, int waves, hipStream_t stream) {
     }
     if (a.splits > 1) {
       const int64_t every = a.tokens * a.heads * a.group;
-      for (a.first = 0; a.first < every && e == hipSuccess; a.first += 4 * kMostBlocks) {
-        k_join<T, DP><<<static_cast<u32>(std::min(kMostBlocks, (every - a.first + 3) / 4)), 256, 0, stream>>>(a, waves * 32,
-                                                                                                         L::rows);
+      const int64_t blocks = a.splits <= 32 ? (every + 3) / 4 : every;
+      for (a.first = 0; a.first < blocks && e == hipSuccess; a.first += kMostBlocks) {
+        const u32 n = static_cast<u32>(std::min(kMostBlocks, blocks - a.first));
+        if (a.splits <= 32) k_join<T, DP, 1><<<n, 256, 0, stream>>>(a, waves * 32, L::rows);
+        else k_join<T, DP, 4><<<n, 256, 0, stream>>>(a, waves * 32, L::rows);
         e = hipGetLastError();
       }
     }
@@ -515,7 +566,7 @@ bool wide_rows(const slowmo_heads &h, int32_t dim, int32_t dtype) {
 bool wide_rows(const slowmo_cache &c, int32_t dim, int32_t dtype) {
   const int64_t size = size_of(dtype);
   return dim * size % 16 == 0 && aligned(c.data, 16) && c.page_stride * size % 16 == 0 && c.token_stride * size % 16 == 0 &&
-         c.head_stride * size % 16 == 0;
+         c.head_stride * size % 16 == 0 && c.token_stride * size < (1 << 25);
 }
 
 }  // namespace attention

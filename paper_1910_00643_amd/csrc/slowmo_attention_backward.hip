@@ -20,7 +20,7 @@ struct Args {
   float scale, scale2;  // of scores; of scores to powers of two
   Mask mask;
   bool wide, clear;
-  int32_t parts;        // pieces of the rows that a tile of keys goes over
+  int32_t parts, stretch;  // stretches of a sequence's rows, and rows of one: a tile of keys has a workgroup for each
   float *lse2, *delta;  // [tokens][query heads]: lse in powers of two; g . out
   float *sums;          // [parts][keys][key heads][2][padded head]: dK and dV of a piece
 };
@@ -82,9 +82,12 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
       for (int i = 0; i < 8; ++i) delta += static_cast<float>(gf[s][i]) * static_cast<float>(of_out[i]);
     }
   }
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) settle(qf[s]), settle(gf[s]);
   delta = both_sum(delta);
   const int64_t at_row = qt * (static_cast<int64_t>(a.heads) * a.group) + qh;
-  const float lse2 = a.lse[at_row] * kLog2E;
+  float lse2 = a.lse[at_row] * kLog2E;
+  settle(lse2);
   if (mine && !high) a.lse2[at_row] = lse2, a.delta[at_row] = delta;
   if (a.dim != DP) {
     for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
@@ -98,8 +101,8 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
     auto bring = [&](int u) {
       char *to = smem + (u & 1) * 2 * L::bytes;
       const int j0 = walk.at(u) * L::rows, end = keys - 1 - j0;
-      bring_rows<T, DP>(to, k + j0 * a.k.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.k.token; });
-      bring_rows<T, DP>(to + L::bytes, v + j0 * a.v.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.v.token; });
+      bring_rows<T, DP>(to, L::rows, k + j0 * a.k.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.k.token; });
+      bring_rows<T, DP>(to + L::bytes, L::rows, v + j0 * a.v.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.v.token; });
     };
     if (walk.count) bring(0);
     for (int u = 0; u < walk.count; ++u) {
@@ -107,21 +110,24 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
       if (u + 1 < walk.count) bring(u + 1);
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
-      if (careful) tame<T, DP, NB, true>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
-      if ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks) continue;
+      if (careful) tame<T, DP, L::rows, NB>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
+      if (row0 + wave * 32 >= rows || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         f32x16 s{}, dp{};
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
           s = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s);
           dp = mma(row_frag<T, DP>(v_tile, 32 * kb + low, st, high), gf[st], dp);
         }
+        read_ahead<T, DP / 8, 1, 1, 6>();
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale2, -lse2)) * (dp[i] - delta);
         if (!all) {
+          branch();
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (!sees(sight, j0 + 32 * kb + 8 * (i / 4) + 4 * high + i % 4)) s[i] = 0.f;
@@ -132,6 +138,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
 #pragma unroll
           for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(k_tile, b, 2 * kb + half, lane), ds, acc[b]);
         }
+        read_ahead<T, 2 * NB, 1, 2, 3>();
       }
     }
     if (careful) break;
@@ -145,36 +152,78 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   store_columns<T, NB>(dq, acc, a.scale, a.dim, high, a.wide, mine);
 }
 
-// A row of a tile as the keys see it.
-template <int ROWS>
+// Rows of a tile as the keys see them.
+constexpr int kRows = 32;
 struct Stats {
-  float lse2[ROWS], delta[ROWS];
-  int position[ROWS];
+  float lse2[kRows], delta[kRows];
+  int position[kRows];
 };
 constexpr int kNowhere = INT32_MIN + 1;  // of rows past the last one
 
+// k_keys holds in shared memory its keys (their values are in registers: both would leave room for one wave of a SIMD,
+// 1152 us for 16 heads on 8192 tokens of 128) and two tiles of 32 rows, or, where rows are 1 KB, one.
 template <typename T, int DP>
-constexpr int keys_bytes() {
-  return 4 * Tile<T, DP>::bytes + 2 * static_cast<int>(sizeof(Stats<Tile<T, DP>::rows>));
-}
-
-__device__ __forceinline__ void word_to_shared(u32 shared, const float *from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(shared), "v"(from) : "memory");
-}
-
-template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void k_keys(Args a) {
+struct Keys {
   using L = Tile<T, DP>;
+  static constexpr int stages = L::row_bytes <= 512 ? 2 : 1, waves = L::row_bytes <= 512 ? 4 : 2;
+  static constexpr int tile = kRows * L::row_bytes;
+  static constexpr int bytes(int w) { return w * tile + stages * (2 * tile + static_cast<int>(sizeof(Stats))); }
+};
+
+// The rows, (token, head) by (token, head), whose queries see some key of j0..j_end, and the positions that see a key.
+struct Seen {
+  int64_t lo, hi;
+};
+// Their pieces z0 .. z0 + count - 1: without a window the stretches of a sequence's rows that they lie in, with one
+// pieces of like length.
+struct Pieces {
+  int z0, count;
+  int64_t lo, hi, per, base;
+  __device__ __forceinline__ int64_t begin(int z) const { return max(lo, base + z * per); }
+  __device__ __forceinline__ int64_t end(int z) const { return min(hi, base + (z + 1) * per); }
+};
+__device__ __forceinline__ Pieces pieces_of(const Seen &s, int window, int stretch, int parts) {
+  Pieces p{0, 1, s.lo, s.hi, stretch, 0};
+  if (s.hi <= s.lo) return p;
+  if (window) {
+    p.count = static_cast<int>(min(static_cast<int64_t>(parts), (s.hi - s.lo + stretch - 1) / stretch));
+    p.per = ((s.hi - s.lo + p.count - 1) / p.count + kRows - 1) / kRows * kRows;
+    p.base = s.lo;
+  } else {
+    p.z0 = static_cast<int>(s.lo / stretch);
+    p.count = static_cast<int>((s.hi - 1) / stretch) - p.z0 + 1;
+  }
+  return p;
+}
+__device__ __forceinline__ int from_of(const Mask &m, int key) {
+  return m.causal ? key : m.window && key >= m.sinks ? key - m.window + 1 : kNowhere + 1;
+}
+__device__ __forceinline__ int to_of(const Mask &m, int key) {
+  return m.window && key >= m.sinks ? key + m.window - 1 : INT32_MAX;
+}
+__device__ __forceinline__ Seen seen_of(const Mask &m, int group, int j0, int j_end, int far, int n) {
+  const int p_lo = from_of(m, j0), p_hi = j0 < m.sinks ? INT32_MAX : to_of(m, j_end);
+  const int64_t lo = clamped(static_cast<int64_t>(p_lo) - far, 0, n), hi = clamped(static_cast<int64_t>(p_hi) - far + 1, lo, n);
+  return {lo * group, hi * group};
+}
+
+__device__ __forceinline__ void word_to_shared(u32 shared, u32 offset, const float *base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(shared), "v"(offset), "s"(base) : "memory");
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 1)) void k_keys(Args a) {
   using frag = typename Kind<T>::frag;
-  constexpr int NB = DP / 32, RB = L::rows / 32;
+  constexpr int NB = DP / 32, S = Keys<T, DP>::stages, B = Keys<T, DP>::tile;
   extern __shared__ __align__(1024) char smem[];
   const int lane = threadIdx.x & 63, low = lane & 31, high = lane >> 5;
   const int wave = uniform(static_cast<int>(threadIdx.x >> 6)), waves = blockDim.x >> 6, width = waves * 32;
   int head;
   int64_t slot;
   if (!head_slot(a.first + blockIdx.x, a.heads, a.slots * a.parts, head, slot)) return;
-  const int part = static_cast<int>(slot % a.parts);
-  slot /= a.parts;  // the first tiles, which the most queries see, first
+  // the last rows, which the most keys are seen by, first, all tiles of keys over the same stretch of rows side by side
+  const int part = a.parts - 1 - static_cast<int>(slot / a.slots);
+  slot %= a.slots;
   const Place at = place_of(a.k_offsets, a.batch, a.keys, 1, width, slot);
   const int keys = at.n;
   const int j0 = at.tile * width;
@@ -182,143 +231,146 @@ __global__ __launch_bounds__(256, 1) void k_keys(Args a) {
   const int j = j0 + wave * 32 + low;
   const bool mine = j < keys;
   const int jc = mine ? j : keys - 1;
-  const int64_t kt = at.begin + jc;
-  T *dk = static_cast<T *>(a.dk.data) + kt * a.dk.token + head * a.dk.head;
-  T *dv = static_cast<T *>(a.dv.data) + kt * a.dv.token + head * a.dv.head;
+  // this lane's row of dK, dV: worked out where it is written, for want of registers in between
+  auto row_of = [&](const Rows &x) { return static_cast<T *>(x.data) + (at.begin + jc) * x.token + head * x.head; };
   f32x16 acck[NB], accv[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
   if (at.b == a.batch) {
     if (!a.clear || part) return;
-    store_columns<T, NB>(dk, acck, 0.f, a.dim, high, a.wide, mine);
-    store_columns<T, NB>(dv, accv, 0.f, a.dim, high, a.wide, mine);
+    store_columns<T, NB>(row_of(a.dk), acck, 0.f, a.dim, high, a.wide, mine);
+    store_columns<T, NB>(row_of(a.dv), accv, 0.f, a.dim, high, a.wide, mine);
     return;
   }
   const int64_t q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
   const int n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
   const int far = keys - n;
-  // positions of the queries that see some key of the tile, of the wave, and this lane's key
-  const int j_end = min(j0 + width, keys) - 1;
-  auto from_of = [&](int key) { return a.mask.causal ? key : a.mask.window && key >= a.mask.sinks ? key - a.mask.window + 1 : kNowhere + 1; };
-  auto to_of = [&](int key) { return a.mask.window && key >= a.mask.sinks ? key + a.mask.window - 1 : INT32_MAX; };
-  int p_lo = from_of(j0), p_hi = to_of(j_end);
-  if (j0 < a.mask.sinks) p_hi = INT32_MAX, p_lo = a.mask.causal ? j0 : kNowhere + 1;
-  const int i_lo = static_cast<int>(clamped(static_cast<int64_t>(p_lo) - far, 0, n)),
-            i_hi = static_cast<int>(clamped(static_cast<int64_t>(p_hi) - far + 1, 0, n));  // exclusive
-  const int64_t r_lo = static_cast<int64_t>(i_lo) * a.group, r_hi = static_cast<int64_t>(max(i_hi, i_lo)) * a.group;
-  const int64_t tiles = (r_hi - r_lo + L::rows - 1) / L::rows, per = (tiles + a.parts - 1) / a.parts;
-  const int64_t u0 = min(part * per, tiles), u1 = min(u0 + per, tiles);
-  const int my_lo = mine ? from_of(j) : 1, my_hi = mine ? to_of(j) : 0;
+  const Seen seen = seen_of(a.mask, a.group, j0, min(j0 + width, keys) - 1, far, n);
+  const Pieces pieces = pieces_of(seen, a.mask.window, a.stretch, a.parts);
+  if (part < pieces.z0 || part >= pieces.z0 + pieces.count) return;
+  const int64_t r_lo = pieces.begin(part), r_hi = pieces.end(part);
+  const int my_lo = mine ? from_of(a.mask, j) : 1, my_hi = mine ? to_of(a.mask, j) : 0;
   const int wj0 = j0 + wave * 32, wj1 = min(wj0 + 31, keys - 1);
   const bool whole = wj0 + 31 < keys;
 
-  frag kf[DP / 16], vf[DP / 16];
-  {
-    const T *k = static_cast<const T *>(a.k.data) + kt * a.k.token + head * a.k.head;
-    const T *v = static_cast<const T *>(a.v.data) + kt * a.v.token + head * a.v.head;
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      kf[s] = load_frag<T>(k, 16 * s + 8 * high, a.dim, a.wide);
-      vf[s] = load_frag<T>(v, 16 * s + 8 * high, a.dim, a.wide);
-    }
-  }
+  char *k_tile = smem, *ring = smem + waves * B;
   if (a.dim != DP) {
-    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < (waves + 2 * S) * B / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
+  }
+  bring_rows<T, DP>(k_tile, width, static_cast<const T *>(a.k.data) + (at.begin + j0) * a.k.token + head * a.k.head, a.dim, a.wide,
+                    [&](int r) { return min(r, keys - 1 - j0) * a.k.token; });
+  frag vf[DP / 16];
+  {
+    const T *v = row_of(a.v);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) vf[s] = load_frag<T>(v, 16 * s + 8 * high, a.dim, a.wide);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) settle(vf[s]);
   }
   const T *q = static_cast<const T *>(a.q.data) + static_cast<int64_t>(head) * a.group * a.q.head;
   const T *g = static_cast<const T *>(a.g.data) + static_cast<int64_t>(head) * a.group * a.g.head;
   const int64_t stat0 = static_cast<int64_t>(head) * a.group, per_token = static_cast<int64_t>(a.heads) * a.group;
-  using S = Stats<L::rows>;
-  S *stats = reinterpret_cast<S *>(smem + 4 * L::bytes);
+  const int t_first = static_cast<int>(r_lo / a.group), o_first = static_cast<int>(r_lo % a.group);
+  const int step_t = kRows / a.group, step_o = kRows % a.group;
+  Stats *stats = reinterpret_cast<Stats *>(ring + 2 * S * B);
   for (bool careful = false;; careful = true) {
-    auto bring = [&](int64_t u) {
-      char *to = smem + (u & 1) * 2 * L::bytes;
-      S *st = stats + (u & 1);
-      // rows r0 .. of the sequence's (token, head) rows; those past the end take the last one's place
-      const int64_t r0 = r_lo + u * L::rows, t0 = r0 / a.group;
-      const int o0 = static_cast<int>(r0 - t0 * a.group), end = static_cast<int>(min(r_hi - r0, static_cast<int64_t>(L::rows))) - 1;
-      auto split = [&](int r, int &t, int &o) {
-        const u32 x = o0 + min(r, end);
-        t = a.group == 1 ? x : __umulhi(x, a.by_group);
-        o = x - t * a.group;
+    // The next tile's first row is the head o0 of token t0; `left` rows are left.
+    int t0 = t_first, o0 = o_first;
+    int64_t left = r_hi - r_lo;
+    auto bring = [&](int u) {
+      char *to = ring + (u % S) * 2 * B;
+      Stats *st = stats + u % S;
+      const int end = static_cast<int>(min(left, static_cast<int64_t>(kRows))) - 1;  // rows past it take its place
+      auto split = [&](int r, u32 &t, u32 &o) {
+        o = o0 + min(r, end);
+        t = a.group > 1 ? __umulhi(o, a.by_group) : o;
+        o -= t * a.group;
       };
       const int64_t qt = q_begin + t0;
-      bring_rows<T, DP>(to, q + qt * a.q.token, a.dim, a.wide, [&](int r) {
-        int t, o;
+      bring_rows<T, DP>(to, kRows, q + qt * a.q.token, a.dim, a.wide, [&](int r) {
+        u32 t, o;
         split(r, t, o);
         return t * a.q.token + o * a.q.head;
       });
-      bring_rows<T, DP>(to + L::bytes, g + qt * a.g.token, a.dim, a.wide, [&](int r) {
-        int t, o;
+      bring_rows<T, DP>(to + B, kRows, g + qt * a.g.token, a.dim, a.wide, [&](int r) {
+        u32 t, o;
         split(r, t, o);
         return t * a.g.token + o * a.g.head;
       });
-      int t, o;
-      split(lane & (L::rows - 1), t, o);
-      const int64_t s = (qt + t) * per_token + stat0 + o;
-      if (lane < L::rows) {
-        if (wave == 0) word_to_shared(uniform(offset_of(st->lse2)), a.lse2 + s);
-        if (wave == waves - 1) {
-          word_to_shared(uniform(offset_of(st->delta)), a.delta + s);
-          st->position[lane] = lane <= end ? static_cast<int>(t0) + t + far : kNowhere;
-        }
+      if (lane < kRows && (wave == 0 || wave == waves - 1)) {
+        u32 t, o;
+        split(lane, t, o);
+        const u32 at = (t * static_cast<u32>(a.heads * a.group) + o) * 4;
+        const int64_t s = qt * per_token + stat0;
+        if (wave == 0) word_to_shared(uniform(offset_of(st->lse2)), at, uniform(a.lse2 + s));
+        if (wave == waves - 1) word_to_shared(uniform(offset_of(st->delta)), at, uniform(a.delta + s));
+        st->position[lane] = lane <= end ? t0 + static_cast<int>(t) + far : kNowhere;
       }
+      left -= kRows;
+      t0 += step_t, o0 += step_o;
+      if (o0 >= a.group) o0 -= a.group, ++t0;
     };
-    if (u0 < u1) bring(u0);
-    for (int64_t u = u0; u < u1; ++u) {
+    const int turns = r_hi > r_lo ? static_cast<int>((r_hi - r_lo + kRows - 1) / kRows) : 0;
+    if (S == 2 && turns) bring(0);
+    for (int u = 0; u < turns; ++u) {
+      if (S == 1) {
+        __syncthreads();
+        bring(u);
+      }
       arrive();
-      if (u + 1 < u1) bring(u + 1);
-      char *q_tile = smem + (u & 1) * 2 * L::bytes, *g_tile = q_tile + L::bytes;
-      const S *st = stats + (u & 1);
+      if (S == 2 && u + 1 < turns) bring(u + 1);
+      char *q_tile = ring + (u % S) * 2 * B, *g_tile = q_tile + B;
+      const Stats *st = stats + u % S;
       auto sees_row = [&](int r) {
         const int p = st->position[r];
         return p >= my_lo && p <= my_hi && p != kNowhere;
       };
       if (careful) {
-        tame<T, DP, NB, true>(q_tile, acck, sees_row);
-        tame<T, DP, NB, true>(g_tile, accv, sees_row);
+        tame<T, DP, kRows, NB>(q_tile, acck, sees_row);
+        tame<T, DP, kRows, NB>(g_tile, accv, sees_row);
+      }
+      const int pa = uniform(st->position[0]), pb = uniform(st->position[kRows - 1]);
+      // every row sees every key of the wave, or (rows in order, none missing) none does
+      bool all = whole && pb != kNowhere && (!a.mask.causal || wj1 <= pa);
+      bool none = pa == kNowhere || wj0 >= keys || (pb != kNowhere && a.mask.causal && wj0 > pb);
+      if (a.mask.window) {
+        all = all && (wj1 < a.mask.sinks || (pb - wj0 < a.mask.window && wj1 - pa < a.mask.window));
+        none = none || (wj0 >= a.mask.sinks && ((pa - wj1 >= a.mask.window) || (pb != kNowhere && wj0 - pb >= a.mask.window)));
+      }
+      if (none) continue;
+      f32x16 s{}, dp{};
+      // worked out anew each time: kept, the addresses would not fit the registers
+      int k_row = wave * 32 + low;
+      settle(k_row);
+#pragma unroll
+      for (int e = 0; e < DP / 16; ++e) {
+        s = mma(row_frag<T, DP>(q_tile, low, e, high), row_frag<T, DP>(k_tile, k_row, e, high), s);
+        dp = mma(row_frag<T, DP>(g_tile, low, e, high), vf[e], dp);
       }
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        const int pa = uniform(st->position[32 * rb]), pb = uniform(st->position[32 * rb + 31]);
-        // every row sees every key of the wave, or (rows in order, none missing) none does
-        bool all = whole && pb != kNowhere && (!a.mask.causal || wj1 <= pa);
-        bool none = pa == kNowhere || wj0 >= keys || (pb != kNowhere && a.mask.causal && wj0 > pb);
-        if (a.mask.window) {
-          all = all && (wj1 < a.mask.sinks || (pb - wj0 < a.mask.window && wj1 - pa < a.mask.window));
-          none = none || (wj0 >= a.mask.sinks && ((pa - wj1 >= a.mask.window) || (pb != kNowhere && wj0 - pb >= a.mask.window)));
+      for (int c = 0; c < 4; ++c) {
+        const int r = 8 * c + 4 * high;
+        const f32x4 l = *reinterpret_cast<const f32x4 *>(st->lse2 + r), d = *reinterpret_cast<const f32x4 *>(st->delta + r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[4 * c + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * c + i], a.scale2, -l[i]));
+          dp[4 * c + i] = s[4 * c + i] * (dp[4 * c + i] - d[i]);
         }
-        if (none) continue;
-        f32x16 s{}, dp{};
+      }
+      if (!all) {
+        branch();
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-          s = mma(row_frag<T, DP>(q_tile, 32 * rb + low, e, high), kf[e], s);
-          dp = mma(row_frag<T, DP>(g_tile, 32 * rb + low, e, high), vf[e], dp);
-        }
+        for (int i = 0; i < 16; ++i)
+          if (!sees_row(8 * (i / 4) + 4 * high + i % 4)) s[i] = dp[i] = 0.f;
+      }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int r = 32 * rb + 8 * c + 4 * high;
-          const f32x4 l = *reinterpret_cast<const f32x4 *>(st->lse2 + r), d = *reinterpret_cast<const f32x4 *>(st->delta + r);
+      for (int half = 0; half < 2; ++half) {
+        const frag pf = as_frag<T>(s, half), df = as_frag<T>(dp, half);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[4 * c + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * c + i], a.scale2, -l[i]));
-            dp[4 * c + i] = s[4 * c + i] * (dp[4 * c + i] - d[i]);
-          }
-          if (!all) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (!sees_row(r + i)) s[4 * c + i] = dp[4 * c + i] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const frag pf = as_frag<T>(s, half), df = as_frag<T>(dp, half);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            accv[b] = mma(column_frag<T, DP>(g_tile, b, 2 * rb + half, lane), pf, accv[b]);
-            acck[b] = mma(column_frag<T, DP>(q_tile, b, 2 * rb + half, lane), df, acck[b]);
-          }
+        for (int b = 0; b < NB; ++b) {
+          accv[b] = mma(column_frag<T, DP>(g_tile, b, half, lane), pf, accv[b]);
+          acck[b] = mma(column_frag<T, DP>(q_tile, b, half, lane), df, acck[b]);
         }
       }
     }
@@ -332,52 +384,83 @@ __global__ __launch_bounds__(256, 1) void k_keys(Args a) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
   }
-  if (a.parts == 1) {
-    store_columns<T, NB>(dk, acck, a.scale, a.dim, high, a.wide, mine);
-    store_columns<T, NB>(dv, accv, 1.f, a.dim, high, a.wide, mine);
+  if (pieces.count == 1) {
+    store_columns<T, NB>(row_of(a.dk), acck, a.scale, a.dim, high, a.wide, mine);
+    store_columns<T, NB>(row_of(a.dv), accv, 1.f, a.dim, high, a.wide, mine);
   } else {
-    float *to = a.sums + ((part * a.keys + kt) * a.heads + head) * (2 * DP);
+    float *to = a.sums + ((part * a.keys + at.begin + jc) * a.heads + head) * (2 * DP);
     store_columns<float, NB>(to, acck, a.scale, DP, high, true, mine);
     store_columns<float, NB>(to + DP, accv, 1.f, DP, high, true, mine);
   }
 }
 
-// The pieces of a key's sums added in their order; 4 elements to a lane.
+// The pieces of a key's sums added in their order: a workgroup a key of 32 keys' tile, 4 elements to a lane.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_add(Args a) {
-  constexpr int N = 2 * DP / 4;
-  const int64_t at = a.first * 256 + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t row = at / N;
-  const int e = static_cast<int>(at - row * N) * 4, d = e % DP;
-  if (row >= a.keys * a.heads || d >= a.dim) return;
-  const int64_t kt = row / a.heads;
-  const int head = static_cast<int>(row - kt * a.heads);
-  if (kt >= a.k_offsets[a.batch]) return;  // behind the last sequence
-  f32x4 sum = *reinterpret_cast<const f32x4 *>(a.sums + row * (2 * DP) + e);
-  for (int p = 1; p < a.parts; ++p) {
-    const f32x4 more = *reinterpret_cast<const f32x4 *>(a.sums + (p * a.keys * a.heads + row) * (2 * DP) + e);
+__global__ __launch_bounds__(256) void k_add(Args a, int width) {
+  constexpr int N = 2 * DP / 4, R = 256 / N;  // lanes of a key and head; such rows of a workgroup
+  int head;
+  int64_t slot;
+  // a slot of 32 rows: those of a sequence's tile of keys, so that all have the same pieces
+  if (!head_slot(a.first + blockIdx.x, a.heads, a.slots, head, slot)) return;
+  const Place at = place_of(a.k_offsets, a.batch, a.keys, 1, 32, slot);
+  const int keys = at.n, first = at.tile * 32;
+  if (at.b < 0 || at.b == a.batch || static_cast<int64_t>(at.tile) * 32 >= keys) return;
+  const int64_t q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
+  const int n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  const int j0 = first / width * width;
+  const Pieces pieces =
+      pieces_of(seen_of(a.mask, a.group, j0, min(j0 + width, keys) - 1, keys - n, n), a.mask.window, a.stretch, a.parts);
+  if (pieces.count == 1) return;
+  const int e = static_cast<int>(threadIdx.x % N) * 4, d = e % DP;
+  if (threadIdx.x >= R * N || d >= a.dim) return;
+  const Rows &to = e < DP ? a.dk : a.dv;
+  for (int j = first + threadIdx.x / N; j < min(first + 32, keys); j += R) {
+    const int64_t row = (at.begin + j) * a.heads + head;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p = pieces.z0; p < pieces.z0 + pieces.count; ++p) {
+      const f32x4 more = *reinterpret_cast<const f32x4 *>(a.sums + (p * a.keys * a.heads + row) * (2 * DP) + e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] += more[i];
+      for (int i = 0; i < 4; ++i) sum[i] += more[i];
+    }
+    T *x = static_cast<T *>(to.data) + (at.begin + j) * to.token + head * to.head + d;
+    for (int i = 0; i < 4; ++i)
+      if (d + i < a.dim) x[i] = static_cast<T>(sum[i]);
   }
-  const Rows &r = e < DP ? a.dk : a.dv;
-  T *to = static_cast<T *>(r.data) + kt * r.token + head * r.head + d;
-  for (int i = 0; i < 4; ++i)
-    if (d + i < a.dim) to[i] = static_cast<T>(sum[i]);
 }
 
 struct Plan {
-  int q_waves, k_waves, parts;
+  int q_waves, k_waves, parts, stretch;
 };
-Plan plan_for(int64_t tokens, int64_t keys, int64_t group, int64_t heads, int64_t batch, int rows_of_tile) {
+// A sequence's rows go by stretches, a workgroup for each and each tile of keys that some row of it sees: with a causal
+// mask the first keys are seen by all queries, and the sinks of a window by all but a few, and tiles of keys that
+// go over the same stretch side by side find it in their L2 (8192 tokens of 16 heads of 128, each tile of keys cut into
+// pieces of its own: 67 % of reads missed the L2, 1318 us).  How long the sequences are is not known here: the more there
+// are, the fewer of their rows one has, and each stretch too many is workgroups that find nothing to do.
+Plan plan_for(const Mask &m, int64_t tokens, int64_t keys, int64_t group, int64_t heads, int64_t batch, int row_bytes) {
   Plan p;
   p.q_waves = waves_of(tokens, group, batch, 4);
-  p.k_waves = waves_of(keys, 1, batch, 4);
-  const int64_t blocks = std::max<int64_t>(1, (keys / (p.k_waves * 32) + std::min<int64_t>(batch, keys)) * heads);
-  const int64_t tiles = tokens * group / std::max<int64_t>(batch, 1) / rows_of_tile;
-  p.parts = static_cast<int>(std::clamp<int64_t>((512 + blocks - 1) / blocks, 1, std::clamp<int64_t>(tiles / 4, 1, 16)));
+  p.k_waves = waves_of(keys, 1, batch, row_bytes > 512 ? 2 : 4);
+  const int64_t sequences = std::max<int64_t>(1, std::min(batch, keys)), width = p.k_waves * 32, n = tokens / sequences;
+  const int64_t seen = m.window ? std::min<int64_t>(n, width + (m.causal ? 1 : 2) * static_cast<int64_t>(m.window)) : m.causal ? n / 2 : n;
+  const int64_t turns = (keys / width + sequences) * heads * (seen * group / kRows + 1);
+  // pieces short enough that a round of the card's 512 workgroups is not the whole of it
+  int64_t stretch = std::clamp<int64_t>(turns / 1024, 24, 1 << 20) * kRows;
+  // no more than a gigabyte of sums
+  const int64_t layer = keys * heads * 2 * SLOWMO_MAX_ATTENTION_DIM * 4;
+  const int64_t most = std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(layer, 1), 1, batch <= 8 ? 16 : batch <= 32 ? 8 : batch <= 96 ? 4 : 2);
+  const int64_t rows = std::max<int64_t>(1, tokens * group);
+  if (m.window) {
+    // a tile with sinks may be seen by every row, the others by those of the window
+    const int64_t longest = m.sinks ? rows : (width + 2 * static_cast<int64_t>(m.window)) * group;
+    p.parts = static_cast<int>(std::clamp<int64_t>((longest + stretch - 1) / stretch, 1, most));
+  } else {
+    stretch = std::max(stretch, ((rows + most - 1) / most + kRows - 1) / kRows * kRows);
+    p.parts = static_cast<int>((rows + stretch - 1) / stretch);
+  }
+  p.stretch = static_cast<int>(std::min<int64_t>(stretch, INT32_MAX / kRows * kRows));
   return p;
 }
-int tile_rows(int dim, int32_t dtype) { return padded(dim) * static_cast<int>(size_of(dtype)) > 512 ? 32 : 64; }
+int row_bytes(int dim, int32_t dtype) { return padded(dim) * static_cast<int>(size_of(dtype)); }
 
 hipError_t run(Args a, int32_t dtype, const Plan &p, hipStream_t stream) {
   hipError_t e = hipSuccess;
@@ -399,17 +482,19 @@ hipError_t run(Args a, int32_t dtype, const Plan &p, hipStream_t stream) {
       }
     }
     if (a.keys && e == hipSuccess) {
-      room(k_keys<T, DP>, keys_bytes<T, DP>());
+      const int bytes = Keys<T, DP>::bytes(p.k_waves);
+      room(k_keys<T, DP>, bytes);
       a.slots = slots_of(a.keys, 1, p.k_waves * 32, a.batch);
       const int64_t items = items_of(a.heads, a.slots * a.parts);
       for (a.first = 0; a.first < items && e == hipSuccess; a.first += kMostBlocks) {
-        k_keys<T, DP><<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.k_waves, keys_bytes<T, DP>(), stream>>>(a);
+        k_keys<T, DP><<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.k_waves, bytes, stream>>>(a);
         e = hipGetLastError();
       }
       if (a.parts > 1) {
-        const int64_t blocks = (a.keys * a.heads * (2 * DP / 4) + 255) / 256;
+        a.slots = slots_of(a.keys, 1, 32, a.batch);
+        const int64_t blocks = items_of(a.heads, a.slots);
         for (a.first = 0; a.first < blocks && e == hipSuccess; a.first += kMostBlocks) {
-          k_add<T, DP><<<static_cast<u32>(std::min(kMostBlocks, blocks - a.first)), 256, 0, stream>>>(a);
+          k_add<T, DP><<<static_cast<u32>(std::min(kMostBlocks, blocks - a.first)), 256, 0, stream>>>(a, p.k_waves * 32);
           e = hipGetLastError();
         }
       }
@@ -434,7 +519,7 @@ size_t slowmo_attention_backward_bytes(const slowmo_attention_config *cfg, int32
   if (check_config(cfg) || batch < 0 || tokens < 0 || keys < 0 || tokens > kLongest || keys > kLongest || q_heads < 1 ||
       k_heads < 1 || q_heads > (1 << 20) || q_heads % k_heads)
     return 0;
-  const Plan p = plan_for(tokens, keys, q_heads / k_heads, k_heads, batch, tile_rows(cfg->head_dim, cfg->dtype));
+  const Plan p = plan_for(mask_of(*cfg), tokens, keys, q_heads / k_heads, k_heads, batch, row_bytes(cfg->head_dim, cfg->dtype));
   return 2 * stat_bytes(tokens, q_heads) +
          (p.parts > 1 ? static_cast<size_t>(p.parts) * keys * k_heads * 2 * padded(cfg->head_dim) * sizeof(float) : 0);
 }
@@ -489,8 +574,8 @@ slowmo_status slowmo_attention_backward(const slowmo_attention_config *cfg, int3
     a.wide = true;
     for (const slowmo_heads *h : in) a.wide = a.wide && wide_rows(*h, d, dt);
     for (const slowmo_heads *h : written) a.wide = a.wide && wide_rows(*h, d, dt);
-    const Plan p = plan_for(tokens, keys, a.group, a.heads, batch, tile_rows(d, dt));
-    a.parts = p.parts;
+    const Plan p = plan_for(a.mask, tokens, keys, a.group, a.heads, batch, row_bytes(d, dt));
+    a.parts = p.parts, a.stretch = p.stretch;
     a.lse2 = static_cast<float *>(workspace);
     a.delta = a.lse2 + stat_bytes(tokens, q->heads) / 4;
     a.sums = a.delta + stat_bytes(tokens, q->heads) / 4;
