@@ -25,6 +25,7 @@ namespace slowmo {
 namespace attention {
 
 using u32 = uint32_t;
+#define SLOWMO_INLINE __attribute__((always_inline))  // of lambdas: what they refer to would go through memory otherwise
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -318,30 +319,54 @@ struct Place {
   int64_t begin;
 };
 __device__ __forceinline__ int64_t clamped(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+__device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
+  const u32x2 w = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(int64_t, u32x2{static_cast<u32>(__builtin_amdgcn_readlane(w[0], lane)),
+                                           static_cast<u32>(__builtin_amdgcn_readlane(w[1], lane))});
+}
+// Four lanes' worth of entries are asked for at once: one trip to memory for up to 255 sequences.
 __device__ __forceinline__ Place place_of(const int64_t *offsets, int batch, int64_t tokens, int group, int height,
                                           int64_t slot) {
-  const int lane = threadIdx.x & 63;
-  int count = 0;
-  for (int first = 0; first <= batch; first += 64) {
-    const int b = first + lane;
-    bool mine = b <= batch;
-    if (mine) mine = clamped(offsets[b], 0, tokens) * group / height + b <= slot;
-    const int got = __popcll(__ballot(mine));
-    count += got;
+  const int lane = threadIdx.x & 63, shift = __builtin_ctz(height);
+  Place p{-1, 0, 0, 0};
+  int64_t end = tokens;
+  for (int first = 0; first <= batch; first += 256) {
+    int64_t v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      v[c] = first + 64 * c <= batch ? clamped(offsets[min(first + 64 * c + lane, batch)], 0, tokens) : 0;
+    int got = 64;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int b = first + 64 * c + lane;
+      if (got < 64 || first + 64 * c > batch) continue;
+      got = __popcll(__ballot(b <= batch && (v[c] * group >> shift) + b <= slot));
+      if (got) p.b = first + 64 * c + got - 1, p.begin = lane_of(v[c], got - 1);
+      if (got < 64 && p.b < batch) end = lane_of(v[c], got);
+    }
     if (got < 64) break;
   }
-  Place p;
-  p.b = uniform(count - 1);
-  if (p.b < 0) {
-    p.n = 0, p.tile = 0, p.begin = 0;
-    return p;
-  }
-  p.begin = clamped(uniform(offsets[p.b]), 0, tokens);
-  const int64_t end = p.b < batch ? clamped(uniform(offsets[p.b + 1]), p.begin, tokens) : tokens;
+  if (p.b < 0) return p;
+  end = p.b < batch ? max(end, p.begin) : tokens;
   p.n = static_cast<int>(end - p.begin);
-  p.tile = static_cast<int>(slot - p.b - p.begin * group / height);
+  p.tile = static_cast<int>(slot - p.b - (p.begin * group >> shift));
   return p;
 }
+
+// Rows, token by token and head by head within, from row0 on as tokens and heads: by one division for a workgroup.
+struct Split {
+  int t0, o0, group;
+  u32 by_group;  // 2^32 / group, rounded up: exact for what is asked here, o0 and some hundred rows
+  __device__ __forceinline__ Split(int64_t row0, int group, u32 by_group) : group(group), by_group(by_group) {
+    if (group == 1) t0 = static_cast<int>(row0), o0 = 0;
+    else if (row0 >> 32) t0 = static_cast<int>(row0 / group), o0 = static_cast<int>(row0 - static_cast<int64_t>(t0) * group);
+    else t0 = static_cast<int>(static_cast<u32>(row0) / static_cast<u32>(group)), o0 = static_cast<int>(row0) - t0 * group;
+  }
+  __device__ __forceinline__ int token(int r) const { return t0 + (group > 1 ? __umulhi(o0 + r, by_group) : r); }
+  __device__ __forceinline__ int head(int r, int token) const { return o0 + r - (token - t0) * group; }
+};
+inline u32 by_group(int group) { return static_cast<u32>(((uint64_t(1) << 32) + group - 1) / group); }
+
 inline int64_t slots_of(int64_t tokens, int64_t group, int64_t height, int64_t batch) {
   return tokens * group / height + batch + 1;
 }
@@ -403,7 +428,7 @@ __device__ __forceinline__ T *element(char *tile, int row, int d) {
 // tile: what is wild is added to the columns that see it and then taken out of the tile.  `seen(row)`: whether the
 // lane's column sees the tile's row.  All waves of the workgroup come here.
 template <typename T, int DP, int ROWS, int NB, typename F>
-__device__ void tame(char *tile, f32x16 (&acc)[NB], F &&seen) {
+__device__ __forceinline__ void tame(char *tile, f32x16 (&acc)[NB], F &&seen) {
   const int high = (threadIdx.x & 63) >> 5;
   int any = 0;
   for (int i = threadIdx.x; i < ROWS * DP; i += blockDim.x)

@@ -20,6 +20,7 @@ struct Args {
   int64_t pages_stride, k_page, v_page;  // elements from one page to the next
   int32_t columns, n_pages, page_log2;
   int32_t batch, heads, group, dim;
+  u32 by_group;
   int64_t tokens, keys, first, slots;
   float scale;  // of scores to powers of two
   Mask mask;
@@ -75,7 +76,7 @@ struct Stage {
     if ((1 << a.page_log2) >= R && j0 + L::rows <= keys &&
         __all(static_cast<u32>(page) < static_cast<u32>(a.n_pages))) {
       const u32 step = static_cast<u32>(x.token) * sizeof(T);
-      auto piece = [&](int n) {
+      auto piece = [&](int n) SLOWMO_INLINE {
         const int row0 = n * R, row = row0 + lane / L::C, c = (lane & (L::C - 1)) ^ L::turn(row);
         const int id = __builtin_amdgcn_readlane(page, row0);
         const T *from = base + static_cast<int64_t>(id) * page_stride + ((j0 + row0) & ((1 << a.page_log2) - 1)) * x.token;
@@ -126,10 +127,10 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
   const int64_t row0 = static_cast<int64_t>(at.tile) * height;
   if (at.b < 0 || row0 >= rows) return;
   // this lane's row
-  const int64_t row = row0 + wave * 32 + low;
-  const bool mine = row < rows;
-  const int64_t there = mine ? row : rows - 1;
-  const int token = static_cast<int>(there / a.group), of = static_cast<int>(there - static_cast<int64_t>(token) * a.group);
+  const int row = wave * 32 + low, last_row = static_cast<int>(min(rows - row0, static_cast<int64_t>(height))) - 1;
+  const bool mine = row <= last_row, idle = wave * 32 > last_row;
+  const Split split_row(row0, a.group, a.by_group);
+  const int token = split_row.token(min(row, last_row)), of = split_row.head(min(row, last_row), token);
   const int64_t qt = at.begin + token;
   const int qh = head * a.group + of;
   T *out = static_cast<T *>(a.out.data) + qt * a.out.token + qh * a.out.head;
@@ -143,17 +144,16 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
     if (lse && mine && !high) *lse = -INFINITY;
     return;
   }
-  int64_t k_begin = 0;
-  int keys;
+  int64_t k_begin = at.begin;
+  int keys = at.n;
   if constexpr (PAGED) {
     keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b]), 0, kLongest));
-  } else {
+  } else if (a.k_offsets != a.q_offsets) {
     k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
     keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
   }
   const int far = keys - at.n;
-  const int64_t row_last = min(row0 + height, rows) - 1;
-  const int p_lo = static_cast<int>(row0 / a.group) + far, p_hi = static_cast<int>(row_last / a.group) + far;
+  const int p_lo = split_row.t0 + far, p_hi = split_row.token(last_row) + far;
   const Walk walk = walk_of(a.mask, p_lo, p_hi, keys, L::rows);
   int per;
   const int pieces = pieces_of(walk.count, a.splits, a.least, per);
@@ -161,11 +161,29 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
   const int u0 = split * per, u1 = min(walk.count, u0 + per);
   const Sight sight = sight_of(a.mask, token + far, keys);
   // what the whole wave sees of every row: between the bounds of its first and last row
-  const int64_t w0 = min(row0 + wave * 32, rows - 1), w1 = min(row0 + wave * 32 + 31, rows - 1);
-  const Sight first = sight_of(a.mask, uniform(static_cast<int>(w0 / a.group)) + far, keys),
-              last = sight_of(a.mask, uniform(static_cast<int>(w1 / a.group)) + far, keys);
-
-  const bool idle = row0 + wave * 32 >= rows;
+  const Sight first = sight_of(a.mask, split_row.token(min(wave * 32, last_row)) + far, keys),
+              last = sight_of(a.mask, split_row.token(min(wave * 32 + 31, last_row)) + far, keys);
+  if (a.dim != DP) {  // the rows' ends that no load writes
+    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  const Stage<T, DP, PAGED> stage{a, keys, lane, wave, waves};
+  int page = 0;
+  auto bring = [&](int u) SLOWMO_INLINE {
+    char *to = smem + (u & 1) * 2 * L::bytes;
+    const int j0 = walk.at(u) * L::rows;
+    if constexpr (PAGED) settle(page);
+    stage.template load<false>(to, a.k, a.k_page, k_begin, head, j0, page);
+    stage.template load<true>(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
+    if constexpr (PAGED)
+      if (u + 1 < u1) page = stage.page_at(at.b, walk.at(u + 1) * L::rows);
+  };
+  auto start = [&]() SLOWMO_INLINE {
+    if (u0 >= u1) return;
+    if constexpr (PAGED) page = stage.page_at(at.b, walk.at(u0) * L::rows);
+    bring(u0);
+  };
+  start();  // beside the queries
   frag qf[DP / 16];
   {
     const T *q = static_cast<const T *>(a.q.data) + qt * a.q.token + qh * a.q.head;
@@ -174,37 +192,15 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) settle(qf[s]);
   }
-  if (a.dim != DP) {  // the rows' ends that no load writes
-    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
-    __syncthreads();
-  }
-  const Stage<T, DP, PAGED> stage{a, keys, lane, wave, waves};
   float m, l;
   for (bool careful = false;; careful = true) {
+    if (careful) start();
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     m = -INFINITY, l = 0.f;
-    int page = 0;
-    auto bring = [&](int u) {
-      char *to = smem + (u & 1) * 2 * L::bytes;
-      const int j0 = walk.at(u) * L::rows;
-      if constexpr (PAGED) settle(page);
-      stage.template load<false>(to, a.k, a.k_page, k_begin, head, j0, page);
-      stage.template load<true>(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
-    };
-    if (u0 < u1) {
-      if constexpr (PAGED) page = stage.page_at(at.b, walk.at(u0) * L::rows);
-      bring(u0);
-      if constexpr (PAGED)
-        if (u0 + 1 < u1) page = stage.page_at(at.b, walk.at(u0 + 1) * L::rows);
-    }
     for (int u = u0; u < u1; ++u) {
       arrive();
-      if (u + 1 < u1) {
-        bring(u + 1);
-        if constexpr (PAGED)
-          if (u + 2 < u1) page = stage.page_at(at.b, walk.at(u + 2) * L::rows);
-      }
+      if (u + 1 < u1) bring(u + 1);
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
       if (careful)
@@ -215,10 +211,18 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+      // Products of fp32 are 16 times as long: those of keys past the last one, and of elements past the head's end, are
+      // left out.
+      constexpr bool kLong = sizeof(T) == 4;
 #pragma unroll
-      for (int st = 0; st < DP / 16; ++st)
+      for (int st = 0; st < DP / 16; ++st) {
+        if (kLong && 16 * st >= a.dim) continue;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s[kb]);
+        for (int kb = 0; kb < KB; ++kb) {
+          if (kLong && j0 + 32 * kb >= keys) continue;
+          s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s[kb]);
+        }
+      }
       read_ahead<T, KB * DP / 16, 1, 1, 6>();
       if (!((j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks)) {
         branch();
@@ -255,6 +259,7 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
         }
 #pragma unroll
       for (int st = 0; st < L::rows / 16; ++st) {
+        if (kLong && j0 + 16 * st >= keys) continue;
         const frag p = as_frag<T>(s[st / 2], st % 2);
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, lane), p, acc[b]);
@@ -411,7 +416,7 @@ hipError_t launch(Args a, int32_t dtype, int waves, hipStream_t stream) {
 
 void fill(Args &a, const slowmo_attention_config &c, int64_t tokens, const slowmo_heads &q, const slowmo_heads &out, int heads) {
   a.q = rows_of(q), a.out = rows_of(out);
-  a.heads = heads, a.group = q.heads / heads, a.dim = c.head_dim, a.tokens = tokens;
+  a.heads = heads, a.group = q.heads / heads, a.by_group = by_group(a.group), a.dim = c.head_dim, a.tokens = tokens;
   a.scale = c.scale * kLog2E;
   a.mask = mask_of(c);
   a.clear = c.clear_rest != 0;

@@ -43,10 +43,10 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   const Place at = place_of(a.q_offsets, a.batch, a.tokens, a.group, height, slot);
   const int64_t rows = static_cast<int64_t>(at.n) * a.group, row0 = static_cast<int64_t>(at.tile) * height;
   if (at.b < 0 || row0 >= rows) return;
-  const int64_t row = row0 + wave * 32 + low;
-  const bool mine = row < rows;
-  const int64_t there = mine ? row : rows - 1;
-  const int token = static_cast<int>(there / a.group), of = static_cast<int>(there - static_cast<int64_t>(token) * a.group);
+  const int row = wave * 32 + low, last_row = static_cast<int>(min(rows - row0, static_cast<int64_t>(height))) - 1;
+  const bool mine = row <= last_row, idle = wave * 32 > last_row;
+  const Split split(row0, a.group, a.by_group);
+  const int token = split.token(min(row, last_row)), of = split.head(min(row, last_row), token);
   const int64_t qt = at.begin + token;
   const int qh = head * a.group + of;
   T *dq = static_cast<T *>(a.dq.data) + qt * a.dq.token + qh * a.dq.head;
@@ -58,15 +58,30 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
     store_columns<T, NB>(dq, acc, 0.f, a.dim, high, a.wide, mine);
     return;
   }
-  const int64_t k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
-  const int keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
+  int64_t k_begin = at.begin;
+  int keys = at.n;
+  if (a.k_offsets != a.q_offsets) {
+    k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
+    keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
+  }
   const int far = keys - at.n;
-  const int64_t row_last = min(row0 + height, rows) - 1;
-  const Walk walk = walk_of(a.mask, static_cast<int>(row0 / a.group) + far, static_cast<int>(row_last / a.group) + far, keys, L::rows);
+  const Walk walk = walk_of(a.mask, split.t0 + far, split.token(last_row) + far, keys, L::rows);
   const Sight sight = sight_of(a.mask, token + far, keys);
-  const int64_t w0 = min(row0 + wave * 32, rows - 1), w1 = min(row0 + wave * 32 + 31, rows - 1);
-  const Sight first = sight_of(a.mask, uniform(static_cast<int>(w0 / a.group)) + far, keys),
-              last = sight_of(a.mask, uniform(static_cast<int>(w1 / a.group)) + far, keys);
+  const Sight first = sight_of(a.mask, split.token(min(wave * 32, last_row)) + far, keys),
+              last = sight_of(a.mask, split.token(min(wave * 32 + 31, last_row)) + far, keys);
+  if (a.dim != DP) {
+    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  const T *k = static_cast<const T *>(a.k.data) + k_begin * a.k.token + head * a.k.head;
+  const T *v = static_cast<const T *>(a.v.data) + k_begin * a.v.token + head * a.v.head;
+  auto bring = [&](int u) SLOWMO_INLINE {
+    char *to = smem + (u & 1) * 2 * L::bytes;
+    const int j0 = walk.at(u) * L::rows, end = keys - 1 - j0;
+    bring_rows<T, DP>(to, L::rows, k + j0 * a.k.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.k.token; });
+    bring_rows<T, DP>(to + L::bytes, L::rows, v + j0 * a.v.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.v.token; });
+  };
+  if (walk.count) bring(0);  // beside the queries
   frag qf[DP / 16], gf[DP / 16];
   float delta = 0.f;
   {
@@ -89,29 +104,17 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   float lse2 = a.lse[at_row] * kLog2E;
   settle(lse2);
   if (mine && !high) a.lse2[at_row] = lse2, a.delta[at_row] = delta;
-  if (a.dim != DP) {
-    for (int i = threadIdx.x; i < 4 * L::bytes / 16; i += blockDim.x) reinterpret_cast<u32x4 *>(smem)[i] = u32x4{0, 0, 0, 0};
-    __syncthreads();
-  }
-  const T *k = static_cast<const T *>(a.k.data) + k_begin * a.k.token + head * a.k.head;
-  const T *v = static_cast<const T *>(a.v.data) + k_begin * a.v.token + head * a.v.head;
   for (bool careful = false;; careful = true) {
+    if (careful && walk.count) bring(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
-    auto bring = [&](int u) {
-      char *to = smem + (u & 1) * 2 * L::bytes;
-      const int j0 = walk.at(u) * L::rows, end = keys - 1 - j0;
-      bring_rows<T, DP>(to, L::rows, k + j0 * a.k.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.k.token; });
-      bring_rows<T, DP>(to + L::bytes, L::rows, v + j0 * a.v.token, a.dim, a.wide, [&](int r) { return min(r, end) * a.v.token; });
-    };
-    if (walk.count) bring(0);
     for (int u = 0; u < walk.count; ++u) {
       arrive();
       if (u + 1 < walk.count) bring(u + 1);
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
       if (careful) tame<T, DP, L::rows, NB>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
-      if (row0 + wave * 32 >= rows || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
+      if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
@@ -232,7 +235,7 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
   const bool mine = j < keys;
   const int jc = mine ? j : keys - 1;
   // this lane's row of dK, dV: worked out where it is written, for want of registers in between
-  auto row_of = [&](const Rows &x) { return static_cast<T *>(x.data) + (at.begin + jc) * x.token + head * x.head; };
+  auto row_of = [&](const Rows &x) SLOWMO_INLINE { return static_cast<T *>(x.data) + (at.begin + jc) * x.token + head * x.head; };
   f32x16 acck[NB], accv[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
@@ -242,8 +245,12 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
     store_columns<T, NB>(row_of(a.dv), accv, 0.f, a.dim, high, a.wide, mine);
     return;
   }
-  const int64_t q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
-  const int n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  int64_t q_begin = at.begin;
+  int n = keys;
+  if (a.k_offsets != a.q_offsets) {
+    q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
+    n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  }
   const int far = keys - n;
   const Seen seen = seen_of(a.mask, a.group, j0, min(j0 + width, keys) - 1, far, n);
   const Pieces pieces = pieces_of(seen, a.mask.window, a.stretch, a.parts);
@@ -260,6 +267,50 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
   }
   bring_rows<T, DP>(k_tile, width, static_cast<const T *>(a.k.data) + (at.begin + j0) * a.k.token + head * a.k.head, a.dim, a.wide,
                     [&](int r) { return min(r, keys - 1 - j0) * a.k.token; });
+  const T *q = static_cast<const T *>(a.q.data) + static_cast<int64_t>(head) * a.group * a.q.head;
+  const T *g = static_cast<const T *>(a.g.data) + static_cast<int64_t>(head) * a.group * a.g.head;
+  const int64_t stat0 = static_cast<int64_t>(head) * a.group, per_token = static_cast<int64_t>(a.heads) * a.group;
+  const Split split(r_lo, a.group, a.by_group);
+  const int step_t = kRows / a.group, step_o = kRows % a.group;
+  Stats *stats = reinterpret_cast<Stats *>(ring + 2 * S * B);
+  // The next tile's first row is the head o0 of token t0; `left` rows are left.
+  int t0 = split.t0, o0 = split.o0;
+  int64_t left = r_hi - r_lo;
+  auto bring = [&](int u) SLOWMO_INLINE {
+    char *to = ring + (u % S) * 2 * B;
+    Stats *st = stats + u % S;
+    const int end = static_cast<int>(min(left, static_cast<int64_t>(kRows))) - 1;  // rows past it take its place
+    auto part_row = [&](int r, u32 &t, u32 &o) SLOWMO_INLINE {
+      o = o0 + min(r, end);
+      t = a.group > 1 ? __umulhi(o, a.by_group) : o;
+      o -= t * a.group;
+    };
+    const int64_t qt = q_begin + t0;
+    bring_rows<T, DP>(to, kRows, q + qt * a.q.token, a.dim, a.wide, [&](int r) {
+      u32 t, o;
+      part_row(r, t, o);
+      return t * a.q.token + o * a.q.head;
+    });
+    bring_rows<T, DP>(to + B, kRows, g + qt * a.g.token, a.dim, a.wide, [&](int r) {
+      u32 t, o;
+      part_row(r, t, o);
+      return t * a.g.token + o * a.g.head;
+    });
+    if (lane < kRows && (wave == 0 || wave == waves - 1)) {
+      u32 t, o;
+      part_row(lane, t, o);
+      const u32 at = (t * static_cast<u32>(a.heads * a.group) + o) * 4;
+      const int64_t s = qt * per_token + stat0;
+      if (wave == 0) word_to_shared(uniform(offset_of(st->lse2)), at, uniform(a.lse2 + s));
+      if (wave == waves - 1) word_to_shared(uniform(offset_of(st->delta)), at, uniform(a.delta + s));
+      st->position[lane] = lane <= end ? t0 + static_cast<int>(t) + far : kNowhere;
+    }
+    left -= kRows;
+    t0 += step_t, o0 += step_o;
+    if (o0 >= a.group) o0 -= a.group, ++t0;
+  };
+  const int turns = r_hi > r_lo ? static_cast<int>((r_hi - r_lo + kRows - 1) / kRows) : 0;
+  if (S == 2 && turns) bring(0);
   frag vf[DP / 16];
   {
     const T *v = row_of(a.v);
@@ -268,51 +319,11 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) settle(vf[s]);
   }
-  const T *q = static_cast<const T *>(a.q.data) + static_cast<int64_t>(head) * a.group * a.q.head;
-  const T *g = static_cast<const T *>(a.g.data) + static_cast<int64_t>(head) * a.group * a.g.head;
-  const int64_t stat0 = static_cast<int64_t>(head) * a.group, per_token = static_cast<int64_t>(a.heads) * a.group;
-  const int t_first = static_cast<int>(r_lo / a.group), o_first = static_cast<int>(r_lo % a.group);
-  const int step_t = kRows / a.group, step_o = kRows % a.group;
-  Stats *stats = reinterpret_cast<Stats *>(ring + 2 * S * B);
   for (bool careful = false;; careful = true) {
-    // The next tile's first row is the head o0 of token t0; `left` rows are left.
-    int t0 = t_first, o0 = o_first;
-    int64_t left = r_hi - r_lo;
-    auto bring = [&](int u) {
-      char *to = ring + (u % S) * 2 * B;
-      Stats *st = stats + u % S;
-      const int end = static_cast<int>(min(left, static_cast<int64_t>(kRows))) - 1;  // rows past it take its place
-      auto split = [&](int r, u32 &t, u32 &o) {
-        o = o0 + min(r, end);
-        t = a.group > 1 ? __umulhi(o, a.by_group) : o;
-        o -= t * a.group;
-      };
-      const int64_t qt = q_begin + t0;
-      bring_rows<T, DP>(to, kRows, q + qt * a.q.token, a.dim, a.wide, [&](int r) {
-        u32 t, o;
-        split(r, t, o);
-        return t * a.q.token + o * a.q.head;
-      });
-      bring_rows<T, DP>(to + B, kRows, g + qt * a.g.token, a.dim, a.wide, [&](int r) {
-        u32 t, o;
-        split(r, t, o);
-        return t * a.g.token + o * a.g.head;
-      });
-      if (lane < kRows && (wave == 0 || wave == waves - 1)) {
-        u32 t, o;
-        split(lane, t, o);
-        const u32 at = (t * static_cast<u32>(a.heads * a.group) + o) * 4;
-        const int64_t s = qt * per_token + stat0;
-        if (wave == 0) word_to_shared(uniform(offset_of(st->lse2)), at, uniform(a.lse2 + s));
-        if (wave == waves - 1) word_to_shared(uniform(offset_of(st->delta)), at, uniform(a.delta + s));
-        st->position[lane] = lane <= end ? t0 + static_cast<int>(t) + far : kNowhere;
-      }
-      left -= kRows;
-      t0 += step_t, o0 += step_o;
-      if (o0 >= a.group) o0 -= a.group, ++t0;
-    };
-    const int turns = r_hi > r_lo ? static_cast<int>((r_hi - r_lo + kRows - 1) / kRows) : 0;
-    if (S == 2 && turns) bring(0);
+    if (careful) {
+      t0 = split.t0, o0 = split.o0, left = r_hi - r_lo;
+      if (S == 2 && turns) bring(0);
+    }
     for (int u = 0; u < turns; ++u) {
       if (S == 1) {
         __syncthreads();
@@ -322,7 +333,7 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
       if (S == 2 && u + 1 < turns) bring(u + 1);
       char *q_tile = ring + (u % S) * 2 * B, *g_tile = q_tile + B;
       const Stats *st = stats + u % S;
-      auto sees_row = [&](int r) {
+      auto sees_row = [&](int r) SLOWMO_INLINE {
         const int p = st->position[r];
         return p >= my_lo && p <= my_hi && p != kNowhere;
       };
@@ -405,8 +416,12 @@ __global__ __launch_bounds__(256) void k_add(Args a, int width) {
   const Place at = place_of(a.k_offsets, a.batch, a.keys, 1, 32, slot);
   const int keys = at.n, first = at.tile * 32;
   if (at.b < 0 || at.b == a.batch || static_cast<int64_t>(at.tile) * 32 >= keys) return;
-  const int64_t q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
-  const int n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  int64_t q_begin = at.begin;
+  int n = keys;
+  if (a.k_offsets != a.q_offsets) {
+    q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
+    n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
+  }
   const int j0 = first / width * width;
   const Pieces pieces =
       pieces_of(seen_of(a.mask, a.group, j0, min(j0 + width, keys) - 1, keys - n, n), a.mask.window, a.stretch, a.parts);
@@ -566,7 +581,7 @@ slowmo_status slowmo_attention_backward(const slowmo_attention_config *cfg, int3
     a.dq = rows_of(*dq), a.dk = rows_of(*dk), a.dv = rows_of(*dv);
     a.lse = lse, a.q_offsets = q_offsets, a.k_offsets = k_offsets ? k_offsets : q_offsets;
     a.batch = batch, a.heads = k->heads, a.group = q->heads / k->heads, a.dim = d;
-    a.by_group = static_cast<u32>(((uint64_t(1) << 32) + a.group - 1) / a.group);
+    a.by_group = by_group(a.group);
     a.tokens = tokens, a.keys = keys;
     a.scale = cfg->scale, a.scale2 = cfg->scale * kLog2E;
     a.mask = mask_of(*cfg);
