@@ -58,7 +58,8 @@ struct Tile {
   static constexpr int used = DP / E;
   static constexpr int C = used <= 4 ? 4 : used <= 8 ? 8 : used <= 16 ? 16 : used <= 32 ? 32 : 64;
   static constexpr int row_bytes = C * 16;
-  static constexpr int rows = row_bytes <= 512 ? 64 : 32;   // of a tile: at most 32 KB
+  // of a tile: at most 32 KB, of fp32 16, so that two workgroups of up to 128 elements share a compute unit
+  static constexpr int rows = row_bytes <= (sizeof(T) == 2 ? 512 : 256) ? 64 : 32;
   static constexpr int bytes = rows * row_bytes;
   static __device__ __forceinline__ int turn(int row) {
     if constexpr (C >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
@@ -493,6 +494,12 @@ void dispatch(int32_t dtype, int dim, F &&f) {
   else with_kind<256>(dtype, f);
 }
 inline int padded(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256; }
+
+inline int rows_of_tile(int dim, int32_t dtype) {
+  int rows = 0;
+  dispatch(dtype, dim, [&](auto kind, auto dp) { rows = Tile<decltype(kind), dp()>::rows; });
+  return rows;
+}
 
 // Waves of a workgroup: as many as a sequence's rows fill on the average.
 inline int waves_of(int64_t tokens, int64_t group, int64_t batch, int most) {

@@ -104,12 +104,10 @@ struct Stage {
   }
 };
 
-// 256 registers a lane let two waves share a SIMD; wider heads and fp32 take up to 512.
-template <typename T, int DP>
-constexpr int kWaves = sizeof(T) == 2 && DP <= 128 ? 8 : 4;
+// 256 registers a lane let two waves share a SIMD; wider heads take up to 512.
 
 template <typename T, int DP, bool PAGED>
-__global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 ? 2 : 1)) void k_attention(Args a) {
+__global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) {
   using L = Tile<T, DP>;
   using frag = typename Kind<T>::frag;
   constexpr int NB = DP / 32, KB = L::rows / 32;
@@ -207,6 +205,10 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
         tame<T, DP, L::rows, NB>(v_tile, acc, [&](int r) { return sees(sight, j0 + r); });
       // the wave has no row, or none that sees a key of the tile
       if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
+      // Wide heads: addresses are worked out anew for each tile; kept, they would be spilled to scratch, and reading them
+      // back would wait for the tiles under way.
+      int row_lane = low, column_lane = lane;
+      if constexpr (DP * sizeof(T) >= 384) settle(row_lane), settle(column_lane);
       f32x16 s[KB];
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -220,7 +222,7 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           if (kLong && j0 + 32 * kb >= keys) continue;
-          s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s[kb]);
+          s[kb] = mma(row_frag<T, DP>(k_tile, 32 * kb + row_lane, st, high), qf[st], s[kb]);
         }
       }
       read_ahead<T, KB * DP / 16, 1, 1, 6>();
@@ -262,7 +264,7 @@ __global__ __launch_bounds__((64 * kWaves<T, DP>), (sizeof(T) == 2 && DP <= 128 
         if (kLong && j0 + 16 * st >= keys) continue;
         const frag p = as_frag<T>(s[st / 2], st % 2);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, lane), p, acc[b]);
+        for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, column_lane), p, acc[b]);
       }
       read_ahead<T, NB * L::rows / 16, 1, 2, 3>();
     }
@@ -619,7 +621,7 @@ size_t slowmo_paged_attention_bytes(const slowmo_attention_config *cfg, const sl
       k_cache->heads <= 0 || q_heads % k_cache->heads || pages->batch <= 0 || pages->columns < 0 || k_cache->page <= 0)
     return 0;
   const int dp = padded(cfg->head_dim);
-  const int rows = dp * static_cast<int>(size_of(cfg->dtype)) > 512 ? 32 : 64;
+  const int rows = rows_of_tile(cfg->head_dim, cfg->dtype);
   const Pieces p = pieces_for(tokens, q_heads / k_cache->heads, k_cache->heads, pages->batch,
                               static_cast<int64_t>(pages->columns) * k_cache->page, rows);
   return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * tokens * q_heads * (dp + 1) * sizeof(float);
@@ -667,7 +669,7 @@ slowmo_status slowmo_paged_attention(const slowmo_attention_config *cfg, const s
     while ((1 << a.page_log2) < k_cache->page) ++a.page_log2;
     a.wide = wide_rows(*q, cfg->head_dim, cfg->dtype) && wide_rows(*out, cfg->head_dim, cfg->dtype) &&
              wide_rows(*k_cache, cfg->head_dim, cfg->dtype) && wide_rows(*v_cache, cfg->head_dim, cfg->dtype);
-    const int dp = padded(cfg->head_dim), rows = dp * static_cast<int>(size_of(cfg->dtype)) > 512 ? 32 : 64;
+    const int dp = padded(cfg->head_dim), rows = rows_of_tile(cfg->head_dim, cfg->dtype);
     const Pieces p = pieces_for(tokens, a.group, a.heads, pages->batch, static_cast<int64_t>(pages->columns) * k_cache->page, rows);
     a.splits = p.splits, a.least = p.least;
     a.part = static_cast<float *>(workspace);

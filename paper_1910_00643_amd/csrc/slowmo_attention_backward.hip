@@ -26,7 +26,7 @@ struct Args {
 };
 
 template <typename T, int DP>
-constexpr bool kTwoWaves = sizeof(T) == 2 && DP <= 128;  // 256 registers a lane are enough for two waves of a SIMD
+constexpr bool kTwoWaves = DP <= (sizeof(T) == 2 ? 128 : 64);  // 256 registers a lane are enough for two waves of a SIMD
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Args a) {
@@ -116,14 +116,17 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
       if (careful) tame<T, DP, L::rows, NB>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
       if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
+      // wide heads: addresses worked out anew for each tile; kept, they would be spilled to scratch
+      int row_lane = low, column_lane = lane;
+      if constexpr (DP * sizeof(T) >= 384) settle(row_lane), settle(column_lane);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         f32x16 s{}, dp{};
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
-          s = mma(row_frag<T, DP>(k_tile, 32 * kb + low, st, high), qf[st], s);
-          dp = mma(row_frag<T, DP>(v_tile, 32 * kb + low, st, high), gf[st], dp);
+          s = mma(row_frag<T, DP>(k_tile, 32 * kb + row_lane, st, high), qf[st], s);
+          dp = mma(row_frag<T, DP>(v_tile, 32 * kb + row_lane, st, high), gf[st], dp);
         }
         read_ahead<T, DP / 8, 1, 1, 6>();
 #pragma unroll
@@ -139,7 +142,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
         for (int half = 0; half < 2; ++half) {
           const frag ds = as_frag<T>(s, half);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(k_tile, b, 2 * kb + half, lane), ds, acc[b]);
+          for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(k_tile, b, 2 * kb + half, column_lane), ds, acc[b]);
         }
         read_ahead<T, 2 * NB, 1, 2, 3>();
       }
@@ -183,7 +186,7 @@ struct Pieces {
   int z0, count;
   int64_t lo, hi, per, base;
   __device__ __forceinline__ int64_t begin(int z) const { return max(lo, base + z * per); }
-  __device__ __forceinline__ int64_t end(int z) const { return min(hi, base + (z + 1) * per); }
+  __device__ __forceinline__ int64_t end(int z) const { return z == z0 + count - 1 ? hi : min(hi, base + (z + 1) * per); }
 };
 __device__ __forceinline__ Pieces pieces_of(const Seen &s, int window, int stretch, int parts) {
   Pieces p{0, 1, s.lo, s.hi, stretch, 0};
@@ -193,8 +196,8 @@ __device__ __forceinline__ Pieces pieces_of(const Seen &s, int window, int stret
     p.per = ((s.hi - s.lo + p.count - 1) / p.count + kRows - 1) / kRows * kRows;
     p.base = s.lo;
   } else {
-    p.z0 = static_cast<int>(s.lo / stretch);
-    p.count = static_cast<int>((s.hi - 1) / stretch) - p.z0 + 1;
+    p.z0 = static_cast<int>(min(s.lo / stretch, static_cast<int64_t>(parts - 1)));  // the last one has no end
+    p.count = static_cast<int>(min((s.hi - 1) / stretch, static_cast<int64_t>(parts - 1))) - p.z0 + 1;
   }
   return p;
 }
@@ -352,12 +355,13 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
       if (none) continue;
       f32x16 s{}, dp{};
       // worked out anew each time: kept, the addresses would not fit the registers
-      int k_row = wave * 32 + low;
+      int k_row = wave * 32 + low, row_lane = low, column_lane = lane;
       settle(k_row);
+      if constexpr (DP * sizeof(T) >= 256) settle(row_lane), settle(column_lane);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e) {
-        s = mma(row_frag<T, DP>(q_tile, low, e, high), row_frag<T, DP>(k_tile, k_row, e, high), s);
-        dp = mma(row_frag<T, DP>(g_tile, low, e, high), vf[e], dp);
+        s = mma(row_frag<T, DP>(q_tile, row_lane, e, high), row_frag<T, DP>(k_tile, k_row, e, high), s);
+        dp = mma(row_frag<T, DP>(g_tile, row_lane, e, high), vf[e], dp);
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -380,8 +384,8 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
         const frag pf = as_frag<T>(s, half), df = as_frag<T>(dp, half);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          accv[b] = mma(column_frag<T, DP>(g_tile, b, half, lane), pf, accv[b]);
-          acck[b] = mma(column_frag<T, DP>(q_tile, b, half, lane), df, acck[b]);
+          accv[b] = mma(column_frag<T, DP>(g_tile, b, half, column_lane), pf, accv[b]);
+          acck[b] = mma(column_frag<T, DP>(q_tile, b, half, column_lane), df, acck[b]);
         }
       }
     }
@@ -432,7 +436,9 @@ __global__ __launch_bounds__(256) void k_add(Args a, int width) {
   for (int j = first + threadIdx.x / N; j < min(first + 32, keys); j += R) {
     const int64_t row = (at.begin + j) * a.heads + head;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int p = pieces.z0; p < pieces.z0 + pieces.count; ++p) {
+    const int last = pieces.z0 + pieces.count;
+#pragma unroll 4
+    for (int p = pieces.z0; p < last; ++p) {
       const f32x4 more = *reinterpret_cast<const f32x4 *>(a.sums + (p * a.keys * a.heads + row) * (2 * DP) + e);
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] += more[i];
@@ -449,8 +455,8 @@ struct Plan {
 // A sequence's rows go by stretches, a workgroup for each and each tile of keys that some row of it sees: with a causal
 // mask the first keys are seen by all queries, and the sinks of a window by all but a few, and tiles of keys that
 // go over the same stretch side by side find it in their L2 (8192 tokens of 16 heads of 128, each tile of keys cut into
-// pieces of its own: 67 % of reads missed the L2, 1318 us).  How long the sequences are is not known here: the more there
-// are, the fewer of their rows one has, and each stretch too many is workgroups that find nothing to do.
+// pieces of its own: 67 % of reads missed the L2, 1318 us).  How long the sequences are is not known here, and each stretch
+// too many is workgroups that find nothing to do: stretches are for twice the average, and the last one has no end.
 Plan plan_for(const Mask &m, int64_t tokens, int64_t keys, int64_t group, int64_t heads, int64_t batch, int row_bytes) {
   Plan p;
   p.q_waves = waves_of(tokens, group, batch, 4);
@@ -462,16 +468,12 @@ Plan plan_for(const Mask &m, int64_t tokens, int64_t keys, int64_t group, int64_
   int64_t stretch = std::clamp<int64_t>(turns / 1024, 24, 1 << 20) * kRows;
   // no more than a gigabyte of sums
   const int64_t layer = keys * heads * 2 * SLOWMO_MAX_ATTENTION_DIM * 4;
-  const int64_t most = std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(layer, 1), 1, batch <= 8 ? 16 : batch <= 32 ? 8 : batch <= 96 ? 4 : 2);
-  const int64_t rows = std::max<int64_t>(1, tokens * group);
-  if (m.window) {
-    // a tile with sinks may be seen by every row, the others by those of the window
-    const int64_t longest = m.sinks ? rows : (width + 2 * static_cast<int64_t>(m.window)) * group;
-    p.parts = static_cast<int>(std::clamp<int64_t>((longest + stretch - 1) / stretch, 1, most));
-  } else {
-    stretch = std::max(stretch, ((rows + most - 1) / most + kRows - 1) / kRows * kRows);
-    p.parts = static_cast<int>((rows + stretch - 1) / stretch);
-  }
+  const int64_t most = std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(layer, 1), 1, 16);
+  // rows that a tile is gone over by, where no sequence is longer than twice the average
+  const int64_t rows = m.window && !m.sinks ? (width + 2 * static_cast<int64_t>(m.window)) * group
+                                            : std::max<int64_t>(1, std::min(tokens, 2 * n) * group);
+  if (!m.window) stretch = std::max(stretch, ((rows + most - 1) / most + kRows - 1) / kRows * kRows);
+  p.parts = static_cast<int>(std::clamp<int64_t>((rows + stretch - 1) / stretch, 1, most));
   p.stretch = static_cast<int>(std::min<int64_t>(stretch, INT32_MAX / kRows * kRows));
   return p;
 }
