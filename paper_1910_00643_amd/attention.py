@@ -10,6 +10,8 @@ arithmetic on elements runs in libslowmo.so.
 from __future__ import annotations
 
 import ctypes as C
+import struct
+import threading
 from typing import Optional
 
 import torch
@@ -70,30 +72,64 @@ def lib() -> C.CDLL:
     return L
 
 
+# the values of eight slowmo_heads side by side, of two slowmo_cache and of a slowmo_pages
+_HEADS = [struct.Struct("@" + "Pi4xqq" * n) for n in range(9)]
+_CACHES, _PAGES = struct.Struct("@" + "Piiqqqq" * 2), struct.Struct("@iiqPPP")
+
+
+class _Arguments(threading.local):
+    """The structures of a handle's calls, for each thread its own: ctypes lets go of the interpreter in a call."""
+
+    def __init__(self):
+        self.rows, self.caches, self.pages = (slowmo_heads * 8)(), (slowmo_cache * 2)(), slowmo_pages()
+        self.row = [C.byref(r) for r in self.rows]
+        self.k_cache, self.v_cache, self.table = C.byref(self.caches[0]), C.byref(self.caches[1]), C.byref(self.pages)
+
+
+def _on(device: torch.device, call, *args):
+    """The call with its tensors' GPU as the current one."""
+    if torch.cuda.current_device() == device.index:
+        status = call(*args)
+    else:
+        with torch.cuda.device(device):
+            status = call(*args)
+    if status:
+        _check(status)
+
+
 class _Holder:
-    """What both kinds of attention check of their tensors."""
+    """What both kinds of attention check of their tensors.  A call on few tokens ends before the next one is issued,
+    so that the time between two is what these checks take: addresses go straight into structures that the handle keeps."""
 
     def __init__(self, head_dim: int, dtype: str):
         self.head_dim, self.dtype = int(head_dim), _TORCH_GRAD[dtype]
+        self._args = _Arguments()
 
-    def _rows(self, x: torch.Tensor, what: str, device: torch.device) -> slowmo_heads:
-        """A slowmo_heads for [tokens, heads, head_dim]."""
-        if x.dim() != 3 or x.shape[2] != self.head_dim or x.dtype is not self.dtype or x.device != device:
+    def _row(self, x: torch.Tensor, what: str, device: torch.device):
+        """The values of a slowmo_heads for [tokens, heads, head_dim]."""
+        shape = x.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or x.dtype is not self.dtype or x.device != device:
             raise ValueError(f"{what}: a {self.dtype} tensor [tokens, heads, {self.head_dim}] on {device} is wanted: got "
-                             f"{tuple(x.shape)}, {x.dtype}, {x.device}")
+                             f"{tuple(shape)}, {x.dtype}, {x.device}")
         s0, s1, s2 = x.stride()
         if s2 != 1 and self.head_dim != 1 and x.numel():
             raise ValueError(f"{what}: a head's elements must be contiguous")
-        return slowmo_heads(x.data_ptr(), x.shape[1], s0, s1)
+        return x.data_ptr(), shape[1], s0, s1
+
+    def _rows(self, device, **tensors):
+        """Fills the kept structures, one for each tensor in order."""
+        values = []
+        for what, x in tensors.items():
+            values += self._row(x, what, device)
+        _HEADS[len(tensors)].pack_into(self._args.rows, 0, *values)
 
     @staticmethod
     def _list(x: torch.Tensor, what: str, device: torch.device, length: Optional[int] = None) -> int:
-        if x.dim() != 1 or x.dtype is not torch.int64 or not x.is_contiguous() or x.device != device or \
-                x.shape[0] != (x.shape[0] if length is None else length):
+        shape = x.shape
+        if len(shape) != 1 or x.dtype is not torch.int64 or not x.is_contiguous() or x.device != device or \
+                (length is not None and shape[0] != length) or (length is None and not shape[0]):
             raise ValueError(f"{what}: a contiguous int64 tensor of {'[batch + 1]' if length is None else [length]} on {device} "
-                             f"is wanted: got {tuple(x.shape)}, {x.dtype}, {x.device}")
-        if not x.shape[0] and length is None:
-            raise ValueError(f"{what}: batch + 1 entries are wanted")
+                             f"is wanted: got {tuple(shape)}, {x.dtype}, {x.device}")
         return x.data_ptr()
 
     @staticmethod
@@ -103,9 +139,8 @@ class _Holder:
         return x.device
 
     def _config(self, dtype, scale, causal, window, sinks) -> dict:
-        window, sinks = int(window or 0), int(sinks)
         return dict(dtype=_DTYPE[dtype], head_dim=self.head_dim, causal=int(bool(causal)),
-                    scale=float(self.head_dim) ** -0.5 if scale is None else scale, window=window, sinks=sinks)
+                    scale=float(self.head_dim) ** -0.5 if scale is None else scale, window=int(window or 0), sinks=int(sinks))
 
 
 class Attention(_Holder):
@@ -140,42 +175,38 @@ class Attention(_Holder):
         exponentials, fp32 [tokens, heads].  Rows behind the last sequence: of `out`, where given, left as they are;
         otherwise zeros.  lse there: -infinity."""
         device = self._device(q)
-        rq, rk, rv = self._rows(q, "q", device), self._rows(k, "k", device), self._rows(v, "v", device)
-        if v.shape[0] != k.shape[0]:
-            raise ValueError("k and v must have the same number of rows")
         batch, at, k_at = self._offsets(device, offsets, k_offsets)
-        fresh = out is None
-        with torch.cuda.device(device):
-            if fresh:
-                out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            elif out.shape != q.shape:
-                raise ValueError("out must have q's shape")
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=device)
-            if not fresh:
-                lse.fill_(float("-inf"))
-            _check(lib().slowmo_attention(self._cleared if fresh else self._kept, batch, at, k_at, q.shape[0], k.shape[0], rq,
-                                          rk, rv, self._rows(out, "out", device), lse.data_ptr() or None,
-                                          _raw_stream(device) or None))
+        cfg = self._kept
+        if out is None:
+            cfg, out = self._cleared, torch.empty_like(q, memory_format=torch.contiguous_format)
+        if v.shape[0] != k.shape[0] or out.shape != q.shape:
+            raise ValueError("k and v must have the same number of rows, out must have q's shape")
+        self._rows(device, q=q, k=k, v=v, out=out)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=device)
+        if cfg is self._kept:
+            lse.fill_(float("-inf"))
+        r = self._args.row
+        _on(device, lib().slowmo_attention, cfg, batch, at, k_at, q.shape[0], k.shape[0], r[0], r[1], r[2], r[3],
+            lse.data_ptr() or None, _raw_stream(device) or None)
         return out, lse
 
     def backward(self, g, q, k, v, out, lse, offsets, k_offsets=None):
         """(dq, dk, dv) from the gradient of forward's result, its inputs and what it returned."""
         device = self._device(q)
-        rows = [self._rows(x, n, device) for x, n in ((g, "g"), (q, "q"), (k, "k"), (v, "v"), (out, "out"))]
         if g.shape != q.shape or out.shape != q.shape or v.shape != k.shape:
             raise ValueError("g and out must have q's shape, v must have k's")
         if lse.shape != q.shape[:2] or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.device != device:
             raise ValueError("lse: what forward returned is wanted")
         batch, at, k_at = self._offsets(device, offsets, k_offsets)
-        with torch.cuda.device(device):
-            new = [torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k, v)]
-            nbytes = lib().slowmo_attention_backward_bytes(self._cleared, batch, q.shape[0], k.shape[0], q.shape[1], k.shape[1])
-            space = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            _check(lib().slowmo_attention_backward(
-                self._cleared, batch, at, k_at, q.shape[0], k.shape[0], *rows, lse.data_ptr() or None,
-                *[self._rows(x, "a gradient", device) for x in new], space.data_ptr() if nbytes else None, nbytes,
-                _raw_stream(device) or None))
-        return tuple(new)
+        dq, dk, dv = (torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k, v))
+        self._rows(device, g=g, q=q, k=k, v=v, out=out, dq=dq, dk=dk, dv=dv)
+        tokens, keys = q.shape[0], k.shape[0]
+        nbytes = lib().slowmo_attention_backward_bytes(self._cleared, batch, tokens, keys, q.shape[1], k.shape[1])
+        space = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        r = self._args.row
+        _on(device, lib().slowmo_attention_backward, self._cleared, batch, at, k_at, tokens, keys, r[0], r[1], r[2], r[3], r[4],
+            lse.data_ptr() or None, r[5], r[6], r[7], space.data_ptr() if nbytes else None, nbytes, _raw_stream(device) or None)
+        return dq, dk, dv
 
     def __call__(self, q, k, v, offsets, k_offsets=None):
         """forward()'s result, which autograd differentiates for q, k and v."""
@@ -231,50 +262,54 @@ class PagedAttention(_Holder):
             dtype=_DTYPE[dtype], head_dim=self.head_dim, rotary_dim=2 * pairs, interleaved=int(bool(interleaved)), clear_rest=c,
             table=table.data_ptr() if pairs else None, table_rows=table.shape[0] if pairs else 0) for c in (0, 1))
 
-    def _cache(self, x: torch.Tensor, what: str, device) -> slowmo_cache:
-        if x.dim() != 4 or x.shape[3] != self.head_dim or x.dtype is not self.dtype or x.device != device:
+    def _cache(self, x: torch.Tensor, what: str, device):
+        shape = x.shape
+        if len(shape) != 4 or shape[3] != self.head_dim or x.dtype is not self.dtype or x.device != device:
             raise ValueError(f"{what}: a {self.dtype} tensor [pages, page, heads, {self.head_dim}] on {device} is wanted: got "
-                             f"{tuple(x.shape)}, {x.dtype}, {x.device}")
-        s = x.stride()
-        if s[3] != 1 and self.head_dim != 1 and x.numel():
+                             f"{tuple(shape)}, {x.dtype}, {x.device}")
+        s0, s1, s2, s3 = x.stride()
+        if s3 != 1 and self.head_dim != 1 and x.numel():
             raise ValueError(f"{what}: a head's elements must be contiguous")
-        return slowmo_cache(x.data_ptr(), x.shape[2], x.shape[1], x.shape[0], s[0], s[1], s[2])
+        return x.data_ptr(), shape[2], shape[1], shape[0], s0, s1, s2
 
-    def _pages(self, pages, lengths, offsets, device) -> slowmo_pages:
+    def _places(self, k_cache, v_cache, pages, lengths, offsets, device):
+        """Fills the kept structures of the caches and of the table."""
+        _CACHES.pack_into(self._args.caches, 0, *self._cache(k_cache, "k_cache", device),
+                          *self._cache(v_cache, "v_cache", device))
         if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.device != device or \
                 (pages.shape[1] > 1 and pages.stride(1) != 1):
             raise ValueError(f"pages: an int32 tensor [batch, columns] on {device}, a row's entries contiguous, is wanted: got "
                              f"{tuple(pages.shape)}, {pages.dtype}, {pages.device}")
         batch, columns = pages.shape
-        return slowmo_pages(batch, columns, max(pages.stride(0), columns), pages.data_ptr() or None,
-                            self._list(lengths, "lengths", device, batch) or None,
-                            self._list(offsets, "offsets", device, batch + 1))
+        _PAGES.pack_into(self._args.pages, 0, batch, columns, pages.stride(0) if batch > 1 else columns, pages.data_ptr(),
+                         self._list(lengths, "lengths", device, batch), self._list(offsets, "offsets", device, batch + 1))
 
     def append(self, k, v, k_cache, v_cache, pages, lengths, offsets, q=None, q_out=None):
         """Writes the new keys, turned, and values to their places.  With q: returns the turned queries, written to
         q_out where given (it may be q).  Rows behind the last sequence: of q_out, where given, left as they are;
         otherwise zeros."""
         device = self._device(k)
-        rk, rv = self._rows(k, "k", device), self._rows(v, "v", device)
-        if v.shape[0] != k.shape[0] or (q is not None and q.shape[0] != k.shape[0]):
-            raise ValueError("q, k and v must have the same number of rows")
-        if q is None and q_out is not None:
-            raise ValueError("q_out without q")
         if self.table is not None and self.table.device != device:
             raise ValueError(f"the table is on {self.table.device}, the tensors on {device}")
-        with torch.cuda.device(device):
-            rq, rqo, cfg = None, None, self._append
-            if q is not None:
-                rq = self._rows(q, "q", device)
-                if q_out is None:
-                    cfg = self._append_cleared
-                    q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-                elif q_out.shape != q.shape:
-                    raise ValueError("q_out must have q's shape")
-                rqo = self._rows(q_out, "q_out", device)
-            _check(lib().slowmo_cache_append(cfg, self._pages(pages, lengths, offsets, device), k.shape[0], rk, rv,
-                                             self._cache(k_cache, "k_cache", device), self._cache(v_cache, "v_cache", device),
-                                             rq, rqo, _raw_stream(device) or None))
+        cfg, r = self._append, self._args.row
+        if q is None:
+            if q_out is not None:
+                raise ValueError("q_out without q")
+            self._rows(device, k=k, v=v)
+            tokens, rq, rqo = k.shape[0], None, None
+        else:
+            if q_out is None:
+                cfg, q_out = self._append_cleared, torch.empty_like(q, memory_format=torch.contiguous_format)
+            self._rows(device, k=k, v=v, q=q, q_out=q_out)
+            tokens, rq, rqo = q.shape[0], r[2], r[3]
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+        if k.shape[0] != tokens or v.shape[0] != tokens:
+            raise ValueError("q, k and v must have the same number of rows")
+        self._places(k_cache, v_cache, pages, lengths, offsets, device)
+        a = self._args
+        _on(device, lib().slowmo_cache_append, cfg, a.table, tokens, r[0], r[1], a.k_cache, a.v_cache, rq, rqo,
+            _raw_stream(device) or None)
         return q_out
 
     def forward(self, q, k_cache, v_cache, pages, lengths, offsets, out=None, return_lse: bool = False):
@@ -282,21 +317,20 @@ class PagedAttention(_Holder):
         tokens included: out, or (out, lse).  Rows behind the last sequence: of `out`, where given, left as they
         are; otherwise zeros."""
         device = self._device(q)
-        rq = self._rows(q, "q", device)
-        ck, cv = self._cache(k_cache, "k_cache", device), self._cache(v_cache, "v_cache", device)
-        pg = self._pages(pages, lengths, offsets, device)
         cfg = self._cfg
-        with torch.cuda.device(device):
-            if out is None:
-                cfg, out = self._cleared, torch.empty_like(q, memory_format=torch.contiguous_format)
-            elif out.shape != q.shape:
-                raise ValueError("out must have q's shape")
-            lse = torch.full(q.shape[:2], float("-inf"), dtype=torch.float32, device=device) if return_lse else None
-            nbytes = lib().slowmo_paged_attention_bytes(cfg, pg, q.shape[0], q.shape[1], ck)
-            space = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-            _check(lib().slowmo_paged_attention(cfg, pg, q.shape[0], rq, ck, cv, self._rows(out, "out", device),
-                                                lse.data_ptr() or None if return_lse else None,
-                                                space.data_ptr() if nbytes else None, nbytes, _raw_stream(device) or None))
+        if out is None:
+            cfg, out = self._cleared, torch.empty_like(q, memory_format=torch.contiguous_format)
+        self._rows(device, q=q, out=out)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+        self._places(k_cache, v_cache, pages, lengths, offsets, device)
+        lse = torch.full(q.shape[:2], float("-inf"), dtype=torch.float32, device=device) if return_lse else None
+        a, tokens = self._args, q.shape[0]
+        nbytes = lib().slowmo_paged_attention_bytes(cfg, a.table, tokens, q.shape[1], a.k_cache)
+        space = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+        _on(device, lib().slowmo_paged_attention, cfg, a.table, tokens, a.row[0], a.k_cache, a.v_cache, a.row[1],
+            lse.data_ptr() or None if return_lse else None, space.data_ptr() if nbytes else None, nbytes,
+            _raw_stream(device) or None)
         return (out, lse) if return_lse else out
 
     __call__ = forward

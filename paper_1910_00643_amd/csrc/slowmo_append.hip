@@ -9,17 +9,19 @@ namespace slowmo {
 namespace attention {
 namespace {
 
+constexpr int kHeads = 4;  // heads of a lane: they share their angles, which are twice as many bytes as a head's elements
+
 struct Args {
   Rows side[3], out[3];  // keys, values, queries; where they go (queries: by token)
   int64_t page_stride[2];
-  int32_t heads[3];
+  int32_t heads[3], groups[3];  // groups of kHeads
   const int64_t *offsets, *lengths;
   const int32_t *pages;
   const float *table;
   int64_t table_rows, pages_stride, tokens, first;
   int32_t columns, n_pages[2], page_log2, batch, dim, rot;
   int32_t turned, plain;  // pieces of a row that is turned, and of one that is not
-  int32_t every;          // pieces of a token
+  int32_t every;          // lanes of a token: a piece of kHeads heads each
   bool clear;
 };
 
@@ -36,10 +38,35 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
   constexpr int C = WIDE ? V : 1;
   using Copy = Piece<T, C, WIDE>;
   const int64_t base = (a.first + blockIdx.x) * 256;
-  const int64_t t0 = base / a.every;
+  const int64_t t0 = base >> 32 ? base / a.every : static_cast<u32>(base) / static_cast<u32>(a.every);
   const u32 in = static_cast<u32>(base - t0 * a.every) + threadIdx.x;
   const int64_t t = t0 + in / a.every;
   int piece = static_cast<int>(in % a.every);
+  // which rows, which piece of them
+  int which = 0, per = a.turned;
+  const int keys = a.groups[0] * a.turned, values = a.groups[1] * a.plain;
+  if (piece >= keys + values) which = 2, piece -= keys + values;
+  else if (piece >= keys) which = 1, piece -= keys, per = a.plain;
+  const int head = piece / per * kHeads, heads = min(kHeads, a.heads[which] - head);
+  piece %= per;
+  const int half = a.rot / 2, pieces = INTER ? a.rot / V : half / V;  // that turn
+  const bool turns = which != 1 && piece < pieces;
+  const int d = turns ? piece * V : which == 1 ? piece * C : a.rot + (piece - pieces) * C;
+  // the elements are asked for beside the token's place, which takes several trips to memory one after the other
+  P x[kHeads], y[kHeads];
+  if (t < a.tokens) {
+    const T *from = static_cast<const T *>(a.side[which].data) + t * a.side[which].token + head * a.side[which].head + d;
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      if (h >= heads) continue;
+      if (turns) {
+        x[h] = *reinterpret_cast<const P *>(from + h * a.side[which].head);
+        if constexpr (!INTER) y[h] = *reinterpret_cast<const P *>(from + h * a.side[which].head + half);
+      } else {
+        __builtin_memcpy(&x[h], reinterpret_cast<const Copy *>(from + h * a.side[which].head), sizeof(Copy));
+      }
+    }
+  }
   // the first token's sequence by all lanes, then on from there
   const int lane = threadIdx.x & 63;
   int b = -1;
@@ -60,21 +87,11 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
     b = lo;
   }
   const bool rest = b >= a.batch;  // behind the last sequence
-  if (rest && !a.clear) return;
+  if (rest && (!a.clear || which != 2)) return;
   const int64_t begin = rest ? 0 : a.offsets[b], end = rest ? 0 : a.offsets[b + 1], position = rest ? 0 : a.lengths[b] - (end - t);
-  // which row, which piece of it
-  int which = 0, per = a.turned, head = 0;
-  const int keys = a.heads[0] * a.turned, values = a.heads[1] * a.plain;
-  if (piece >= keys + values) which = 2, piece -= keys + values;
-  else if (piece >= keys) which = 1, piece -= keys, per = a.plain;
-  head = piece / per;
-  piece -= head * per;
-  const T *from = static_cast<const T *>(a.side[which].data) + t * a.side[which].token + head * a.side[which].head;
-  T *to = static_cast<T *>(a.out[which].data) + head * a.out[which].head;
+  T *to = static_cast<T *>(a.out[which].data) + head * a.out[which].head + d;
   if (which == 2) {
     to += t * a.out[2].token;
-  } else if (rest) {
-    return;
   } else {
     const int64_t column = position >> a.page_log2;
     if (t < begin || position < 0 || column >= a.columns) return;
@@ -82,16 +99,19 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
     if (static_cast<u32>(page) >= static_cast<u32>(a.n_pages[which])) return;
     to += page * a.page_stride[which] + (position & ((int64_t(1) << a.page_log2) - 1)) * a.out[which].token;
   }
-  const int half = a.rot / 2, pieces = INTER ? a.rot / V : half / V;  // that turn
-  if (which == 1 || piece >= pieces) {
-    const int d = which == 1 ? piece * C : a.rot + (piece - pieces) * C;
-    *reinterpret_cast<Copy *>(to + d) = rest ? Copy{} : *reinterpret_cast<const Copy *>(from + d);
-    return;
-  }
-  if (rest) {
-    const int d = piece * V;
-    *reinterpret_cast<P *>(to + d) = P{};
-    if constexpr (!INTER) *reinterpret_cast<P *>(to + half + d) = P{};
+  const int64_t next = a.out[which].head;
+  if (!turns || rest) {
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      if (h >= heads) continue;
+      if (rest) x[h] = y[h] = P{};
+      Copy copy;
+      __builtin_memcpy(&copy, &x[h], sizeof(Copy));
+      if (!turns) *reinterpret_cast<Copy *>(to + h * next) = copy;
+      if (turns) *reinterpret_cast<P *>(to + h * next) = x[h];
+      if constexpr (!INTER)
+        if (turns) *reinterpret_cast<P *>(to + h * next + half) = y[h];
+    }
     return;
   }
   const bool known = position >= 0 && position < a.table_rows;
@@ -105,25 +125,18 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
     __builtin_memcpy(c, __builtin_assume_aligned(cos + pair, 4), sizeof(c));
     __builtin_memcpy(s, __builtin_assume_aligned(sin + pair, 4), sizeof(s));
   }
-  if constexpr (INTER) {
-    P x = *reinterpret_cast<const P *>(from + 2 * pair);
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    if (h >= heads) continue;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float u = static_cast<float>(x.e[2 * i]), v = static_cast<float>(x.e[2 * i + 1]);
-      x.e[2 * i] = static_cast<T>(u * c[i] - v * s[i]);
-      x.e[2 * i + 1] = static_cast<T>(u * s[i] + v * c[i]);
+      T &first = INTER ? x[h].e[2 * i] : x[h].e[i], &second = INTER ? x[h].e[2 * i + 1] : y[h].e[i];
+      const float u = static_cast<float>(first), v = static_cast<float>(second);
+      first = static_cast<T>(u * c[i] - v * s[i]);
+      second = static_cast<T>(u * s[i] + v * c[i]);
     }
-    *reinterpret_cast<P *>(to + 2 * pair) = x;
-  } else {
-    P x = *reinterpret_cast<const P *>(from + pair), y = *reinterpret_cast<const P *>(from + half + pair);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float u = static_cast<float>(x.e[i]), v = static_cast<float>(y.e[i]);
-      x.e[i] = static_cast<T>(u * c[i] - v * s[i]);
-      y.e[i] = static_cast<T>(u * s[i] + v * c[i]);
-    }
-    *reinterpret_cast<P *>(to + pair) = x;
-    *reinterpret_cast<P *>(to + half + pair) = y;
+    *reinterpret_cast<P *>(to + h * next) = x[h];
+    if constexpr (!INTER) *reinterpret_cast<P *>(to + h * next + half) = y[h];
   }
 }
 
@@ -136,7 +149,8 @@ hipError_t launch(Args a, bool wide, bool inter, hipStream_t stream) {
   const int turning = inter ? a.rot / v : a.rot / 2 / v;
   a.turned = turning + (a.dim - a.rot) / rest;
   a.plain = a.dim / rest;
-  a.every = (a.heads[0] + a.heads[2]) * a.turned + a.heads[1] * a.plain;
+  for (int i = 0; i < 3; ++i) a.groups[i] = (a.heads[i] + kHeads - 1) / kHeads;
+  a.every = (a.groups[0] + a.groups[2]) * a.turned + a.groups[1] * a.plain;
   const int64_t blocks = (a.tokens * a.every + 255) / 256;
   for (a.first = 0; a.first < blocks && e == hipSuccess; a.first += kMostBlocks) {
     const u32 n = static_cast<u32>(std::min(kMostBlocks, blocks - a.first));
