@@ -71,16 +71,20 @@ struct Stage {
     }
     const u32 shared = uniform(offset_of(tile));
     constexpr int R = L::C < 64 ? 64 / L::C : 1;  // rows of a piece
-    // Whole tiles whose pieces each lie in one page: the page's address is worked out once for a piece, by scalar
-    // instructions (48 single tokens over 16 000: 667 -> 452 us).
+    // Whole tiles whose pieces each lie in one page: every lane works out one row's address, and a piece takes that of
+    // its first row (48 single tokens over 16 000: 667 -> 452 us with an address for each lane and piece; this way 365, 4.3 TB/s).
     if ((1 << a.page_log2) >= R && j0 + L::rows <= keys &&
         __all(static_cast<u32>(page) < static_cast<u32>(a.n_pages))) {
       const u32 step = static_cast<u32>(x.token) * sizeof(T);
+      const int j = j0 + (lane & (L::rows - 1));
+      const u32x2 mine = __builtin_bit_cast(
+          u32x2, base + static_cast<int64_t>(page) * page_stride + (j & ((1 << a.page_log2) - 1)) * x.token);
       auto piece = [&](int n) SLOWMO_INLINE {
-        const int row0 = n * R, row = row0 + lane / L::C, c = (lane & (L::C - 1)) ^ L::turn(row);
-        const int id = __builtin_amdgcn_readlane(page, row0);
-        const T *from = base + static_cast<int64_t>(id) * page_stride + ((j0 + row0) & ((1 << a.page_log2) - 1)) * x.token;
-        if (c * L::E < a.dim) to_shared(uniform(shared + n * 1024), (lane / L::C) * step + c * 16, uniform(from));
+        const int row0 = n * R, c = (lane & (L::C - 1)) ^ L::turn(row0 + lane / L::C);
+        const u32x2 from = {static_cast<u32>(__builtin_amdgcn_readlane(mine[0], row0)),
+                            static_cast<u32>(__builtin_amdgcn_readlane(mine[1], row0))};
+        if (c * L::E < a.dim)
+          to_shared(uniform(shared + n * 1024), (lane / L::C) * step + c * 16, __builtin_bit_cast(const T *, from));
       };
       if (waves == 1) {
 #pragma unroll
@@ -341,12 +345,21 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
     __syncthreads();
   }
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int y = WAVES == 1 ? 0 : wave; y < pieces; y += WAVES) {
-    const float w = WAVES == 1 ? __shfl(weight, y) : weights[y / 64][y % 64];
-    if (4 * lane >= DP) continue;
-    const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part + (y * every + at_row) * DP + 4 * lane);
+  for (int y0 = WAVES == 1 ? 0 : wave; y0 < pieces; y0 += 8 * WAVES) {  // eight are asked for at once
+    f32x4 v[8];
+    float w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] += w == 0.f ? 0.f : w * v[i];
+    for (int e = 0; e < 8; ++e) {
+      const int y = min(y0 + WAVES * e, pieces - 1);
+      w[e] = WAVES == 1 ? __shfl(weight, y) : weights[y / 64][y % 64];
+      if (y0 + WAVES * e >= pieces) w[e] = 0.f;
+      v[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (4 * lane < DP && w[e] != 0.f) v[e] = *reinterpret_cast<const f32x4 *>(a.part + (y * every + at_row) * DP + 4 * lane);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += w[e] * v[e][i];
   }
   float total = weight;
   if constexpr (WAVES > 1) {
@@ -371,17 +384,22 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
 struct Pieces {
   int splits, least, waves;
 };
-// Pieces of the key axis: enough workgroups for two rounds of the card where rows are few.
-Pieces pieces_for(int64_t tokens, int64_t group, int64_t heads, int64_t batch, int64_t positions, int rows_of_tile) {
+// Pieces of the key axis, of like length for long and short sequences: some thousand where rows are few, one of 4 waves
+// for at least 16 tiles, since its sums are 64 KB.  How long the sequences are is not known here: the table's width is taken.
+Pieces pieces_for(const slowmo_attention_config &c, int64_t tokens, int64_t group, int64_t heads, int64_t batch, int64_t positions,
+                  int rows_of_tile) {
   Pieces p;
   p.waves = waves_of(tokens, group, batch, 4);
-  const int64_t tiles = (std::min<int64_t>(positions, kLongest) + rows_of_tile - 1) / rows_of_tile;
-  const int64_t groups = std::max<int64_t>(1, std::min(batch, tokens) * heads + tokens * group / (p.waves * 32) * heads);
-  p.least = p.waves == 1 ? 8 : 16;
-  p.splits = static_cast<int>(std::clamp<int64_t>(((p.waves == 1 ? 2048 : 1024) + groups - 1) / groups, 1, std::clamp<int64_t>(tiles / p.least, 1, kMostPieces)));
+  const int64_t height = p.waves * 32;
+  int64_t seen = std::min<int64_t>(positions, kLongest);
+  if (c.window) seen = std::min(seen, std::min<int64_t>(c.window, kLongest) + height / group + std::min<int64_t>(c.sinks, kLongest) + 2 * rows_of_tile);
+  const int64_t tiles = (seen + rows_of_tile - 1) / rows_of_tile;
+  const int64_t groups = std::max<int64_t>(1, std::min(batch, tokens) + tokens * group / height) * heads;
+  p.least = static_cast<int>(std::clamp<int64_t>(groups * tiles / (p.waves == 1 ? 8192 : 2048), p.waves == 1 ? 8 : 16, kLongest));
   // no more than a gigabyte of sums
   const int64_t row_bytes = tokens * heads * group * (SLOWMO_MAX_ATTENTION_DIM + 1) * 4;
-  p.splits = static_cast<int>(std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(row_bytes, 1), 1, p.splits));
+  const int64_t most = std::clamp<int64_t>((int64_t(1) << 30) / std::max<int64_t>(row_bytes, 1), 1, kMostPieces);
+  p.splits = static_cast<int>(std::clamp<int64_t>((tiles + p.least - 1) / p.least, 1, most));
   return p;
 }
 
@@ -622,7 +640,7 @@ size_t slowmo_paged_attention_bytes(const slowmo_attention_config *cfg, const sl
     return 0;
   const int dp = padded(cfg->head_dim);
   const int rows = rows_of_tile(cfg->head_dim, cfg->dtype);
-  const Pieces p = pieces_for(tokens, q_heads / k_cache->heads, k_cache->heads, pages->batch,
+  const Pieces p = pieces_for(*cfg, tokens, q_heads / k_cache->heads, k_cache->heads, pages->batch,
                               static_cast<int64_t>(pages->columns) * k_cache->page, rows);
   return p.splits == 1 ? 0 : static_cast<size_t>(p.splits) * tokens * q_heads * (dp + 1) * sizeof(float);
 }
@@ -670,7 +688,7 @@ slowmo_status slowmo_paged_attention(const slowmo_attention_config *cfg, const s
     a.wide = wide_rows(*q, cfg->head_dim, cfg->dtype) && wide_rows(*out, cfg->head_dim, cfg->dtype) &&
              wide_rows(*k_cache, cfg->head_dim, cfg->dtype) && wide_rows(*v_cache, cfg->head_dim, cfg->dtype);
     const int dp = padded(cfg->head_dim), rows = rows_of_tile(cfg->head_dim, cfg->dtype);
-    const Pieces p = pieces_for(tokens, a.group, a.heads, pages->batch, static_cast<int64_t>(pages->columns) * k_cache->page, rows);
+    const Pieces p = pieces_for(*cfg, tokens, a.group, a.heads, pages->batch, static_cast<int64_t>(pages->columns) * k_cache->page, rows);
     a.splits = p.splits, a.least = p.least;
     a.part = static_cast<float *>(workspace);
     a.part_lse = a.part + static_cast<int64_t>(p.splits) * tokens * q->heads * dp;
