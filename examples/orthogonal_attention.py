@@ -1,9 +1,9 @@
-"""Workers that train a small attention model with orthogonalised local steps.
+"""Workers that train a small attention model with orthogonalised local steps, and one that answers.
 
 m logical workers on one GPU learn to repeat the token of two places before.  In
 every local step of a worker
   - queries and keys go through HeadNormRotary: their norm for each head and the
-    position rotation in one pass, differentiated by autograd;
+    position rotation in one pass, and Attention over the batch's sequences, both differentiated by autograd;
   - the projections' gradients become directions by Orthogonalizer: the SGD row's
     momentum, then Newton-Schulz products.  They go to SlowMo.local_step as the gradient
     (momentum 0 there; its coupled decay is then the decoupled one);
@@ -11,6 +11,9 @@ every local step of a worker
 Every tau steps the workers' replicas are averaged and the slow momentum is applied.  The directions'
 momentum is this program's: it is kept over the outer step, each worker's own, whatever the buffer policy
 of SlowMo does to Adam's buffers.
+
+A trained worker answers with PagedAttention: the prompts' keys and values go to a paged cache, then those of one token
+after the other, and each new token attends to what is cached.
 
     python examples/orthogonal_attention.py [outer iterations]
 """
@@ -23,8 +26,8 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_1910_00643_amd import (HeadNormRotary, Orthogonalizer, SlowMo, make_config,  # noqa: E402
-                                  rotary_table)
+from paper_1910_00643_amd import (Attention, HeadNormRotary, Orthogonalizer, PagedAttention, SlowMo,  # noqa: E402
+                                  make_config, rotary_table)
 
 VOCAB, WIDTH, HEADS, DIM, LENGTH, BATCH = 64, 128, 4, 32, 48, 32
 MATRICES = ["wq", "wk", "wv", "wo"]
@@ -39,19 +42,60 @@ def make_worker(device, seed):
     return {n: t.requires_grad_() for n, t in p.items()}
 
 
-def loss_of(p, tokens, rotate, positions):
-    """Cross entropy of every token from the third on against the one of two places before."""
-    b, t = tokens.shape
+SCALE = 4.0 / DIM ** 0.5
+
+
+def projections(p, tokens):
+    """The embedded tokens and their queries, keys and values, [tokens, heads, DIM]."""
     x = p["embed"][tokens]
-    q, k, v = ((x @ p[n].t()).view(b * t, HEADS, DIM) for n in ("wq", "wk", "wv"))
+    return x, *((x @ p[n].t()).unflatten(-1, (HEADS, DIM)) for n in ("wq", "wk", "wv"))
+
+
+def logits_of(p, tokens, rotate, attend):
+    """[batch, length, VOCAB] of a batch of sequences of one length."""
+    b, t = tokens.shape
+    positions = torch.arange(t, device=tokens.device).repeat(b)
+    offsets = torch.arange(b + 1, device=tokens.device) * t
+    x, q, k, v = projections(p, tokens.flatten())
     q, k = rotate(q, k, positions, p["q_norm"], p["k_norm"])
-    q, k, v = (y.view(b, t, HEADS, DIM).transpose(1, 2).contiguous() for y in (q, k, v))
-    scores = (q @ k.transpose(2, 3).contiguous()) * (4.0 / DIM ** 0.5)
-    later = torch.ones(t, t, dtype=torch.bool, device=x.device).triu(1)
-    mixed = torch.softmax(scores.masked_fill(later, float("-inf")), -1) @ v
-    y = x + mixed.transpose(1, 2).reshape(b, t, WIDTH) @ p["wo"].t()
-    logits = y @ p["head"].t()
+    y = x + attend(q, k, v, offsets).flatten(1) @ p["wo"].t()
+    return (y @ p["head"].t()).view(b, t, VOCAB)
+
+
+def loss_of(p, tokens, rotate, attend):
+    """Cross entropy of every token from the third on against the one of two places before."""
+    logits = logits_of(p, tokens, rotate, attend)
     return torch.nn.functional.cross_entropy(logits[:, 2:].reshape(-1, VOCAB), tokens[:, :-2].reshape(-1))
+
+
+@torch.no_grad()
+def answer(p, prompts, more, page=8):
+    """The logits at every token of `prompts`, a list of token tensors of any lengths, and then of `more`, [prompts, n],
+    handed over one token of each sequence at a time: [tokens of the prompts, VOCAB] and [prompts, n, VOCAB]."""
+    device, batch, n = more.device, len(prompts), more.shape[1]
+    lengths = torch.tensor([t.numel() for t in prompts], device=device)
+    columns = -(-(int(lengths.max()) + n) // page)
+    pages = torch.randperm(batch * columns, device=device).int().view(batch, columns)
+    cache = torch.empty(2, batch * columns, page, HEADS, DIM, device=device)
+    table = rotary_table(columns * page, DIM // 2, device=device)
+    # the norm is taken before the keys are cached; the turn comes with the append
+    norm = HeadNormRotary(DIM, None, dtype="f32")
+    paged = PagedAttention(DIM, table, dtype="f32", scale=SCALE)
+
+    def step(tokens, offsets):
+        x, q, k, v = projections(p, tokens)
+        q, k = norm.forward(q, k, None, p["q_norm"].detach(), p["k_norm"].detach())
+        q = paged.append(k, v, cache[0], cache[1], pages, lengths, offsets, q=q)
+        y = x + paged.forward(q, cache[0], cache[1], pages, lengths, offsets).flatten(1) @ p["wo"].t()
+        return y @ p["head"].t()
+
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64, device=device), lengths.cumsum(0)])
+    first, each = step(torch.cat(prompts), offsets), torch.arange(batch + 1, device=device)
+    rest = []
+    for i in range(n):
+        lengths += 1
+        rest.append(step(more[:, i], each))
+    return first, torch.stack(rest, 1)
 
 
 def train(outer=20, m=2, tau=6, lr=0.02, adam_lr=3e-3, device="cuda:0"):
@@ -66,7 +110,7 @@ def train(outer=20, m=2, tau=6, lr=0.02, adam_lr=3e-3, device="cuda:0"):
     momentum = [torch.zeros(s, device=device) for s in shapes]
     directions = [[torch.empty_like(t) for t in w] for w in matrices]
     rotate = HeadNormRotary(DIM, rotary_table(LENGTH, DIM // 2, device=device), dtype="f32")
-    positions = torch.arange(LENGTH, device=device).repeat(BATCH)
+    attend = Attention(DIM, dtype="f32", scale=SCALE)
     g = torch.Generator(device=device).manual_seed(7)
     losses = []
     for _ in range(outer):
@@ -76,7 +120,7 @@ def train(outer=20, m=2, tau=6, lr=0.02, adam_lr=3e-3, device="cuda:0"):
                 tokens = torch.randint(0, VOCAB, (BATCH, LENGTH), device=device, generator=g)
                 for t in w.values():
                     t.grad = None
-                loss = loss_of(w, tokens, rotate, positions)
+                loss = loss_of(w, tokens, rotate, attend)
                 loss.backward()
                 mean += loss.detach() / m
             losses.append(mean)
