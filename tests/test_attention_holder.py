@@ -144,6 +144,13 @@ def test_tables_that_are_none_are_refused():
             A.PagedAttention(16, bad, dtype="f32")
 
 
+@pytest.mark.parametrize("kw", [dict(window=0), dict(window=-3), dict(sinks=-1), dict(window=5, sinks=-1)], ids=str)
+def test_windows_that_are_none_are_refused(kw):
+    for kind in (A.Attention, A.PagedAttention):
+        with pytest.raises(ValueError):
+            kind(16, **kw)
+
+
 def test_tensors_that_are_not_on_a_gpu_are_refused():
     x = torch.zeros(3, 1, 16)
     with pytest.raises(ValueError):

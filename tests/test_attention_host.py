@@ -74,6 +74,13 @@ def test_bad_calls(kw, status):
     assert P.slowmo_last_error(None)
 
 
+def test_more_rows_than_2_36_are_refused():
+    many = _heads(0x100000, 1 << 12, token=1 << 20, head=64)
+    assert _forward(tokens=(1 << 24) + 1, keys=4, k_offsets=0x2000, q=many, out=_heads(0x40000000000000, 1 << 12, token=1 << 20),
+                    k=_heads(0x200000, 1), v=_heads(0x300000, 1), lse=None) == ARG
+    assert "2^36" in P.slowmo_last_error(None)
+
+
 def test_nothing_to_do_is_no_error():
     none = _heads(None, 4)
     assert _forward(tokens=0, keys=0, q=none, out=none, k=_heads(None), v=_heads(None), lse=None) == B.SLOWMO_OK

@@ -130,12 +130,13 @@ def test_rows_behind_the_last_sequence():
         assert (d[73:] == 0).all() and d[:73].isfinite().all()
 
 
-def test_a_captured_step_is_replayed():
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "bf16"), (128, "f32"), (256, "bf16")])
+def test_a_captured_step_is_replayed(dim, dtype):
     """Forward and backward in a graph, on offsets that change between replays, beside an eager graph of the same leaves."""
-    case = ([90, 60, 50], None, 4, 2, 64, True, 33, 2, 0, 0)
-    op, q, k, v, at, _, g = _inputs(case, "bf16")
+    case = ([90, 60, 50], None, 4, 2, dim, True, 33, 2, 0, 0)
+    op, q, k, v, at, _, g = _inputs(case, dtype)
     leaves = [t.contiguous().requires_grad_() for t in (q, k, v)]
-    gout = _grad(q, "bf16", g)
+    gout = _grad(q, dtype, g)
     held = op(*leaves, at)                      # an eager graph that stays alive
 
     def step():
@@ -153,7 +154,7 @@ def test_a_captured_step_is_replayed():
         kept = step()
     for turn, lengths in enumerate(([90, 60, 50], [200, 0, 0], [1, 2, 150], [64, 65, 71])):
         at.copy_(torch.tensor(U.offsets_of(lengths), device=DEV))
-        gout.copy_(_grad(q, "bf16", g))
+        gout.copy_(_grad(q, dtype, g))
         graph.replay()
         torch.cuda.synchronize()
         got = [t.clone() for t in kept]

@@ -107,6 +107,24 @@ def test_pages_outside_the_cache(dtype):
     assert short.isnan().all()
 
 
+@pytest.mark.parametrize("window,sinks", [(None, 0), (90, 0), (90, 3), (90, 1 << 40)])
+def test_lengths_far_past_the_table(window, sinks):
+    """Queries at positions without pages have NaN, and no more is walked than the table holds."""
+    g = torch.Generator(device=DEV).manual_seed(20)
+    kc, vc = (torch.randn(20, 16, 1, 64, device=DEV, generator=g).bfloat16() for _ in range(2))
+    pages = torch.arange(20, dtype=torch.int32, device=DEV).view(1, 20)
+    q = U.rows(g, 300, 4, 64, "bf16")
+    op = _P().PagedAttention(64, window=window, sinks=sinks)
+    at = torch.tensor([0, 300], device=DEV)
+    for length in (2 ** 29 + 7, 2 ** 62, 10 ** 6, 650):
+        assert op.forward(q, kc, vc, pages, torch.tensor([length], device=DEV), at).isnan().all()
+    # the first 20 of these are at positions 300 to 319, which have pages
+    out = op.forward(q, kc, vc, pages, torch.tensor([600], device=DEV), at)
+    want, tol = U.dense(q[:20], _gathered(kc, pages[0], 320), _gathered(vc, pages[0], 320), "bf16", window=window, sinks=sinks)
+    U.near(out[:20], want["out"], tol["out"] * 1.01, "out")
+    assert out[20:].isnan().all()
+
+
 def test_one_bad_page_leaves_the_queries_before_it():
     g = torch.Generator(device=DEV).manual_seed(13)
     pages, total = _paged(g, [64], 16)
