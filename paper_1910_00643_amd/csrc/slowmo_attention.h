@@ -108,35 +108,41 @@ __device__ __forceinline__ u32 offset_of(const void *p) {
   return static_cast<u32>(reinterpret_cast<uintptr_t>((const lds *)p));
 }
 
+// Shared memory by its offset.  A tile begins at a multiple of its rows' length, a power of two, so that a chunk's place
+// in a row is an exclusive or: one instruction from a lane's address to any chunk of its row.
+template <typename V>
+__device__ __forceinline__ V shared_at(u32 offset) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V *>(offset);
+}
+
 // The rows of a product's left factor: row `row` of the tile, elements 16 step + 8 high .. + 7.
 template <typename T, int DP>
 __device__ __forceinline__ typename Kind<T>::frag row_frag(const char *tile, int row, int step, int high) {
   using L = Tile<T, DP>;
-  const char *at = tile + row * L::row_bytes;
-  const int t = L::turn(row);
+  const u32 at = offset_of(tile) + row * L::row_bytes;
   if constexpr (sizeof(T) == 2) {
-    return *reinterpret_cast<const bf16x8 *>(at + (((2 * step + high) ^ t) << 4));
+    return shared_at<bf16x8>((at + ((high ^ L::turn(row)) << 4)) ^ (step << 5));
   } else {
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(at + (((4 * step + 2 * high) ^ t) << 4));
-    const f32x4 b = *reinterpret_cast<const f32x4 *>(at + (((4 * step + 2 * high + 1) ^ t) << 4));
+    const u32 first = (at + ((2 * high ^ L::turn(row)) << 4)) ^ (step << 6);
+    const f32x4 a = shared_at<f32x4>(first), b = shared_at<f32x4>(first ^ 16);
     return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   }
 }
 
 // The same for the tile transposed: element 32 block + low of the rows 16 step + {4 high .. + 3, 8 + 4 high .. + 3}.
-// bf16: a transposing read hands 16 lanes a column each of 4 rows of 16.
+// bf16: a transposing read hands 16 lanes a column each of 4 rows of 16.  Rows 8 further on have their chunks turned by 2 more.
 template <typename T, int DP>
 __device__ __forceinline__ typename Kind<T>::frag column_frag(const char *tile, int block, int step, int lane) {
   using L = Tile<T, DP>;
   const int high = lane >> 5;
   if constexpr (sizeof(T) == 2) {
-    const int in = lane & 15, chunk = 4 * block + ((lane >> 4) & 1) * 2 + ((in & 3) >> 1);
+    const int in = lane & 15, chunk = ((lane >> 4) & 1) * 2 + ((in & 3) >> 1), row = 4 * high + (in >> 2);
+    const u32 at = offset_of(tile) + row * L::row_bytes + ((chunk ^ L::turn(row)) << 4) + (in & 1) * 8;
     s16x4 got[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int row = 16 * step + 8 * s + 4 * high + (in >> 2);
-      const char *at = tile + row * L::row_bytes + ((chunk ^ L::turn(row)) << 4) + (in & 1) * 8;
-      got[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+      const u32 from = (at ^ (block << 6) ^ (s << 5)) + (16 * step + 8 * s) * L::row_bytes;
+      got[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(from));
     }
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8, s16x8{got[0][0], got[0][1], got[0][2], got[0][3], got[1][0], got[1][1], got[1][2],
