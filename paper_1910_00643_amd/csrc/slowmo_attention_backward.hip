@@ -223,7 +223,8 @@ __device__ __forceinline__ void word_to_shared(u32 shared, u32 offset, const flo
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(shared), "v"(offset), "s"(base) : "memory");
 }
 
-template <typename T, int DP>
+// WHAT: 1 dV, 2 dK, 3 both.
+template <typename T, int DP, int WHAT>
 __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 1)) void k_keys(Args a) {
   using frag = typename Kind<T>::frag;
   constexpr int NB = DP / 32, S = Keys<T, DP>::stages, B = Keys<T, DP>::tile;
@@ -245,13 +246,20 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
   const int jc = mine ? j : keys - 1;
   // this lane's row of dK, dV: worked out where it is written, for want of registers in between
   auto row_of = [&](const Rows &x) SLOWMO_INLINE { return static_cast<T *>(x.data) + (at.begin + jc) * x.token + head * x.head; };
-  f32x16 acck[NB], accv[NB];
+  constexpr bool kV = WHAT & 1, kK = WHAT & 2;
+  constexpr int NK = kK ? NB : 1, NV = kV ? NB : 1;
+  f32x16 acck[NK], accv[NV];
+  auto clear = [&]() SLOWMO_INLINE {
 #pragma unroll
-  for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
+    for (int b = 0; b < NK; ++b) acck[b] = f32x16{};
+#pragma unroll
+    for (int b = 0; b < NV; ++b) accv[b] = f32x16{};
+  };
+  clear();
   if (at.b == a.batch) {
     if (!a.clear || part) return;
-    store_columns<T, NB>(row_of(a.dk), acck, 0.f, a.dim, high, a.wide, mine);
-    store_columns<T, NB>(row_of(a.dv), accv, 0.f, a.dim, high, a.wide, mine);
+    if constexpr (kK) store_columns<T, NB>(row_of(a.dk), acck, 0.f, a.dim, high, a.wide, mine);
+    if constexpr (kV) store_columns<T, NB>(row_of(a.dv), accv, 0.f, a.dim, high, a.wide, mine);
     return;
   }
   int64_t q_begin = at.begin;
@@ -324,9 +332,9 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
   {
     const T *v = row_of(a.v);
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) vf[s] = load_frag<T>(v, 16 * s + 8 * high, a.dim, a.wide);
+    for (int s = 0; s < (kK ? DP / 16 : 0); ++s) vf[s] = load_frag<T>(v, 16 * s + 8 * high, a.dim, a.wide);
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) settle(vf[s]);
+    for (int s = 0; s < (kK ? DP / 16 : 0); ++s) settle(vf[s]);
   }
   for (bool careful = false;; careful = true) {
     if (careful) {
@@ -347,8 +355,8 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
         return p >= my_lo && p <= my_hi && p != kNowhere;
       };
       if (careful) {
-        tame<T, DP, kRows, NB>(q_tile, acck, sees_row);
-        tame<T, DP, kRows, NB>(g_tile, accv, sees_row);
+        if constexpr (kK) tame<T, DP, kRows, NB>(q_tile, acck, sees_row);
+        if constexpr (kV) tame<T, DP, kRows, NB>(g_tile, accv, sees_row);
       }
       const int pa = uniform(st->position[0]), pb = uniform(st->position[kRows - 1]);
       // every row sees every key of the wave, or (rows in order, none missing) none does
@@ -367,7 +375,7 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e) {
         s = mma(row_frag<T, DP>(q_tile, row_lane, e, high), row_frag<T, DP>(k_tile, k_row, e, high), s);
-        dp = mma(row_frag<T, DP>(g_tile, row_lane, e, high), vf[e], dp);
+        if constexpr (kK) dp = mma(row_frag<T, DP>(g_tile, row_lane, e, high), vf[e], dp);
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -376,7 +384,7 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           s[4 * c + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * c + i], a.scale2, -l[i]));
-          dp[4 * c + i] = s[4 * c + i] * (dp[4 * c + i] - d[i]);
+          if constexpr (kK) dp[4 * c + i] = s[4 * c + i] * (dp[4 * c + i] - d[i]);
         }
       }
       if (!all) {
@@ -390,8 +398,8 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
         const frag pf = as_frag<T>(s, half), df = as_frag<T>(dp, half);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          accv[b] = mma(column_frag<T, DP>(g_tile, b, half, column_lane), pf, accv[b]);
-          acck[b] = mma(column_frag<T, DP>(q_tile, b, half, column_lane), df, acck[b]);
+          if constexpr (kV) accv[b] = mma(column_frag<T, DP>(g_tile, b, half, column_lane), pf, accv[b]);
+          if constexpr (kK) acck[b] = mma(column_frag<T, DP>(q_tile, b, half, column_lane), df, acck[b]);
         }
       }
     }
@@ -400,18 +408,20 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) any |= wild(acck[b][i]) || wild(accv[b][i]);
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (kK) any |= wild(acck[b][i]);
+        if constexpr (kV) any |= wild(accv[b][i]);
+      }
     if (!__syncthreads_or(any)) break;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) acck[b] = accv[b] = f32x16{};
+    clear();
   }
   if (pieces.count == 1) {
-    store_columns<T, NB>(row_of(a.dk), acck, a.scale, a.dim, high, a.wide, mine);
-    store_columns<T, NB>(row_of(a.dv), accv, 1.f, a.dim, high, a.wide, mine);
+    if constexpr (kK) store_columns<T, NB>(row_of(a.dk), acck, a.scale, a.dim, high, a.wide, mine);
+    if constexpr (kV) store_columns<T, NB>(row_of(a.dv), accv, 1.f, a.dim, high, a.wide, mine);
   } else {
     float *to = a.sums + ((part * a.keys + at.begin + jc) * a.heads + head) * (2 * DP);
-    store_columns<float, NB>(to, acck, a.scale, DP, high, true, mine);
-    store_columns<float, NB>(to + DP, accv, 1.f, DP, high, true, mine);
+    if constexpr (kK) store_columns<float, NB>(to, acck, a.scale, DP, high, true, mine);
+    if constexpr (kV) store_columns<float, NB>(to + DP, accv, 1.f, DP, high, true, mine);
   }
 }
 
@@ -506,12 +516,23 @@ hipError_t run(Args a, int32_t dtype, const Plan &p, hipStream_t stream) {
     }
     if (a.keys && e == hipSuccess) {
       const int bytes = Keys<T, DP>::bytes(p.k_waves);
-      room(k_keys<T, DP>, bytes);
-      a.slots = slots_of(a.keys, 1, p.k_waves * 32, a.batch);
-      const int64_t items = items_of(a.heads, a.slots * a.parts);
-      for (a.first = 0; a.first < items && e == hipSuccess; a.first += kMostBlocks) {
-        k_keys<T, DP><<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.k_waves, bytes, stream>>>(a);
-        e = hipGetLastError();
+      const auto go = [&](auto kernel) {
+        room(kernel, bytes);
+        a.slots = slots_of(a.keys, 1, p.k_waves * 32, a.batch);
+        const int64_t items = items_of(a.heads, a.slots * a.parts);
+        for (a.first = 0; a.first < items && e == hipSuccess; a.first += kMostBlocks) {
+          kernel<<<static_cast<u32>(std::min(kMostBlocks, items - a.first)), 64 * p.k_waves, bytes, stream>>>(a);
+          e = hipGetLastError();
+        }
+      };
+      // Both sums of heads of 256 do not fit the registers: dV and dK by a pass each, five products for four without
+      // scratch in the loop (4096 tokens of 8 heads of 256 on 2, bf16, the whole gradient 1670 -> 1068 us).  A fifth product
+      // of fp32 takes longer than the scratch (5937 -> 6891).
+      if constexpr (DP == 256 && sizeof(T) == 2) {
+        go(k_keys<T, DP, 1>);
+        if (e == hipSuccess) go(k_keys<T, DP, 2>);
+      } else {
+        go(k_keys<T, DP, 3>);
       }
       if (a.parts > 1) {
         a.slots = slots_of(a.keys, 1, 32, a.batch);
