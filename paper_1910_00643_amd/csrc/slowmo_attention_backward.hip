@@ -5,11 +5,11 @@
 // pass), k_keys has 32 keys to a wave and goes over the rows of the query heads that share them (dK, dV).
 // That is seven products of a pair for five: the scores and g V^T are computed twice.
 //
-// 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 450 us, 916 TFLOP/s of its three products; k_keys 960 us, 573
+// 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 490 us, 841 TFLOP/s of its three products; k_keys 960 us, 573
 // of its four, 32 % of the matrix units' cycles and 40 % of the vector units', which take turns; 30 us to add the pieces.
 //
-// bf16: P and dS are rounded to bf16 where they meet bf16 factors, and g . out takes the rounded result, as it is what a
-// training program keeps: dQ and dK are off by 2.5e-3 to 2.9e-3 of their norm against 64 bits, where their own rounding is 1.7e-3.
+// bf16: P and dS are rounded to bf16 where they meet bf16 factors: dQ, dK and dV are off by 2.4e-3 of their norm against 64
+// bits, where their own rounding is 1.7e-3.
 #include "slowmo_attention.h"
 
 namespace slowmo {
@@ -109,14 +109,23 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   const int64_t at_row = qt * (static_cast<int64_t>(a.heads) * a.group) + qh;
   float lse2 = a.lse[at_row] * kLog2E;
   settle(lse2);
-  if (mine && !high) a.lse2[at_row] = lse2, a.delta[at_row] = delta;
-  for (bool careful = false;; careful = true) {
-    if (careful && walk.count) bring(0);
+  // g . out is off by what `out` was rounded by, which is little beside dS unless few keys have a row's weight: then
+  // dP and g . out all but cancel (two keys, bf16: dQ off by 5e-3 to 0.4 of its norm).  So a row's dS, whose sum
+  // is 0, is summed: the sum is what g . out was off by.  k_keys takes it into account as it is; a tile with rows where it is
+  // more than a share of the sum of |dS| is gone over again with their mended g . out.  bf16: 2^-12 where the rows see up to
+  // four tiles of keys, which makes nearly all of them do so (sentences of 5 to 100 tokens 47 -> 64 us) and leaves dQ off by
+  // 2.4e-3, 3.7e-3 at the most; past that half a step, 2^-8, which few rows reach.  fp32: 2^-21.
+  const float slack = sizeof(T) == 4 ? 1.f / (1 << 21) : walk.count <= 4 ? 1.f / 4096 : 1.f / 256;
+  float off, size;
+  for (bool careful = false, mended = false, again = false;; again = true) {
+    const bool there = again && !careful && walk.count <= 2;  // both tiles are in shared memory still
+    if (again && walk.count && !there) bring(0);
+    off = size = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     for (int u = 0; u < walk.count; ++u) {
       arrive();
-      if (u + 1 < walk.count) bring(u + 1);
+      if (u + 1 < walk.count && !there) bring(u + 1);
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
       if (careful) tame<T, DP, L::rows, NB>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
@@ -145,6 +154,8 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
             if (!sees(sight, j0 + 32 * kb + 8 * (i / 4) + 4 * high + i % 4)) s[i] = 0.f;
         }
 #pragma unroll
+        for (int i = 0; i < 16; ++i) off += s[i], size += fabsf(s[i]);
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
           const frag ds = as_frag<T>(s, half);
 #pragma unroll
@@ -153,14 +164,22 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
         read_ahead<T, 2 * NB, 1, 2, 3>();
       }
     }
-    if (careful) break;
-    int any = 0;
+    off = both_sum(off), size = both_sum(size);
+    if (!careful) {
+      int any = 0;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) any |= wild(acc[b][i]);
-    if (!__syncthreads_or(any)) break;
+        for (int i = 0; i < 16; ++i) any |= wild(acc[b][i]);
+      careful = __syncthreads_or(any);
+      if (careful) continue;
+    }
+    const bool far_off = fabsf(off) > slack * size;
+    if (mended || !__syncthreads_or(far_off)) break;
+    mended = true;
+    if (far_off) delta += off;  // the other rows come out as they were
   }
+  if (mine && !high) a.lse2[at_row] = lse2, a.delta[at_row] = delta + off;
   store_columns<T, NB>(dq, acc, a.scale, a.dim, high, a.wide, mine);
 }
 

@@ -40,6 +40,26 @@ def test_backward(case, dtype):
         U.near(got["dv"][b], want["dv"], tol["dv"], "dv")
 
 
+@pytest.mark.parametrize("dim", [32, 128, 256])
+@pytest.mark.parametrize("times", [1.0, 4.0])
+def test_rows_of_few_keys(dim, times):
+    """Where few keys have a row's weight, g V^T and g . out all but cancel: what the rounding of `out` leaves of them is
+    not what dQ and dK are made of."""
+    lengths = [2, 3, 1, 5, 17, 2, 64, 100]
+    g = torch.Generator(device=DEV).manual_seed(41)
+    n, at = sum(lengths), U.offsets_of(lengths)
+    q = U.rows(g, n, 4, dim, "bf16", times=times)
+    k, v, gout = (U.rows(g, n, h, dim, "bf16") for h in (2, 2, 4))
+    op, offsets = _P().Attention(dim), torch.tensor(at, device=DEV)
+    out, lse = op.forward(q, k, v, offsets)
+    got = dict(zip(("dq", "dk", "dv"), op.backward(gout, q, k, v, out, lse, offsets)))
+    for i, m in enumerate(lengths):
+        s = slice(at[i], at[i + 1])
+        want, tol = U.dense(q[s], k[s], v[s], "bf16", g=gout[s], mended=True)
+        for name, x in got.items():
+            U.near(x[s], want[name], tol[name], name)
+
+
 @pytest.mark.parametrize("window,sinks", [(None, 0), (20, 3)])
 def test_against_differences(window, sinks):
     """The derivative along a direction, from the definition in 64 bits on either side."""
