@@ -53,7 +53,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
             raise RuntimeError("hipcc failed:\n" + r.stderr)
         return r.stderr
 
-    # Every source by itself, side by side: 48 s, one after the other 87 s (8 cores).
+    # Every source by itself, side by side: 70 s for 180 s of processor time (8 cores).
     with tempfile.TemporaryDirectory() as made, ThreadPoolExecutor(len(SOURCES)) as pool:
         objects = [os.path.join(made, s + ".o") for s in SOURCES]
         compile_flags = [f for f in FLAGS if f != "-shared"]

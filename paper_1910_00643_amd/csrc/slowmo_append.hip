@@ -71,8 +71,10 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
   }
   // the first token's sequence by all lanes, then on from there
   const int lane = threadIdx.x & 63;
-  int b = -1;
-  for (int first = 0; first <= a.batch; first += 64) {
+  // (the copy of the pointer keeps the arguments out of scratch memory: 306 us for 131 with a captured)
+  const int64_t *offsets = a.offsets;
+  int b = stretch_of(a.batch, [=](int i) { return offsets[i] <= t0; }) - 1;
+  for (int first = b + 1; first <= a.batch; first += 64) {
     const int got = __popcll(__ballot(first + lane <= a.batch && a.offsets[min(first + lane, a.batch)] <= t0));
     b += got;
     if (got < 64) break;

@@ -317,8 +317,8 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
   const int64_t qt = at_row / (a.heads * a.group);
   const int qh = static_cast<int>(at_row - qt * (a.heads * a.group));
   // the token's sequence: the last one that starts at or before it
-  int count = 0;
-  for (int first = 0; first <= a.batch; first += 64) {
+  int count = stretch_of(a.batch, [&](int b) { return clamped(uniform(a.q_offsets[b]), 0, a.tokens) <= qt; });
+  for (int first = count; first <= a.batch; first += 64) {
     const int b = first + lane;
     const int got = __popcll(__ballot(b <= a.batch && clamped(a.q_offsets[min(b, a.batch)], 0, a.tokens) <= qt));
     count += got;

@@ -26,6 +26,9 @@ LISTS = [  # lengths, hq, hk, dim, window, sinks
     ([3] * 255 + [130], 1, 1, 64, None, 0),                        # as many as one look covers
     ([3] * 256 + [130], 1, 1, 64, None, 0),
     ([1] * 600, 4, 4, 32, None, 0),
+    ([1] * 1023 + [90], 1, 1, 32, None, 0),                        # more than a thousand sequences
+    ([2, 0, 5] * 1000 + [90, 0, 0, 3], 2, 1, 32, None, 0),
+    ([0] * 1500 + [70] + [1] * 1500, 1, 1, 64, 9, 1),
     ([1, 1, 1, 1900], 4, 1, 64, None, 0),                          # one far longer than the average
     ([1, 1, 1, 1900], 4, 1, 64, 100, 2),
     ([2100], 2, 1, 128, 1000, 1500),                               # more sinks than window
@@ -80,6 +83,32 @@ def test_offsets_of_no_meaning_reach_nothing_outside(offsets):
     torch.cuda.synchronize()
     for x, used in zip(whole, (130, 130, 130, 2)):
         assert (x[:100] == 5).all() and (x[100 + used:] == 5).all()
+
+
+def test_thousands_of_running_sequences():
+    """Append and a step of single tokens, some of whose keys are cut into pieces."""
+    g = torch.Generator(device=DEV).manual_seed(35)
+    batch, page = 2500, 16
+    new = [1 if i % 3 else 0 for i in range(batch)]
+    lengths = [3000 if i == 1700 else 1 + i % 40 for i in range(batch)]
+    held = [-(-m // page) for m in lengths]
+    order = torch.randperm(sum(held), device=DEV, generator=g).int()
+    pages = torch.full((batch, max(held)), -1, dtype=torch.int32, device=DEV)
+    row = torch.repeat_interleave(torch.arange(batch), torch.tensor(held)).to(DEV)
+    column = torch.cat([torch.arange(m) for m in held]).to(DEV)
+    pages[row, column] = order
+    kc, vc = (torch.randn(sum(held), page, 1, 64, device=DEV, generator=g) for _ in range(2))
+    q, k, v = (torch.randn(sum(new), h, 64, device=DEV, generator=g) for h in (2, 1, 1))
+    n, at = torch.tensor(lengths, device=DEV), torch.tensor(U.offsets_of(new), device=DEV)
+    op = _P().PagedAttention(64, dtype="f32")
+    op.append(k, v, kc, vc, pages, n, at)
+    out = op.forward(q, kc, vc, pages, n, at)
+    for b in [i for i in range(batch) if new[i] and (i < 5 or i > batch - 6 or i % 200 == 100 or i == 1700)]:
+        j, s = torch.arange(lengths[b], device=DEV), slice(int(at[b]), int(at[b]) + 1)
+        place = pages[b, j // page].long()
+        assert torch.equal(kc[place[-1], (lengths[b] - 1) % page], k[s][0])
+        want, tol = U.dense(q[s], kc[place, j % page], vc[place, j % page], "f32")
+        U.near(out[s], want["out"], tol["out"] * 1.01, "out")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
