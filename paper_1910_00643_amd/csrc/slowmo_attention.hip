@@ -35,6 +35,7 @@ struct Args {
   float scale;  // of scores to powers of two
   Mask mask;
   bool wide, clear;
+  bool apart;  // the keys' rows are not the queries': another list of offsets, or the same one over another number of rows
   int32_t splits, least;  // pieces of the key axis at most; tiles of a piece at least
   float *part, *part_lse;
 };
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
   int keys = at.n;
   if constexpr (PAGED) {
     keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b]), 0, kLongest));
-  } else if (a.k_offsets != a.q_offsets) {
+  } else if (a.apart) {
     k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
     keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
   }
@@ -637,6 +638,7 @@ slowmo_status slowmo_attention(const slowmo_attention_config *cfg, int32_t batch
     fill(a, *cfg, tokens, *q, *out, k->heads);
     a.k = rows_of(*k), a.v = rows_of(*v), a.lse = lse, a.keys = keys, a.batch = batch;
     a.q_offsets = q_offsets, a.k_offsets = k_offsets ? k_offsets : q_offsets;
+    a.apart = a.k_offsets != q_offsets || keys != tokens;
     a.wide = true;
     for (const slowmo_heads *h : every) a.wide = a.wide && wide_rows(*h, cfg->head_dim, cfg->dtype);
     const hipError_t e = launch<false>(a, cfg->dtype, waves_of(tokens, a.group, batch, 4), static_cast<hipStream_t>(stream));

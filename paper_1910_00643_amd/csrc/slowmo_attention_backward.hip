@@ -26,6 +26,7 @@ struct Args {
   float scale, scale2;  // of scores; of scores to powers of two
   Mask mask;
   bool wide, clear;
+  bool apart;  // the keys' rows are not the queries': another list of offsets, or the same one over another number of rows
   int32_t parts, stretch;  // stretches of a sequence's rows, and rows of one: a tile of keys has a workgroup for each
   float *lse2, *delta;  // [tokens][query heads]: lse in powers of two; g . out
   float *sums;          // [parts][keys][key heads][2][padded head]: dK and dV of a piece
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   }
   int64_t k_begin = at.begin;
   int keys = at.n;
-  if (a.k_offsets != a.q_offsets) {
+  if (a.apart) {
     k_begin = clamped(uniform(a.k_offsets[at.b]), 0, a.keys);
     keys = static_cast<int>(clamped(uniform(a.k_offsets[at.b + 1]), k_begin, a.keys) - k_begin);
   }
@@ -283,7 +284,7 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
   }
   int64_t q_begin = at.begin;
   int n = keys;
-  if (a.k_offsets != a.q_offsets) {
+  if (a.apart) {
     q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
     n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
   }
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(256) void k_add(Args a, int width) {
   if (at.b < 0 || at.b == a.batch || static_cast<int64_t>(at.tile) * 32 >= keys) return;
   int64_t q_begin = at.begin;
   int n = keys;
-  if (a.k_offsets != a.q_offsets) {
+  if (a.apart) {
     q_begin = clamped(uniform(a.q_offsets[at.b]), 0, a.tokens);
     n = static_cast<int>(clamped(uniform(a.q_offsets[at.b + 1]), q_begin, a.tokens) - q_begin);
   }
@@ -628,6 +629,7 @@ slowmo_status slowmo_attention_backward(const slowmo_attention_config *cfg, int3
     a.q = rows_of(*q), a.k = rows_of(*k), a.v = rows_of(*v), a.g = rows_of(*g), a.out = rows_of(*out);
     a.dq = rows_of(*dq), a.dk = rows_of(*dk), a.dv = rows_of(*dv);
     a.lse = lse, a.q_offsets = q_offsets, a.k_offsets = k_offsets ? k_offsets : q_offsets;
+    a.apart = a.k_offsets != q_offsets || keys != tokens;
     a.batch = batch, a.heads = k->heads, a.group = q->heads / k->heads, a.dim = d;
     a.by_group = by_group(a.group);
     a.tokens = tokens, a.keys = keys;

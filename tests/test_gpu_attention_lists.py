@@ -154,3 +154,31 @@ def test_two_graphs_replayed_side_by_side():
                 graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("at,tokens,keys", [
+    ([0, 100], 100, 50), ([0, 30, 100], 100, 40), ([0, 30, 100], 50, 100), ([0, 30, 100], 130, 100), ([0, 30, 100], 20, 25),
+    ([0, 900], 900, 40), ([0, 900], 40, 900), ([0, 50], 0, 50), ([0, 50], 50, 0),
+], ids=str)
+def test_one_list_over_unequal_numbers_of_rows(at, tokens, keys, dtype):
+    """The same tensor as both lists: each is cut by its own number of rows, and the rows behind them, NaN here, are not
+    read."""
+    g = torch.Generator(device=DEV).manual_seed(36)
+
+    def inside(n, heads):
+        x = torch.full((n + 1000, heads, 64), float("nan"), device=DEV, dtype=U.TD[dtype])
+        x[:n] = torch.randn(n, heads, 64, device=DEV, generator=g)
+        return x[:n]
+
+    q, k, v, gout = inside(tokens, 4), inside(keys, 2), inside(keys, 2), inside(tokens, 4)
+    op, offsets = _P().Attention(64, dtype=dtype), torch.tensor(at, device=DEV)
+    out, lse = op.forward(q, k, v, offsets, offsets)
+    got = op.backward(gout, q, k, v, out, lse, offsets, offsets)
+    for name, x in zip(("out", "dq", "dk", "dv"), (out, *got)):
+        assert x.isfinite().all(), name
+    for lo, hi in zip(at, at[1:]):
+        a, b = slice(min(lo, tokens), min(hi, tokens)), slice(min(lo, keys), min(hi, keys))
+        want, tol = U.dense(q[a], k[b], v[b], dtype, g=gout[a])
+        for name, x, s in zip(("out", "lse", "dq", "dk", "dv"), (out, lse, *got), (a, a, a, b, b)):
+            U.near(x[s], want[name], tol[name], name)
