@@ -141,7 +141,7 @@ slowmo_status slowmo_cache_append(const slowmo_append_config *cfg, const slowmo_
  *   lse       : device, [tokens][q heads] floats, or NULL
  *   workspace : device, 16-byte aligned, slowmo_paged_attention_bytes() long; NULL if that is 0
  * Pages that no query sees are not looked at.  A query that sees a position whose page lies outside the
- * cache, or past the table's columns, has NaN.  Lengths past 2^30 count as 2^30, below 0 as 0.
+ * cache, or past the table's columns, has NaN, and so has its lse.  Lengths past 2^30 count as 2^30, below 0 as 0.
  * Errors: ARG, ALIGN, NOMEM, HIP.
  */
 size_t slowmo_paged_attention_bytes(const slowmo_attention_config *cfg, const slowmo_pages *pages, int64_t tokens,

@@ -41,11 +41,9 @@ struct Args {
 };
 
 __device__ const u32x4 kNothing[1] = {{0, 0, 0, 0}};
-// NaN in bf16 and in fp32
-__device__ const u32x4 kNoNumber[1] = {{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u}};
 
 // A tile's way from memory to shared memory.  j0: its first position; rows past `keys` take the last one's place
-// and are masked.
+// and are masked.  Positions without a page are zeros: a row that sees one is marked by its sum.
 template <typename T, int DP, bool PAGED>
 struct Stage {
   using L = Tile<T, DP>;
@@ -56,7 +54,10 @@ struct Stage {
     const int column = min(j0 + (lane & (L::rows - 1)), keys - 1) >> a.page_log2;
     return column < a.columns ? a.pages[static_cast<int64_t>(b) * a.pages_stride + column] : -1;
   }
-  template <bool VALUE>
+  // the rows of a tile, a bit each, that have no page
+  __device__ __forceinline__ uint64_t without(int page) const {
+    return __ballot(lane < L::rows && static_cast<u32>(page) >= static_cast<u32>(a.n_pages));
+  }
   __device__ __forceinline__ void load(char *tile, const Rows &x, int64_t page_stride, int64_t begin, int head, int j0,
                                        int page) const {
     const T *base = static_cast<const T *>(x.data) + head * x.head;
@@ -76,7 +77,7 @@ struct Stage {
         for (int e = 0; e < L::E; ++e)
           to[e] = c * L::E + e >= a.dim ? static_cast<T>(0.f)
                   : there               ? from[c * L::E + e]
-                                        : static_cast<T>(VALUE ? __builtin_nanf("") : 0.f);
+                                        : static_cast<T>(0.f);
       }
       return;
     }
@@ -113,7 +114,7 @@ struct Stage {
       const char *p = reinterpret_cast<const char *>(base + static_cast<int64_t>(id) * page_stride +
                                                      ((j0 + r) & ((1 << a.page_log2) - 1)) * x.token + c * L::E);
       if (static_cast<u32>(id) >= static_cast<u32>(a.n_pages))
-        p = reinterpret_cast<const char *>(VALUE ? kNoNumber : kNothing);
+        p = reinterpret_cast<const char *>(kNothing);
       if (c * L::E < a.dim) to_shared(to, p);
     }
   }
@@ -182,12 +183,16 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
   }
   const Stage<T, DP, PAGED> stage{a, keys, lane, wave, waves};
   int page = 0;
+  uint64_t missing[2] = {0, 0};  // of the current tile and of the next one
   auto bring = [&](int u) SLOWMO_INLINE {
     char *to = smem + (u & 1) * 2 * L::bytes;
     const int j0 = walk.at(u) * L::rows;
-    if constexpr (PAGED) settle(page);
-    stage.template load<false>(to, a.k, a.k_page, k_begin, head, j0, page);
-    stage.template load<true>(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
+    if constexpr (PAGED) {
+      settle(page);
+      missing[0] = missing[1], missing[1] = stage.without(page);
+    }
+    stage.load(to, a.k, a.k_page, k_begin, head, j0, page);
+    stage.load(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
     if constexpr (PAGED)
       if (u + 1 < u1) page = stage.page_at(at.b, walk.at(u + 1) * L::rows);
   };
@@ -214,6 +219,7 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
     for (int u = u0; u < u1; ++u) {
       arrive();
       if (u + 1 < u1) bring(u + 1);
+      else missing[0] = missing[1];
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
       if (careful)
@@ -282,6 +288,10 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
         for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, column_lane), p, acc[b]);
       }
       read_ahead<T, NB * L::rows / 16, 1, 2, 3>();
+      if constexpr (PAGED)
+        // NaN in the sum is NaN in the result and in its lse, and survives pieces whose weight underflows
+        for (uint64_t left = missing[0]; left; left &= left - 1)
+          if (sees(sight, j0 + __builtin_ctzll(left))) l = __builtin_nanf("");
     }
     if (careful) break;
     int any = 0;

@@ -339,3 +339,65 @@ def test_an_offset_past_32_bits():
     out = op.forward(q, kc, vc, pages, n, o)
     want, tol = U.dense(q, _gathered(kc, pages[0], 2050), _gathered(vc, pages[0], 2050), "bf16")
     U.near(out, want["out"], tol["out"] * 1.01, "out")
+
+
+def _far_apart(dtype, seqs, times, seed=21):
+    """Sequences whose keys are cut into 40 pieces (one sequence) or 24: one key of each, at position 100 i + 5000, has a
+    score far above the others."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    length = 20000 if seqs == 1 else 12000
+    pages, total = _paged(g, [length] * seqs, 16)
+    kc, vc = (torch.randn(total, 16, 1, 64, device=DEV, generator=g).to(U.TD[dtype]) for _ in range(2))
+    q = U.rows(g, seqs, 4, 64, dtype)
+    q[:] = q[:, :1]                       # all heads of a token ask for the same key
+    for i in range(seqs):
+        at = 5000 + 100 * i
+        kc[pages[i, at // 16], at % 16] = times * q[i, 0]
+    n, at = torch.full((seqs,), length, device=DEV), torch.arange(seqs + 1, device=DEV)
+    from paper_1910_00643_amd import attention as A
+    cfg = A.slowmo_attention_config(dtype=A._DTYPE[dtype], head_dim=64, causal=1, clear_rest=0, scale=0.125)
+    assert A.lib().slowmo_paged_attention_bytes(cfg, A.slowmo_pages(seqs, pages.shape[1], pages.shape[1]), seqs, 4,
+                                                A.slowmo_cache(None, 1, 16, total)) > 0
+    return q, kc, vc, pages, n, at, total
+
+
+@pytest.mark.parametrize("times", [0.0, 60.0])   # scores of up to 1 and of some 300 beside it: weights underflow
+@pytest.mark.parametrize("seqs", [1, 40])        # many pieces, joined by a workgroup a row, and few, by a wave
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_page_missing_in_one_of_several_pieces(dtype, seqs, times):
+    q, kc, vc, pages, n, at, total = _far_apart(dtype, seqs, times)
+    op = _P().PagedAttention(64, dtype=dtype)
+    want, want_lse = op.forward(q, kc, vc, pages, n, at, return_lse=True)
+    assert want.isfinite().all() and want_lse.isfinite().all()
+    bad = pages.clone()
+    gone = torch.arange(seqs, device=DEV) % 3 == 0
+    for i in range(0, seqs, 3):
+        bad[i, (i * 31) % 600] = total if i % 2 else -1
+    got, lse = op.forward(q, kc, vc, bad, n, at, return_lse=True)
+    assert got[gone].isnan().all() and lse[gone].isnan().all()
+    assert torch.equal(got[~gone], want[~gone]) and torch.equal(lse[~gone], want_lse[~gone])
+    # the table ends before the sequence: the positions without a column are the last ones
+    got, lse = op.forward(q, kc, vc, pages[:, :-1].contiguous(), n, at, return_lse=True)
+    assert got.isnan().all() and lse.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_missing_page_marks_the_queries_that_see_it(dtype):
+    """And their lse, in one piece or several: no other row."""
+    g = torch.Generator(device=DEV).manual_seed(22)
+    pages, total = _paged(g, [9000], 16)
+    kc, vc = (torch.randn(total, 16, 2, 64, device=DEV, generator=g).to(U.TD[dtype]) for _ in range(2))
+    q = U.rows(g, 300, 4, 64, dtype)
+    n, at = torch.tensor([9000], device=DEV), torch.tensor([0, 300], device=DEV)
+    position = torch.arange(8700, 9000, device=DEV)
+    for window, sinks, column in ((None, 0, 550), (None, 0, 3), (100, 0, 548), (4000, 20, 1), (4000, 20, 300)):
+        op = _P().PagedAttention(64, dtype=dtype, window=window, sinks=sinks)
+        want, want_lse = op.forward(q, kc, vc, pages, n, at, return_lse=True)
+        bad = pages.clone()
+        bad[0, column] = -1
+        j = torch.arange(column * 16, column * 16 + 16, device=DEV)[None]
+        p = position[:, None]
+        gone = ((j <= p) & ((p - j < (window or 1 << 30)) | (j < sinks))).any(1)
+        got, lse = op.forward(q, kc, vc, bad, n, at, return_lse=True)
+        assert got[gone].isnan().all() and lse[gone].isnan().all(), (window, sinks, column)
+        assert torch.equal(got[~gone], want[~gone]) and torch.equal(lse[~gone], want_lse[~gone]), (window, sinks, column)
