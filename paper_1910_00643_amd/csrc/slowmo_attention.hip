@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[b][i] *= by;
+          for (int i = 0; i < 16; ++i) acc[b][i] = careful && wild(acc[b][i]) ? acc[b][i] : acc[b][i] * by;  // by may be 0
         m = now;
       }
       const float under = m == -INFINITY ? 0.f : m;

@@ -150,3 +150,18 @@ def test_another_stream():
         got = op.forward(q, k, v, at)[0]
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("times", [1.0, 60.0])      # 60: a later score is some 300 higher, by which the sums are brought down
+@pytest.mark.parametrize("where", [0, 3, 100, 290])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_an_infinite_value_that_is_seen_stays_one(dtype, where, times):
+    case = ([300], None, 2, 1, 64, True, None, 0, 0, 0)
+    op, q, k, v, at, _, _ = _inputs(case, dtype)
+    q[:] = q[250, 0]
+    k[200] = times * q[250, 0]
+    want, want_lse = op.forward(q, k, v, at)
+    v[where, 0, 5], v[where, 0, 40] = float("inf"), -float("inf")
+    want[where:, :, 5], want[where:, :, 40] = float("inf"), -float("inf")
+    out, lse = op.forward(q, k, v, at)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
