@@ -315,7 +315,8 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
   }
 }
 
-// The pieces of a row joined in their order.  WAVES = 1: a wave a row, for up to 32 pieces; 4: a workgroup a row, every
+// The pieces of a row joined in their order.  What is wild in one, a key's value that the row sees, stays so if its weight
+// underflows.  WAVES = 1: a wave a row, for up to 32 pieces; 4: a workgroup a row, every
 // fourth piece to a wave.  4 elements to a lane.
 template <typename T, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
@@ -375,12 +376,12 @@ __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
       w[e] = WAVES == 1 ? __shfl(weight, y) : weights[y / 64][y % 64];
       if (y0 + WAVES * e >= pieces) w[e] = 0.f;
       v[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (4 * lane < DP && w[e] != 0.f) v[e] = *reinterpret_cast<const f32x4 *>(a.part + (y * every + at_row) * DP + 4 * lane);
+      if (4 * lane < DP && y0 + WAVES * e < pieces) v[e] = *reinterpret_cast<const f32x4 *>(a.part + (y * every + at_row) * DP + 4 * lane);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[i] += w[e] * v[e][i];
+      for (int i = 0; i < 4; ++i) sum[i] += wild(v[e][i]) ? v[e][i] : w[e] * v[e][i];
   }
   float total = weight;
   if constexpr (WAVES > 1) {

@@ -401,3 +401,20 @@ def test_a_missing_page_marks_the_queries_that_see_it(dtype):
         got, lse = op.forward(q, kc, vc, bad, n, at, return_lse=True)
         assert got[gone].isnan().all() and lse[gone].isnan().all(), (window, sinks, column)
         assert torch.equal(got[~gone], want[~gone]) and torch.equal(lse[~gone], want_lse[~gone]), (window, sinks, column)
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")], ids=str)
+@pytest.mark.parametrize("times", [0.0, 60.0])
+@pytest.mark.parametrize("seqs", [1, 40])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_wild_value_in_one_of_several_pieces(dtype, seqs, times, what):
+    """A value that a query sees has a part in its result, however small its probability; no other element has."""
+    q, kc, vc, pages, n, at, total = _far_apart(dtype, seqs, times)
+    op = _P().PagedAttention(64, dtype=dtype)
+    want, want_lse = op.forward(q, kc, vc, pages, n, at, return_lse=True)
+    for i in range(0, seqs, 3):
+        vc[pages[i, (i * 31) % 600], 5, 0, 7 + i % 50] = what
+        want[i, :, 7 + i % 50] = what
+    got, lse = op.forward(q, kc, vc, pages, n, at, return_lse=True)
+    assert torch.equal(got.nan_to_num(1e30), want.nan_to_num(1e30)) and torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(lse, want_lse)
