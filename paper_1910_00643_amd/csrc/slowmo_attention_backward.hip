@@ -3,7 +3,8 @@
 // Two passes over the visible pairs, each the owner of what it sums, so that nothing is added by atomics: k_queries
 // has 32 queries to a wave and goes over the keys (dQ; it also leaves each row's g . out and its statistics for the other
 // pass), k_keys has 32 keys to a wave and goes over the rows of the query heads that share them (dK, dV).
-// That is seven products of a pair for five: the scores and g V^T are computed twice.
+// That is seven products of a pair for five: the scores and g V^T are computed twice.  bf16: nine, they are computed once more
+// for an exact g . out.
 //
 // 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 490 us, 841 TFLOP/s of its three products; k_keys 960 us, 573
 // of its four, 32 % of the matrix units' cycles and 40 % of the vector units', which take turns; 30 us to add the pieces.
@@ -110,14 +111,17 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   const int64_t at_row = qt * (static_cast<int64_t>(a.heads) * a.group) + qh;
   float lse2 = a.lse[at_row] * kLog2E;
   settle(lse2);
-  // g . out is off by what `out` was rounded by, which is little beside dS unless few keys have a row's weight: then
-  // dP and g . out all but cancel (two keys, bf16: dQ off by 5e-3 to 0.4 of its norm).  So a row's dS, whose sum
-  // is 0, is summed: the sum is what g . out was off by.  k_keys takes it into account as it is; a tile with rows where it is
-  // more than a share of the sum of |dS| is gone over again with their mended g . out.  bf16: 2^-12 where the rows see up to
-  // four tiles of keys, which makes nearly all of them do so (sentences of 5 to 100 tokens 47 -> 64 us) and leaves dQ off by
-  // 2.4e-3, 3.7e-3 at the most; past that half a step, 2^-8, which few rows reach.  fp32: 2^-21.
-  const float slack = sizeof(T) == 4 ? 1.f / (1 << 21) : walk.count <= 4 ? 1.f / 4096 : 1.f / 256;
+  // g . out is off by what `out` was rounded by, and where keys or values have something in common, or few keys have a row's
+  // weight, that is far from little beside dS, which is what is left when dP and g . out all but cancel.  A row's dS sums to 0, so
+  // the sum of P (dP - g . out) is what g . out is off by.  bf16: a first pass, of the two products that dS takes, is for that
+  // sum alone (2048 causal tokens, D = 128, keys and values around a vector of deviation 1 each: dQ off by 2.9e-3 of
+  // its norm, 4.4e-2 with g . out as it is, 3.5e-2 where only rows are mended that it is 2^-8 of the sum of |dS| off in).  Five
+  // products for three: the gradient's call for 8192 tokens of 16 heads of 128 takes 1932 us for 1659.  fp32: the pass that
+  // forms dQ sums it too, and is made again where it is more than 2^-21 of the sum of |dS|: dQ is then nearer 64 bits than
+  // that of elementary fp32 operations is.
+  constexpr bool kMends = sizeof(T) == 4;
   float off, size;
+  bool forms = kMends;  // whether the pass forms dQ
   for (bool careful = false, mended = false, again = false;; again = true) {
     const bool there = again && !careful && walk.count <= 2;  // both tiles are in shared memory still
     if (again && walk.count && !there) bring(0);
@@ -154,8 +158,11 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
           for (int i = 0; i < 16; ++i)
             if (!sees(sight, j0 + 32 * kb + 8 * (i / 4) + 4 * high + i % 4)) s[i] = 0.f;
         }
+        if (kMends || !forms) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) off += s[i], size += fabsf(s[i]);
+          for (int i = 0; i < 16; ++i) off += s[i], size += fabsf(s[i]);
+        }
+        if (!forms) continue;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const frag ds = as_frag<T>(s, half);
@@ -165,7 +172,12 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
         read_ahead<T, 2 * NB, 1, 2, 3>();
       }
     }
-    off = both_sum(off), size = both_sum(size);
+    off = both_sum(off);
+    if (!forms) {
+      delta += off, forms = true;
+      __syncthreads();  // this pass's reads of shared memory are done
+      continue;
+    }
     if (!careful) {
       int any = 0;
 #pragma unroll
@@ -175,7 +187,11 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
       careful = __syncthreads_or(any);
       if (careful) continue;
     }
-    const bool far_off = fabsf(off) > slack * size;
+    if (!kMends) {
+      off = 0.f;
+      break;
+    }
+    const bool far_off = fabsf(off) > both_sum(size) * (1.f / (1 << 21));
     if (mended || !__syncthreads_or(far_off)) break;
     mended = true;
     if (far_off) delta += off;  // the other rows come out as they were
