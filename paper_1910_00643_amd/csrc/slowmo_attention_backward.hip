@@ -124,16 +124,24 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   bool forms = kMends;  // whether the pass forms dQ
   for (bool careful = false, mended = false, again = false;; again = true) {
     const bool there = again && !careful && walk.count <= 2;  // both tiles are in shared memory still
-    if (again && walk.count && !there) bring(0);
+    if (again && walk.count && !there && !careful) bring(0);
     off = size = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     for (int u = 0; u < walk.count; ++u) {
-      arrive();
-      if (u + 1 < walk.count && !there) bring(u + 1);
-      char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
+      if (careful) __syncthreads();
+      else arrive();
+      const int next = careful ? u : u + 1;
+      if (next < walk.count && !there) bring(next);
+      char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes, *column_tile = k_tile;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
-      if (careful) tame<T, DP, L::rows, NB>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); });
+      if (careful) {
+        // The scores want the keys as they are: a wild one that a row of finite lse sees has -infinity there, and no weight.
+        // The product with dS takes them from the next tile's place, which comes after this one here.
+        arrive();
+        column_tile = smem + (~u & 1) * 2 * L::bytes;
+        tame<T, DP, L::rows, NB, true>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); }, column_tile);
+      }
       if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
       // wide heads: addresses worked out anew for each tile; kept, they would be spilled to scratch
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
         for (int half = 0; half < 2; ++half) {
           const frag ds = as_frag<T>(s, half);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(k_tile, b, 2 * kb + half, column_lane), ds, acc[b]);
+          for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(column_tile, b, 2 * kb + half, column_lane), ds, acc[b]);
         }
         read_ahead<T, 2 * NB, 1, 2, 3>();
       }

@@ -198,3 +198,25 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for w, y in zip(want, got):
         assert all(torch.equal(a, b) for a, b in zip(w, y))
+
+
+@pytest.mark.parametrize("window", [None, 70])
+@pytest.mark.parametrize("dim", [32, 64, 128, 192])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_key_whose_score_is_minus_infinity(dtype, dim, window):
+    """It has no weight: the element that holds the infinity gets 0 times it, and every other gradient is that of a key far
+    below the others."""
+    case = ([200], None, 4, 2, dim, True, window, 0, 0, 0)
+    op, q, k, v, at, _, g = _inputs(case, dtype)
+    gout = _grad(q, dtype, g)
+    q[:, :, 6] = q[:, :, 6].abs() + 1
+    k[100, :, 6] = -1e5
+    out, lse = op.forward(q, k, v, at)
+    want = op.backward(gout, q, k, v, out, lse, at)
+    k[100, :, 6] = -float("inf")
+    assert all(torch.equal(a, b) for a, b in zip(op.forward(q, k, v, at), (out, lse)))
+    dq, dk, dv = op.backward(gout, q, k, v, out, lse, at)
+    rest = [d for d in range(dim) if d != 6]
+    assert torch.equal(dq[:, :, rest], want[0][:, :, rest]) and torch.equal(dk, want[1]) and torch.equal(dv, want[2])
+    seen = U.visible(200, 200, True, window, 0)[:, 100]
+    assert dq[seen][:, :, 6].isnan().all() and torch.equal(dq[~seen], want[0][~seen])
