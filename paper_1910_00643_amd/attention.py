@@ -142,7 +142,9 @@ class _Holder:
         if window is not None and window < 1 or sinks < 0:
             raise ValueError("window must be at least 1, or None for any distance, and sinks at least 0")
         return dict(dtype=_DTYPE[dtype], head_dim=self.head_dim, causal=int(bool(causal)),
-                    scale=float(self.head_dim) ** -0.5 if scale is None else scale, window=int(window or 0), sinks=int(sinks))
+                    scale=float(self.head_dim) ** -0.5 if scale is None else scale,
+                    # past every length; ctypes would keep the last 64 bits alone
+                    window=min(int(window or 0), 1 << 62), sinks=min(int(sinks), 1 << 62))
 
 
 class Attention(_Holder):

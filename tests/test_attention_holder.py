@@ -171,3 +171,10 @@ def test_two_threads_on_one_handle(library):
     for name, b, tokens in (("first", 1 << 20, 5), ("second", 2 << 20, 7)):
         assert library.seen[name] == (2, b + 64, None, tokens, 5, b, b + 4096, b + 8192, b + 12288, 0)
     assert paged._cfg.causal == 1
+
+
+@pytest.mark.parametrize("many", [1 << 62, (1 << 63) - 1, 1 << 63, (1 << 64) + 1, 10 ** 30])
+def test_windows_and_sinks_past_64_bits_are_past_every_length(many):
+    for op in (A.Attention(64, window=many, sinks=many), A.PagedAttention(64, window=many, sinks=many)):
+        for cfg in (op._cleared, op._kept if isinstance(op, A.Attention) else op._cfg):
+            assert cfg.window >= 1 << 30 and cfg.sinks >= 1 << 30
