@@ -214,3 +214,19 @@ def test_append_of_nothing():
     for k, v in ((_cache(0x300000, token=256, page_stride=16 * 256), _cache(0x300000 + 256, token=256, page_stride=16 * 256)),
                  (_cache(0x300000, page_stride=2 * 16 * 128), _cache(0x300000 + 16 * 256, page_stride=2 * 16 * 128))):
         assert _append(k_cache=k, v_cache=v, pages=_pages(batch=0)) == B.SLOWMO_OK
+
+
+def test_outputs_beside_inputs_in_one_array_pass():
+    """Rows of q, k, v and out in turn.  What is refused is the lse, which lies in out's last row, behind the inputs, and is
+    looked at after them."""
+    at, token, tokens = 0x100000, 10 * 64, 100
+    q, k, v, out = (slowmo_heads(at + 2 * 64 * i, n, token, 64) for i, n in ((0, 4), (4, 1), (5, 1), (6, 4)))
+    lse = at + 2 * (token * (tokens - 1) + 6 * 64)
+    assert _forward(q=q, k=k, v=v, out=out, tokens=tokens, keys=tokens, lse=lse) == ARG
+    assert P.slowmo_last_error(None) == "out and lse overlap"
+    # one element nearer, out reaches into v
+    assert _forward(q=q, k=k, v=v, out=slowmo_heads(out.data - 2, 4, token, 64), tokens=tokens, keys=tokens, lse=None) == ARG
+    assert P.slowmo_last_error(None) == "an output overlaps an input"
+    # rows of another length are not beside them
+    assert _forward(q=q, k=k, v=v, out=slowmo_heads(out.data, 4, token + 64, 64), tokens=tokens, keys=tokens, lse=None) == ARG
+    assert P.slowmo_last_error(None) == "an output overlaps an input"

@@ -418,3 +418,32 @@ def test_a_wild_value_in_one_of_several_pieces(dtype, seqs, times, what):
     got, lse = op.forward(q, kc, vc, pages, n, at, return_lse=True)
     assert torch.equal(got.nan_to_num(1e30), want.nan_to_num(1e30)) and torch.equal(got.isnan(), want.isnan())
     assert torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 0), (60, 5)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_without_a_causal_mask(dtype, window, sinks):
+    """Through the C entry, which takes it: new tokens that see each other, in one piece and in several."""
+    from paper_1910_00643_amd import attention as A
+    g = torch.Generator(device=DEV).manual_seed(23)
+    new, lengths = [40, 0, 3, 1], [100, 7, 9000, 50]
+    pages, total = _paged(g, lengths, 16)
+    kc, vc = (torch.randn(total, 16, 2, 64, device=DEV, generator=g).to(U.TD[dtype]) for _ in range(2))
+    q = U.rows(g, 44, 4, 64, dtype)
+    at = U.offsets_of(new)
+    n, o = torch.tensor(lengths, device=DEV), torch.tensor(at, device=DEV)
+    out, lse = torch.empty_like(q), torch.empty(44, 4, device=DEV)
+    cfg = A.slowmo_attention_config(dtype=A._DTYPE[dtype], head_dim=64, causal=0, clear_rest=0, scale=0.125, window=window, sinks=sinks)
+    table = A.slowmo_pages(4, pages.shape[1], pages.shape[1], pages.data_ptr(), n.data_ptr(), o.data_ptr())
+    k, v = (A.slowmo_cache(c.data_ptr(), 2, 16, total, 16 * 128, 128, 64) for c in (kc, vc))
+    rows = [A.slowmo_heads(x.data_ptr(), 4, 256, 64) for x in (q, out)]
+    need = A.lib().slowmo_paged_attention_bytes(cfg, table, 44, 4, k)
+    space = torch.empty(need, dtype=torch.uint8, device=DEV)
+    assert A.lib().slowmo_paged_attention(cfg, table, 44, rows[0], k, v, rows[1], lse.data_ptr(), space.data_ptr() if need else None,
+                                          need, torch.cuda.current_stream().cuda_stream or None) == 0
+    for b, m in enumerate(lengths):
+        s = slice(at[b], at[b + 1])
+        want, tol = U.dense(q[s], _gathered(kc, pages[b], m), _gathered(vc, pages[b], m), dtype, causal=False, window=window or None,
+                            sinks=sinks)
+        U.near(out[s], want["out"], tol["out"] * 1.01, "out")
+        U.near(lse[s], want["lse"], tol["lse"], "lse")
