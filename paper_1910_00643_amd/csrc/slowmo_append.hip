@@ -54,9 +54,10 @@ __global__ __launch_bounds__(256) void k_append(Args a) {
   const int half = a.rot / 2, pieces = INTER ? a.rot / V : half / V;  // that turn
   const bool turns = which != 1 && piece < pieces;
   const int d = turns ? piece * V : which == 1 ? piece * C : a.rot + (piece - pieces) * C;
-  // the elements are asked for beside the token's place, which takes several trips to memory one after the other
+  // The elements are asked for beside the token's place, which takes several trips to memory one after the other; those of
+  // rows behind the last sequence, which may not be there yet, are not (no difference for 48 or 25 393 tokens).
   P x[kHeads], y[kHeads];
-  if (t < a.tokens) {
+  if (t < min(a.tokens, a.offsets[a.batch])) {
     const T *from = static_cast<const T *>(a.side[which].data) + t * a.side[which].token + head * a.side[which].head + d;
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
