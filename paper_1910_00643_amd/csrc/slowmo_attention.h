@@ -447,34 +447,36 @@ __device__ __forceinline__ T *element(char *tile, int row, int d) {
 }
 
 // Where a row of a tile is seen by some columns of a product only, what is wild in it must not meet the
-// others' zeros (0 times infinity).  Only a pass whose result came out wild is done again with this, tile by
-// tile: what is wild is added to the columns that see it and then taken out of the tile.  Where the tile is a factor of
-// something else as well (COPY), it stays as it is and `to` is what it would be; a column that sees what is wild there, and is
-// not NaN anyway, sees it times a zero of its own, which is NaN.  `seen(row)`: whether the lane's column sees the tile's
-// row.  All waves of the workgroup come here.
-template <typename T, int DP, int ROWS, int NB, bool COPY = false, typename F>
-__device__ __forceinline__ void tame(char *tile, f32x16 (&acc)[NB], F &&seen, char *to = nullptr) {
-  const int high = (threadIdx.x & 63) >> 5;
+// others' zeros (0 times infinity).  Only a pass whose result came out wild is done again, tile by tile, with what is wild
+// taken out of the tiles (tame, or, where the tile is a factor of something else as well, a copy without it) and added to
+// the columns that see it (add_wild).  All waves of the workgroup come to these.
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ bool any_wild(char *tile) {
   int any = 0;
   for (int i = threadIdx.x; i < ROWS * DP; i += blockDim.x)
     any |= wild(static_cast<float>(*element<T, DP>(tile, i / DP, i % DP)));
-  any = __syncthreads_or(any);
-  if (!COPY && !any) return;
-  for (int row = 0; any && row < ROWS; ++row) {
+  return __syncthreads_or(any);
+}
+// `seen(row)`: whether the lane's column sees the tile's row.  `times` what is wild: 0 makes NaN of it.
+template <typename T, int DP, int ROWS, int NB, typename F>
+__device__ __forceinline__ void add_wild(char *tile, f32x16 (&acc)[NB], float times, F &&seen) {
+  const int high = (threadIdx.x & 63) >> 5;
+  for (int row = 0; row < ROWS; ++row) {
     const bool mine = seen(row);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float v = static_cast<float>(*element<T, DP>(tile, row, 32 * b + 8 * (i / 4) + 4 * high + i % 4));
-        if (mine && wild(v)) acc[b][i] += COPY ? v * 0.f : v;
+        if (mine && wild(v)) acc[b][i] += v * times;
       }
   }
-  if (!COPY) __syncthreads();
+}
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ void tame(char *to, char *tile) {
   for (int i = threadIdx.x; i < ROWS * DP; i += blockDim.x) {
-    T *e = element<T, DP>(tile, i / DP, i % DP);
-    if constexpr (COPY) *element<T, DP>(to, i / DP, i % DP) = wild(static_cast<float>(*e)) ? static_cast<T>(0.f) : *e;
-    else if (wild(static_cast<float>(*e))) *e = static_cast<T>(0.f);
+    const T e = *element<T, DP>(tile, i / DP, i % DP);
+    *element<T, DP>(to, i / DP, i % DP) = wild(static_cast<float>(e)) ? static_cast<T>(0.f) : e;
   }
   __syncthreads();
 }

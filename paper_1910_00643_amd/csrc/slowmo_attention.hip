@@ -54,9 +54,9 @@ struct Stage {
     const int column = min(j0 + (lane & (L::rows - 1)), keys - 1) >> a.page_log2;
     return column < a.columns ? a.pages[static_cast<int64_t>(b) * a.pages_stride + column] : -1;
   }
-  // the rows of a tile, a bit each, that have no page
+  // the rows of a tile, a bit each (twice, where they are 32), that have no page
   __device__ __forceinline__ uint64_t without(int page) const {
-    return __ballot(lane < L::rows && static_cast<u32>(page) >= static_cast<u32>(a.n_pages));
+    return __ballot(static_cast<u32>(page) >= static_cast<u32>(a.n_pages));
   }
   __device__ __forceinline__ void load(char *tile, const Rows &x, int64_t page_stride, int64_t begin, int head, int j0,
                                        int page) const {
@@ -183,13 +183,13 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
   }
   const Stage<T, DP, PAGED> stage{a, keys, lane, wave, waves};
   int page = 0;
-  uint64_t missing[2] = {0, 0};  // of the current tile and of the next one
+  bool gone = false;  // some position of a tile has no page
   auto bring = [&](int u) SLOWMO_INLINE {
     char *to = smem + (u & 1) * 2 * L::bytes;
     const int j0 = walk.at(u) * L::rows;
     if constexpr (PAGED) {
       settle(page);
-      missing[0] = missing[1], missing[1] = stage.without(page);
+      gone = gone || stage.without(page);
     }
     stage.load(to, a.k, a.k_page, k_begin, head, j0, page);
     stage.load(to + L::bytes, a.v, a.v_page, k_begin, head, j0, page);
@@ -219,11 +219,9 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
     for (int u = u0; u < u1; ++u) {
       arrive();
       if (u + 1 < u1) bring(u + 1);
-      else missing[0] = missing[1];
       char *k_tile = smem + (u & 1) * 2 * L::bytes, *v_tile = k_tile + L::bytes;
       const int j0 = walk.at(u) * L::rows, j1 = j0 + L::rows - 1;
-      if (careful)
-        tame<T, DP, L::rows, NB>(v_tile, acc, [&](int r) { return sees(sight, j0 + r); });
+      if (careful && any_wild<T, DP, L::rows>(v_tile)) tame<T, DP, L::rows>(v_tile, v_tile);
       // the wave has no row, or none that sees a key of the tile
       if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       // Wide heads: addresses are worked out anew for each tile; kept, they would be spilled to scratch, and reading them
@@ -269,7 +267,7 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[b][i] = careful && wild(acc[b][i]) ? acc[b][i] : acc[b][i] * by;  // by may be 0
+          for (int i = 0; i < 16; ++i) acc[b][i] *= by;
         m = now;
       }
       const float under = m == -INFINITY ? 0.f : m;
@@ -288,12 +286,20 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
         for (int b = 0; b < NB; ++b) acc[b] = mma(column_frag<T, DP>(v_tile, b, st, column_lane), p, acc[b]);
       }
       read_ahead<T, NB * L::rows / 16, 1, 2, 3>();
-      if constexpr (PAGED)
-        // NaN in the sum is NaN in the result and in its lse, and survives pieces whose weight underflows
-        for (uint64_t left = missing[0]; left; left &= left - 1)
-          if (sees(sight, j0 + __builtin_ctzll(left))) l = __builtin_nanf("");
     }
-    if (careful) break;
+    if (careful) {
+      // what is wild comes to the sums that are no longer brought down, by 0 at times, to a higher maximum
+      __syncthreads();
+      start();
+      for (int u = u0; u < u1; ++u) {
+        arrive();
+        if (u + 1 < u1) bring(u + 1);
+        char *v_tile = smem + (u & 1) * 2 * L::bytes + L::bytes;
+        const int j0 = walk.at(u) * L::rows;
+        if (any_wild<T, DP, L::rows>(v_tile)) add_wild<T, DP, L::rows>(v_tile, acc, 1.f, [&](int r) { return sees(sight, j0 + r); });
+      }
+      break;
+    }
     int any = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -302,6 +308,13 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
     // also ends this pass's reads of shared memory
     if (!__syncthreads_or(any)) break;
   }
+  if constexpr (PAGED)
+    // NaN in a row's sum is NaN in its result and lse, and survives pieces whose weight underflows
+    for (int u = u0; gone && u < u1; ++u) {
+      const int j0 = walk.at(u) * L::rows;
+      for (uint64_t left = stage.without(stage.page_at(at.b, j0)); left; left &= left - 1)
+        if (sees(sight, j0 + __builtin_ctzll(left) % L::rows)) l = __builtin_nanf("");
+    }
   l = both_sum(l);
   const float by = l == 0.f ? 0.f : 1.f / l;
   const float log2_sum = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);

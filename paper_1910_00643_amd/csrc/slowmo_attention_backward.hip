@@ -139,8 +139,10 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
         // The scores want the keys as they are: a wild one that a row of finite lse sees has -infinity there, and no weight.
         // The product with dS takes them from the next tile's place, which comes after this one here.
         arrive();
+        // A row that sees one, and is not NaN anyway, sees it times 0.
         column_tile = smem + (~u & 1) * 2 * L::bytes;
-        tame<T, DP, L::rows, NB, true>(k_tile, acc, [&](int r) { return sees(sight, j0 + r); }, column_tile);
+        if (any_wild<T, DP, L::rows>(k_tile)) add_wild<T, DP, L::rows>(k_tile, acc, 0.f, [&](int r) { return sees(sight, j0 + r); });
+        tame<T, DP, L::rows>(column_tile, k_tile);
       }
       if (idle || ((j0 > last.hi || j1 < first.lo) && j0 >= last.sinks)) continue;
       const bool all = (j0 >= last.lo && j1 <= first.hi) || j1 < first.sinks;
@@ -399,8 +401,16 @@ __global__ __launch_bounds__((64 * Keys<T, DP>::waves), (kTwoWaves<T, DP> ? 2 : 
         return p >= my_lo && p <= my_hi && p != kNowhere;
       };
       if (careful) {
-        if constexpr (kK) tame<T, DP, kRows, NB>(q_tile, acck, sees_row);
-        if constexpr (kV) tame<T, DP, kRows, NB>(g_tile, accv, sees_row);
+        if (kK && any_wild<T, DP, kRows>(q_tile)) {
+          if constexpr (kK) add_wild<T, DP, kRows>(q_tile, acck, 1.f, sees_row);
+          __syncthreads();
+          tame<T, DP, kRows>(q_tile, q_tile);
+        }
+        if (kV && any_wild<T, DP, kRows>(g_tile)) {
+          if constexpr (kV) add_wild<T, DP, kRows>(g_tile, accv, 1.f, sees_row);
+          __syncthreads();
+          tame<T, DP, kRows>(g_tile, g_tile);
+        }
       }
       const int pa = uniform(st->position[0]), pb = uniform(st->position[kRows - 1]);
       // every row sees every key of the wave, or (rows in order, none missing) none does
