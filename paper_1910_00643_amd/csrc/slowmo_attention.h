@@ -78,7 +78,7 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
 }
 
 // m0 is written and read within the block, with the one wait between that the two need; no vector register
-// is written.
+// is written.  The compiler keeps m0 to itself (named as clobbered it warns of it) and has no other use for it in these kernels.
 __device__ __forceinline__ void to_shared(u32 shared, u32 offset, const void *base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(shared), "v"(offset), "s"(base)
                : "memory");
@@ -332,8 +332,8 @@ __device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
                                            static_cast<u32>(__builtin_amdgcn_readlane(w[1], lane))});
 }
 // The first entry of a stretch of at most 256 that holds the last one that `before` is true of (it is true up to some
-// entry and false from there on): halved down to that from 1024 sequences on, 3 to 6 single entries in place of 4 to 32
-// stretches.  One token of each of 1024 and 8192 sequences over a cache of 50 each, 8 heads of 64: 29.8 -> 26.3 us and
+// entry and false from there on): halved down to that from 1024 sequences on, for 1024 to 8192 of them 3 to 6 single entries in
+// place of 4 to 32 stretches, for 2^20, the most, 13 in place of 4096.  One token of each of 1024 and 8192 sequences over a cache of 50 each, 8 heads of 64: 29.8 -> 26.3 us and
 // 464 -> 167 us.
 template <typename F>
 __device__ __forceinline__ int stretch_of(int batch, F &&before) {
@@ -539,8 +539,6 @@ inline int waves_of(int64_t tokens, int64_t group, int64_t batch, int most) {
   while (waves < most && waves * 32 < rows) waves *= 2;
   return waves;
 }
-
-
 
 inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 inline size_t size_of(int32_t dtype) { return dtype == SLOWMO_BF16 ? 2 : 4; }

@@ -6,10 +6,10 @@
 // result's sums stay in a wave's registers.  Where rows are few the key axis is cut into pieces, which a second kernel joins.
 //
 // Long prompts are bound by the matrix and the vector units of a SIMD, which take turns (43 % and 51 % of the cycles), at the
-// clock that their power leaves (1.8 GHz): 8192 tokens of 32 heads of 128, bf16, 599 us, 918 TFLOP/s of the 1123 of a large
-// matrix product; with a window of 2048, 16 384 tokens of 8 heads, 170 us, 760.  Single tokens are bound by memory: 48 over
-// caches of up to 16 000 positions 359 us, 4.4 TB/s of a large copy's 4.6; one over 131 070 134 us, of which 15 join 256
-// pieces.  fp32 (61 x 197 tokens of 16 heads of 72) 220 us, 49 TFLOP/s of the 154 of a large product: 72 elements and 197 keys are
+// clock that their power leaves (1.8 GHz): 8192 tokens of 32 heads of 128, bf16, 607 us, 906 TFLOP/s of the 1123 of a large
+// matrix product; with a window of 2048, 16 384 tokens of 8 heads, 172 us, 751.  Single tokens are bound by memory: 48 over
+// caches of up to 16 000 positions 364 us, 4.3 TB/s of a large copy's 4.6; one over 131 070 136 us, of which 14 join 256
+// pieces.  fp32 (61 x 197 tokens of 16 heads of 72) 211 us, 51 TFLOP/s of the 154 of a large product: 72 elements and 197 keys are
 // padded to 96 and 224, the last 69 rows of a sequence to 96.
 //
 // P is rounded to bf16 where it meets bf16 values, to the nearest: that, and the result's own rounding, are 2.2e-3 of a
@@ -329,8 +329,8 @@ __global__ __launch_bounds__(256, (DP <= 128 ? 2 : 1)) void k_attention(Args a) 
 }
 
 // The pieces of a row joined in their order.  What is wild in one, a key's value that the row sees, stays so if its weight
-// underflows.  WAVES = 1: a wave a row, for up to 32 pieces; 4: a workgroup a row, every
-// fourth piece to a wave.  4 elements to a lane.
+// underflows.  WAVES = 1: a wave a row, for up to 32 pieces; 4: a workgroup a row, every fourth piece to a wave.  4 elements
+// to a lane.
 template <typename T, int DP, int WAVES>
 __global__ __launch_bounds__(256) void k_join(Args a, int height, int tile) {
   __shared__ float weights[4][64], of_wave[4];

@@ -6,11 +6,13 @@
 // That is seven products of a pair for five: the scores and g V^T are computed twice.  bf16: nine, they are computed once more
 // for an exact g . out.
 //
-// 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 490 us, 841 TFLOP/s of its three products; k_keys 960 us, 573
-// of its four, 32 % of the matrix units' cycles and 40 % of the vector units', which take turns; 30 us to add the pieces.
+// 8192 tokens of 16 heads of 128 on 4 key heads, bf16: k_queries 775 us, 887 TFLOP/s of its five products, 46 % of the matrix
+// units' cycles and 51 % of the vector units', which take turns; k_keys 892 us, 616 of its four, 33 % and 37 %, half of its
+// waves' time a wait; 30 us to add the pieces.
 //
-// bf16: P and dS are rounded to bf16 where they meet bf16 factors: dQ, dK and dV are off by 2.4e-3 of their norm against 64
-// bits, where their own rounding is 1.7e-3.
+// bf16: P and dS are rounded to bf16 where they meet bf16 factors, and nothing else is: dQ, dK and dV are off by what these
+// roundings and their own make, 2.4e-3 of their norm against 64 bits for normal inputs, where their own is 1.7e-3.  Keys with a
+// vector in common, which dS, whose sum is 0, takes out of dQ but its rounding does not: 2.8e-3 (of deviation 1), 8.1e-3 (5).
 #include "slowmo_attention.h"
 
 namespace slowmo {
@@ -114,9 +116,9 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_queries(Arg
   // g . out is off by what `out` was rounded by, and where keys or values have something in common, or few keys have a row's
   // weight, that is far from little beside dS, which is what is left when dP and g . out all but cancel.  A row's dS sums to 0, so
   // the sum of P (dP - g . out) is what g . out is off by.  bf16: a first pass, of the two products that dS takes, is for that
-  // sum alone (2048 causal tokens, D = 128, keys and values around a vector of deviation 1 each: dQ off by 2.9e-3 of
-  // its norm, 4.4e-2 with g . out as it is, 3.5e-2 where only rows are mended that it is 2^-8 of the sum of |dS| off in).  Five
-  // products for three: the gradient's call for 8192 tokens of 16 heads of 128 takes 1932 us for 1659.  fp32: the pass that
+  // sum alone (2048 causal tokens, D = 128, keys and values around a vector of deviation 1 each: dQ off by 2.8e-3 of
+  // its norm, which is the rounding of dS alone; 1.5e-2 where only rows are mended that it is 2^-8 of the sum of |dS| off in).
+  // Five products for three: a step of 8192 tokens of 16 heads of 128 takes 1967 us for 1677.  fp32: the pass that
   // forms dQ sums it too, and is made again where it is more than 2^-21 of the sum of |dS|: dQ is then nearer 64 bits than
   // that of elementary fp32 operations is.
   constexpr bool kMends = sizeof(T) == 4;
