@@ -71,7 +71,7 @@ slowmo_status slowmo_attention(const slowmo_attention_config *cfg, int32_t batch
  * dK and dV summed over the query heads that share a key head.  All sums run in an order
  * fixed by the sizes.  g out is taken of the rounded result and mended by the sum of the row's dS: bf16 in every row, fp32
  * where it is more than 2^-21 of the sum of |dS|.
- *   g, q, k, v, out, lse : of the forward call (lse is wanted here)
+ *   g, q, k, v, out, lse : of the forward call (lse is wanted here), over these very keys: a row's P sums to 1
  *   dq, dk, dv : written; may overlap no input and not one another.  Keys that no query sees: zeros
  *   workspace  : device, 16-byte aligned, slowmo_attention_backward_bytes() long
  * Errors: ARG, ALIGN, NOMEM (workspace too small), HIP.

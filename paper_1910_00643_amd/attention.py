@@ -195,7 +195,8 @@ class Attention(_Holder):
         return out, lse
 
     def backward(self, g, q, k, v, out, lse, offsets, k_offsets=None):
-        """(dq, dk, dv) from the gradient of forward's result, its inputs and what it returned."""
+        """(dq, dk, dv) from the gradient of forward's result, its inputs and what it returned for them: `out` and `lse` of more
+        keys than these, joined from several calls, are not meant, since dS of a row is taken to sum to 0."""
         device = self._device(q)
         if g.shape != q.shape or out.shape != q.shape or v.shape != k.shape:
             raise ValueError("g and out must have q's shape, v must have k's")

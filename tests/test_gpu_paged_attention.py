@@ -447,3 +447,26 @@ def test_without_a_causal_mask(dtype, window, sinks):
                             sinks=sinks)
         U.near(out[s], want["out"], tol["out"] * 1.01, "out")
         U.near(lse[s], want["lse"], tol["lse"], "lse")
+
+
+@pytest.mark.parametrize("columns", [300, 8192])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_table_far_wider_than_its_sequences(dtype, columns):
+    """As a program has it that captures its steps for the longest text it accepts: how the keys are cut follows the table's
+    width."""
+    g = torch.Generator(device=DEV).manual_seed(24)
+    new, lengths = [1, 1, 0, 1, 30, 1], [4700, 17, 5, 1, 900, 2048]
+    pages, total = _paged(g, lengths, 16, columns=columns)
+    kc, vc = (torch.randn(total, 16, 2, 128, device=DEV, generator=g).to(U.TD[dtype]) for _ in range(2))
+    q = U.rows(g, sum(new), 8, 128, dtype, times=2.0)
+    at = U.offsets_of(new)
+    for window, sinks in ((None, 0), (700, 4)):
+        op = _P().PagedAttention(128, dtype=dtype, window=window, sinks=sinks)
+        out, lse = op.forward(q, kc, vc, pages, torch.tensor(lengths, device=DEV), torch.tensor(at, device=DEV), return_lse=True)
+        for b, m in enumerate(lengths):
+            s = slice(at[b], at[b + 1])
+            if not new[b]:
+                continue
+            want, tol = U.dense(q[s], _gathered(kc, pages[b], m), _gathered(vc, pages[b], m), dtype, window=window, sinks=sinks)
+            U.near(out[s], want["out"], tol["out"] * 1.01, "out")
+            U.near(lse[s], want["lse"], tol["lse"], "lse")
